@@ -284,7 +284,8 @@ def prepare(case, seed):
     if case["kind"] in ("logprobs", "loss"):
         R, V = case["rows"], case["vocab"]
         s["x"], s["tokens"] = _logits(case, seed)
-        s["logprob"], s["entropy"], s["lse"] = (torch.zeros(R, device="cuda") for _ in range(3))
+        s["logprob"], s["entropy"] = torch.zeros(R, device="cuda"), torch.zeros(R, device="cuda")
+        s["norm"] = torch.zeros(R, 2, device="cuda")     # a row's maximum, and the logarithm of its sum relative to it
         if case["kind"] == "loss":
             g = _gen(seed, 6)
             s["g_logprob"], s["g_entropy"] = _normal(g, R), _normal(g, R, std=0.1)
@@ -377,13 +378,13 @@ def _own_logprobs(s):
         s["ws"] = torch.empty(jf.token_logprobs_ws_bytes(c["rows"], c["vocab"], k), dtype=torch.uint8, device="cuda")
     if c["kind"] == "loss":
         jf.token_logprobs(s["x"], s["ws"], d_tokens=s["tokens"], d_logprob=s["logprob"], d_entropy=s["entropy"],
-                          d_lse=s["lse"])
-        jf.token_logprobs_grad(s["x"], s["lse"], s["grad"], d_tokens=s["tokens"], d_entropy=s["entropy"],
+                          d_norm=s["norm"])
+        jf.token_logprobs_grad(s["x"], s["norm"], s["grad"], d_tokens=s["tokens"], d_entropy=s["entropy"],
                                d_g_logprob=s["g_logprob"], d_g_entropy=s["g_entropy"])
         return [s["logprob"], s["entropy"], s["grad"]]
     jf.token_logprobs(s["x"], s["ws"], d_tokens=s["tokens"], k=k, d_logprob=s["logprob"], d_entropy=s["entropy"],
-                      d_lse=s["lse"], d_top_ids=s["top_ids"], d_top_logprob=s["top_logprob"])
-    return [s["logprob"], s["entropy"], s["lse"], s["top_ids"], s["top_logprob"]]
+                      d_norm=s["norm"], d_top_ids=s["top_ids"], d_top_logprob=s["top_logprob"])
+    return [s["logprob"], s["entropy"], s["norm"], s["top_ids"], s["top_logprob"]]
 
 
 # ---- the plain forms ------------------------------------------------------------------
@@ -514,9 +515,9 @@ def _plain_logprobs(s):
     m = x.amax(1, keepdim=True)
     e = torch.exp(x - m)
     total = e.sum(1, keepdim=True)
-    lse = m + torch.log(total)
     p = e / total
-    lp = x - lse
+    norm = torch.cat([m, torch.log(total)], 1)
+    lp = x - m - norm[:, 1:]
     entropy = -torch.where(p > 0, p * lp, 0.0).sum(1)
     logprob = torch.where(tok >= 0, lp.gather(1, tok.clamp(min=0)[:, None])[:, 0], 0.0)
     if c["kind"] == "loss":
@@ -526,7 +527,7 @@ def _plain_logprobs(s):
         return [logprob, entropy, g.to(s["x"].dtype)]
     best, ids = torch.sort(x, dim=1, descending=True, stable=True)    # ties: the lowest index first
     k = c["k"]
-    return [logprob, entropy, lse[:, 0], ids[:, :k].to(torch.int32), best[:, :k] - lse]
+    return [logprob, entropy, norm, ids[:, :k].to(torch.int32), best[:, :k] - m - norm[:, 1:]]
 
 
 # ---- what a pass cannot do without ----------------------------------------------------
@@ -665,7 +666,8 @@ def _exact_logprobs(case, seed):
         grad[torch.arange(len(tok), device="cuda"), tok.clamp(min=0).long()] += g_lp * (tok >= 0)
         return [logprob, entropy, grad + (torch.special.entr(p) - p * entropy[:, None]) * g_h[:, None]]
     top = torch.topk(lp, case["k"], 1).values
-    return [logprob, entropy, torch.logsumexp(x.double(), 1), None, top]
+    m = x.double().max(1).values
+    return [logprob, entropy, torch.stack([m, torch.logsumexp(x.double(), 1) - m], 1), None, top]
 
 
 def exact(case, seed):
