@@ -56,7 +56,9 @@ typedef enum {
   JF_E_STATE = -6     /* call not valid in the model's current state   */
 } jf_status;
 
-typedef enum { JF_F32 = 0, JF_BF16 = 1 } jf_dtype;
+/* JF_E4M3 (OCP 8-bit floating point, largest value 448) is a type of the paged
+ * caches of jf_kv_append / jf_kv_read / jf_attention_kv8 only. */
+typedef enum { JF_F32 = 0, JF_BF16 = 1, JF_E4M3 = 2 } jf_dtype;
 
 /* Decoder shape: RMSNorm (gain), RoPE (rotate-half pairs i, i + head_dim/2,
  * inverse frequency rope_base^(-2i/head_dim)), grouped-query attention with
@@ -124,6 +126,9 @@ typedef struct {
 #define JF_FLAG_SYNC 4      /* a wait between the phases of a fused launch gave
                                up (the device did not run all its workgroups
                                at once); the step's outputs are invalid      */
+
+#define JF_FLAG_BAD_PAGE 8 /* a page table entry was outside [0, n_pages); that
+                              page was neither read nor written            */
 
 typedef struct jf_model jf_model;
 typedef void *jf_stream; /* hipStream_t; NULL is the null stream */
@@ -374,6 +379,136 @@ jf_status jf_trajectory_select(const int32_t *d_traj, const int32_t *d_len,
                                int32_t w, const int32_t *d_t_num,
                                int32_t *d_sel, int32_t *d_unconv,
                                jf_stream stream);
+
+/* ---- batches of sequences over a paged cache --------------------------------
+ * Component calls for programs that decode many sequences: they append rows
+ * to a paged cache (rotating them), attend over an 8-bit one and read it back.
+ * A layer's cache is a pool of n_pages pages of 64 tokens, shared by all
+ * sequences; one call works on one layer.
+ *
+ * Rows (queries, keys, values, outputs) of all sequences lie one after the
+ * other: rows d_row_start[s] .. d_row_start[s + 1] - 1 belong to sequence s,
+ * which has d_ctx[s] committed tokens, and row i of them has slot
+ * d_ctx[s] + i.  Slot t is token t % 64 of physical page
+ * d_page_table[s * table_stride + t / 64].  Rows before d_row_start[0] and
+ * from d_row_start[n_seqs] on (padding) are neither read nor written.
+ *
+ * The three arrays stay on the device, so a captured call takes new lengths at
+ * every replay; the host gives bounds: n_rows rows in the row tensors, at most
+ * max_rows rows a sequence, at most max_ctx slots a sequence (committed and
+ * rows; at most 64 table_stride).  What the device holds beyond these bounds
+ * is not followed: such a sequence's rows are left as they were and
+ * JF_FLAG_CAPACITY is raised; a page table entry outside [0, n_pages) raises
+ * JF_FLAG_BAD_PAGE and its tokens are skipped.  d_flags (optional, one int32)
+ * gets these bits ORed in; the caller clears it.  n_seqs, n_rows or max_rows
+ * = 0 does nothing.  n_seqs times the workgroups that max_rows and max_ctx
+ * call for must stay within 2^22 (JF_E_CAPACITY). */
+typedef struct {
+  int32_t n_seqs, n_rows, max_rows, max_ctx, n_pages, table_stride;
+  const int32_t *d_row_start;  /* [n_seqs + 1] */
+  const int32_t *d_ctx;        /* [n_seqs] */
+  const int32_t *d_page_table; /* [n_seqs][table_stride] */
+} jf_batch;
+
+/* Bytes of one page of one layer.  JF_F32 / JF_BF16: the page of
+ * jf_model_load (K [G][64][hd], then V transposed [G][hd][64]), so such a pool
+ * is also what jf_attention reads.  JF_E4M3: codes of the keys [G][64 hd] and
+ * of the values [G][64 hd], then fp32 scales [G][2] (keys, values; powers of
+ * two: a stored value is its code times its scale), padded to a multiple of
+ * 128 bytes.  A head's codes are hd / 16 pieces of 64 lanes x 16 bytes, the
+ * order in which the matrix cores take them: byte b of lane l is at
+ * (b / 16) * 1024 + l * 16 + b % 16, and
+ *   key of token t, dim i:   l = t % 16 + 16 (i / (hd / 4)),
+ *                            b = (t / 16) (hd / 4) + i % (hd / 4)
+ *   value of token t, dim i: l = i % 16 + 16 ((t / 4) % 4),
+ *                            b = 16 (i / 16) + 4 (t / 16) + t % 4.
+ * 0 for an unknown type, head_dim not in {32, 64, 128} or n_kv_heads < 1. */
+size_t jf_kv_page_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t kv_dtype);
+
+/* Appends the rows' keys and values to the cache (type kv_dtype), and rotates
+ * the queries.  d_k, d_v [n_rows][n_kv_heads * head_dim] and d_q (optional)
+ * [n_rows][n_heads * head_dim] are rows of x_dtype (JF_F32 or JF_BF16), ld_*
+ * elements apart (views into one fused projection, for instance).
+ * Rotation: rope_base > 1 turns dims (i, i + head_dim / 2) of queries and keys
+ * by p * rope_base^(-2 i / head_dim), p = d_pos[row] (rows of a tree share
+ * positions) or, for d_pos NULL, the row's slot; rope_base 0 leaves them.
+ * d_q_out gets the queries as activation planes [n_rows][n_heads][head_dim] of
+ * act_dtype, as the attention calls take them.
+ * JF_E4M3: the keys and the values of one head in one page share a scale.  A
+ * call that appends into a page takes the smallest power of two that brings
+ * the finite new values there to 448 or less (1 if they are all 0) or, where
+ * the page keeps earlier tokens (slots below d_ctx), the scale it has if that
+ * is larger; if the scale grows, the kept tokens' codes are rounded anew on
+ * it.  Codes round to nearest, ties to even; infinities saturate at 448 times
+ * the scale and NaN stays NaN.  A scale never shrinks until the page is
+ * appended to from its first token on.
+ * Rows dropped by a verification need no call: the next append at the shorter
+ * d_ctx overwrites them.  Slots that no row names keep what they hold.
+ * d_kv and d_q_out must start on 16-byte boundaries.  No two sequences of a
+ * call may write into the same page. */
+jf_status jf_kv_append(const jf_batch *batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t kv_dtype,
+                       int32_t x_dtype, int32_t act_dtype, const void *d_q, int64_t ld_q, const void *d_k,
+                       int64_t ld_k, const void *d_v, int64_t ld_v, const int32_t *d_pos, double rope_base,
+                       void *d_kv, void *d_q_out, int32_t *d_flags, jf_stream stream);
+
+/* Reads slots d_ctx[s] .. d_ctx[s] + rows - 1 back as the values they hold:
+ * d_k, d_v rows [n_rows][n_kv_heads * head_dim] of x_dtype, ld_* elements
+ * apart (JF_BF16 holds an e4m3 value exactly). */
+jf_status jf_kv_read(const jf_batch *batch, int32_t n_kv_heads, int32_t head_dim, int32_t kv_dtype, int32_t x_dtype,
+                     const void *d_kv, void *d_k, int64_t ld_k, void *d_v, int64_t ld_v, int32_t *d_flags,
+                     jf_stream stream);
+
+/* Attention over a JF_E4M3 cache that already holds the rows' keys and values:
+ * row i of sequence s sees slots [0, d_ctx[s]) and in-step slot d_ctx[s] + j
+ * iff bit j of d_vis[row][JF_VIS_WORDS] is set (d_vis NULL: j <= i).  A row
+ * that sees nothing gets zeros; what a slot holds does not reach a row that
+ * does not see it, NaN included.  d_q [n_rows][n_heads][head_dim] and d_out
+ * are activation planes of act_dtype, d_out in the GEMM-input layout of
+ * [n_rows][n_heads * head_dim] (a multiple of 128 columns); max_rows <=
+ * JF_MAX_ROWS.  d_q, d_kv, d_out and d_ws must start on 16-byte boundaries;
+ * d_ws holds jf_attention_kv8_ws_bytes(...) bytes, needs no clearing and may
+ * be shared by calls that do not overlap. */
+size_t jf_attention_kv8_ws_bytes(const jf_batch *batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+jf_status jf_attention_kv8(const jf_batch *batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                           int32_t act_dtype, const void *d_q, const void *d_kv, const uint64_t *d_vis, void *d_out,
+                           void *d_ws, int32_t *d_flags, jf_stream stream);
+
+/* ---- log probabilities ------------------------------------------------------
+ * Of logits d_logits [R][V] (JF_F32 as the steps and jf_packed_forward return
+ * them, or JF_BF16), rows ld elements apart, with p = softmax of a row.  Each
+ * output may be NULL:
+ *   d_logprob[R]: log p of token d_tokens[row]; 0 where that is -1 (a row
+ *     without a token), NaN for any other id outside [0, V);
+ *   d_entropy[R]: -sum p log p;
+ *   d_norm[R][2]: the row's maximum m and log sum e^(x - m), whose sum is the
+ *     logarithm of the softmax's denominator (kept apart: no digits are lost
+ *     at large offsets), which the gradient takes;
+ *   d_top_ids, d_top_logprob [R][k], 0 <= k <= JF_MAX_TOP: the k largest
+ *     logits' ids and log probabilities in order (ties: lowest id first).
+ * A logit of -inf has p = 0 and is no alternative; places beyond the finite
+ * logits get id -1 and -inf.  A row that is no distribution (all -inf, +inf or
+ * NaN among its logits) gets NaN everywhere and ids -1.  d_ws, 16-byte
+ * aligned, holds jf_token_logprobs_ws_bytes(R, V, k) bytes, which are enough
+ * for fewer rows too, and needs no clearing.
+ * R = 0 does nothing.  V <= 2^30, R <= 2^22. */
+#define JF_MAX_TOP 32
+size_t jf_token_logprobs_ws_bytes(int32_t R, int32_t V, int32_t k);
+jf_status jf_token_logprobs(int32_t R, int32_t V, int32_t dtype, const void *d_logits, int64_t ld,
+                            const int32_t *d_tokens, int32_t k, float *d_logprob, float *d_entropy, float *d_norm,
+                            int32_t *d_top_ids, float *d_top_logprob, void *d_ws, jf_stream stream);
+
+/* Gradient of sum(d_g_logprob * logprob + d_g_entropy * entropy) to the
+ * logits, d_grad [R][V] of their type, rows ld_grad elements apart:
+ *   g (1[j = token] - p_j) - h p_j (log p_j + entropy).
+ * d_norm and d_entropy are those of jf_token_logprobs on the same logits.
+ * d_g_logprob NULL: g = 0 (else d_tokens is needed); d_g_entropy NULL: h = 0
+ * (else d_entropy is needed).  Rows with g = h = 0 get zeros, rows whose token
+ * is -1 have g = 0.  d_grad may be d_logits (same ld): in place.  Writes only
+ * columns [0, V). */
+jf_status jf_token_logprobs_grad(int32_t R, int32_t V, int32_t dtype, const void *d_logits, int64_t ld,
+                                 const int32_t *d_tokens, const float *d_norm, const float *d_entropy,
+                                 const float *d_g_logprob, const float *d_g_entropy, void *d_grad, int64_t ld_grad,
+                                 jf_stream stream);
 
 #ifdef __cplusplus
 }

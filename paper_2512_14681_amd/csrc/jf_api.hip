@@ -943,3 +943,230 @@ extern "C" jf_status jf_trajectory_select(const int32_t* d_traj, const int32_t* 
                              (hipStream_t)stream));
   return JF_OK;
 }
+
+// ---- batches of sequences over a paged cache --------------------------------------------
+static_assert(kFlagCapacity == JF_FLAG_CAPACITY && kFlagBadPage == JF_FLAG_BAD_PAGE && kKvE4m3 == JF_E4M3 &&
+                  kMaxTop == JF_MAX_TOP,
+              "constants of jf.h");
+constexpr int64_t kMaxBlocks = (int64_t)1 << 22;  // workgroups of one launch
+
+static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+static bool head_dim_ok(int hd) { return hd == 32 || hd == 64 || hd == 128; }
+
+// Checks a batch descriptor and the head counts; *none: nothing to do.
+static jf_status check_batch(const jf_batch* b, int n_heads, int n_kv_heads, int head_dim, int32_t* d_flags,
+                             BatchArgs* out, bool* none) {
+  if (!b) return fail(JF_E_INVAL, "batch is null");
+  if (b->n_seqs < 0 || b->n_rows < 0 || b->max_rows < 0 || b->max_ctx < 0 || b->n_pages < 0 || b->table_stride < 0)
+    return fail(JF_E_INVAL, "negative count in the batch");
+  if (n_heads < 1 || n_kv_heads < 1 || n_heads > 65536 || n_heads % n_kv_heads)
+    return fail(JF_E_SHAPE, "bad head counts %d, %d", n_heads, n_kv_heads);
+  if (!head_dim_ok(head_dim)) return fail(JF_E_SHAPE, "head_dim must be 32, 64 or 128");
+  if (b->max_ctx > (1 << 30) || b->n_rows > (1 << 30)) return fail(JF_E_CAPACITY, "max_ctx and n_rows go up to 2^30");
+  if ((int64_t)b->max_ctx > (int64_t)64 * b->table_stride)
+    return fail(JF_E_CAPACITY, "max_ctx %d needs more than table_stride %d pages", b->max_ctx, b->table_stride);
+  if (b->max_rows > b->max_ctx) return fail(JF_E_CAPACITY, "max_rows %d exceeds max_ctx %d", b->max_rows, b->max_ctx);
+  *none = b->n_seqs == 0 || b->n_rows == 0 || b->max_rows == 0;
+  if (!*none && (!b->d_row_start || !b->d_ctx || !b->d_page_table)) return fail(JF_E_INVAL, "null array in the batch");
+  *out = BatchArgs{b->n_seqs, b->n_rows,      b->max_rows, b->max_ctx,      b->n_pages,
+                   b->table_stride, b->d_row_start, b->d_ctx,    b->d_page_table, d_flags};
+  return JF_OK;
+}
+static jf_status check_blocks(int64_t per_seq, int n_seqs) {
+  if (per_seq > kMaxBlocks || per_seq * n_seqs > kMaxBlocks)
+    return fail(JF_E_CAPACITY, "%d sequences of %lld workgroups exceed the %lld of a launch", n_seqs,
+                (long long)per_seq, (long long)kMaxBlocks);
+  return JF_OK;
+}
+
+extern "C" size_t jf_kv_page_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t kv_dtype) {
+  if (n_kv_heads < 1 || !head_dim_ok(head_dim)) return 0;
+  if (kv_dtype == JF_E4M3) return ((size_t)2 * n_kv_heads * kPage * head_dim + (size_t)8 * n_kv_heads + 127) / 128 * 128;
+  if (kv_dtype != JF_F32 && kv_dtype != JF_BF16) return 0;
+  return (size_t)2 * n_kv_heads * kPage * head_dim * (kv_dtype == JF_BF16 ? 2 : 4);
+}
+
+// Whether four elements from any multiple of four of a row on can be read at once.
+static bool vector4(const void* p, int64_t ld, size_t esz) {
+  return ((uintptr_t)p % (4 * esz)) == 0 && ld % 4 == 0;
+}
+
+extern "C" jf_status jf_kv_append(const jf_batch* batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                  int32_t kv_dtype, int32_t x_dtype, int32_t act_dtype, const void* d_q, int64_t ld_q,
+                                  const void* d_k, int64_t ld_k, const void* d_v, int64_t ld_v, const int32_t* d_pos,
+                                  double rope_base, void* d_kv, void* d_q_out, int32_t* d_flags, jf_stream stream) {
+  AppendArgs a{};
+  bool none = false;
+  jf_status s = check_batch(batch, n_heads, n_kv_heads, head_dim, d_flags, &a.b, &none);
+  if (s != JF_OK) return s;
+  if (kv_dtype != JF_F32 && kv_dtype != JF_BF16 && kv_dtype != JF_E4M3)
+    return fail(JF_E_DTYPE, "cache type %d unsupported", kv_dtype);
+  if (x_dtype != JF_F32 && x_dtype != JF_BF16) return fail(JF_E_DTYPE, "row type %d unsupported", x_dtype);
+  if (act_dtype != JF_F32 && act_dtype != JF_BF16) return fail(JF_E_DTYPE, "activation type %d unsupported", act_dtype);
+  if (!(rope_base == 0.0 || (rope_base > 1.0 && std::isfinite(rope_base))))
+    return fail(JF_E_INVAL, "rope_base must be 0 or above 1");
+  if (none) return JF_OK;
+  if (!d_k || !d_v || !d_kv || (d_q && !d_q_out)) return fail(JF_E_INVAL, "null pointer argument");
+  if (!aligned16(d_kv) || (d_q && !aligned16(d_q_out)))
+    return fail(JF_E_INVAL, "d_kv and d_q_out must start on 16-byte boundaries");
+  if (ld_k < (int64_t)n_kv_heads * head_dim || ld_v < (int64_t)n_kv_heads * head_dim ||
+      (d_q && ld_q < (int64_t)n_heads * head_dim))
+    return fail(JF_E_SHAPE, "row strides are shorter than the rows");
+  const int64_t cache = ((int64_t)batch->max_rows + kPage - 2) / kPage + 1;
+  s = check_blocks(cache * n_kv_heads + ((int64_t)batch->max_rows * ((n_heads + 3) / 4) * (head_dim / 8) + 255) / 256,
+                   batch->n_seqs);
+  if (s != JF_OK) return s;
+  const size_t esz = x_dtype == JF_BF16 ? 2 : 4;
+  a.H = n_heads; a.G = n_kv_heads; a.hd = head_dim;
+  a.q = d_q; a.k = d_k; a.v = d_v;
+  a.ld_q = (size_t)ld_q; a.ld_k = (size_t)ld_k; a.ld_v = (size_t)ld_v;
+  a.vec_q = vector4(d_q, ld_q, esz); a.vec_k = vector4(d_k, ld_k, esz); a.vec_v = vector4(d_v, ld_v, esz);
+  a.pos = d_pos;
+  a.rotate = rope_base > 0.0;
+  if (a.rotate)
+    for (int i = 0; i < head_dim / 2; ++i) a.freq[i] = std::pow(rope_base, -(2.0 * i) / head_dim) / (2.0 * M_PI);
+  a.kv = d_kv;
+  a.page_bytes = jf_kv_page_bytes(n_kv_heads, head_dim, kv_dtype);
+  a.q_out = d_q_out;
+  a.q_plane = (size_t)batch->n_rows * n_heads * head_dim;
+  HIP_TRY(launch_kv_append(kv_dtype, x_dtype, act_dtype, a, (hipStream_t)stream));
+  return JF_OK;
+}
+
+extern "C" jf_status jf_kv_read(const jf_batch* batch, int32_t n_kv_heads, int32_t head_dim, int32_t kv_dtype,
+                                int32_t x_dtype, const void* d_kv, void* d_k, int64_t ld_k, void* d_v, int64_t ld_v,
+                                int32_t* d_flags, jf_stream stream) {
+  ReadArgs a{};
+  bool none = false;
+  jf_status s = check_batch(batch, n_kv_heads, n_kv_heads, head_dim, d_flags, &a.b, &none);
+  if (s != JF_OK) return s;
+  if (kv_dtype != JF_F32 && kv_dtype != JF_BF16 && kv_dtype != JF_E4M3)
+    return fail(JF_E_DTYPE, "cache type %d unsupported", kv_dtype);
+  if (x_dtype != JF_F32 && x_dtype != JF_BF16) return fail(JF_E_DTYPE, "row type %d unsupported", x_dtype);
+  if (none) return JF_OK;
+  if (!d_kv || !d_k || !d_v) return fail(JF_E_INVAL, "null pointer argument");
+  if (!aligned16(d_kv)) return fail(JF_E_INVAL, "d_kv must start on a 16-byte boundary");
+  if (ld_k < (int64_t)n_kv_heads * head_dim || ld_v < (int64_t)n_kv_heads * head_dim)
+    return fail(JF_E_SHAPE, "row strides are shorter than the rows");
+  s = check_blocks((((int64_t)batch->max_rows + kPage - 2) / kPage + 1) * n_kv_heads, batch->n_seqs);
+  if (s != JF_OK) return s;
+  a.G = n_kv_heads; a.hd = head_dim;
+  a.kv = d_kv;
+  a.page_bytes = jf_kv_page_bytes(n_kv_heads, head_dim, kv_dtype);
+  a.k = d_k; a.v = d_v;
+  a.ld_k = (size_t)ld_k; a.ld_v = (size_t)ld_v;
+  HIP_TRY(launch_kv_read(kv_dtype, x_dtype, a, (hipStream_t)stream));
+  return JF_OK;
+}
+
+// Split partials: outputs, then (max, sum); the plan depends on the batch's host counts alone.
+static size_t kv8_part_floats(const Kv8Args& a) { return (size_t)a.splits * a.b.n_rows * a.H; }
+
+static jf_status kv8_args(const jf_batch* batch, int n_heads, int n_kv_heads, int head_dim, int32_t* d_flags,
+                          Kv8Args* a, bool* none) {
+  jf_status s = check_batch(batch, n_heads, n_kv_heads, head_dim, d_flags, &a->b, none);
+  if (s != JF_OK) return s;
+  if ((int64_t)n_heads * head_dim % 128) return fail(JF_E_SHAPE, "n_heads * head_dim must be a multiple of 128");
+  if (batch->max_rows > kMaxRows) return fail(JF_E_CAPACITY, "max_rows must be at most %d", kMaxRows);
+  if (*none) return JF_OK;
+  a->H = n_heads; a->G = n_kv_heads; a->hd = head_dim;
+  kv8_plan(*a);
+  s = check_blocks(std::max<int64_t>((int64_t)n_kv_heads * a->groups * a->splits,
+                                     ((int64_t)batch->max_rows * n_heads * (head_dim / 4) + 255) / 256),
+                   batch->n_seqs);
+  return s;
+}
+
+extern "C" size_t jf_attention_kv8_ws_bytes(const jf_batch* batch, int32_t n_heads, int32_t n_kv_heads,
+                                            int32_t head_dim) {
+  Kv8Args a{};
+  bool none = false;
+  if (kv8_args(batch, n_heads, n_kv_heads, head_dim, nullptr, &a, &none) != JF_OK) return 0;
+  if (none || a.splits == 1) return 256;
+  return kv8_part_floats(a) * (head_dim + 2) * 4 + 256;
+}
+
+extern "C" jf_status jf_attention_kv8(const jf_batch* batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                      int32_t act_dtype, const void* d_q, const void* d_kv, const uint64_t* d_vis,
+                                      void* d_out, void* d_ws, int32_t* d_flags, jf_stream stream) {
+  if (act_dtype != JF_F32 && act_dtype != JF_BF16) return fail(JF_E_DTYPE, "activation type %d unsupported", act_dtype);
+  Kv8Args a{};
+  bool none = false;
+  jf_status s = kv8_args(batch, n_heads, n_kv_heads, head_dim, d_flags, &a, &none);
+  if (s != JF_OK) return s;
+  if (none) return JF_OK;
+  if (!d_q || !d_kv || !d_out || !d_ws) return fail(JF_E_INVAL, "null pointer argument");
+  if (!aligned16(d_q) || !aligned16(d_kv) || !aligned16(d_out) || !aligned16(d_ws))
+    return fail(JF_E_INVAL, "d_q, d_kv, d_out and d_ws must start on 16-byte boundaries");
+  a.q = d_q;
+  a.q_plane = (size_t)batch->n_rows * n_heads * head_dim;
+  a.kv = (const uint8_t*)d_kv;
+  a.page_bytes = jf_kv_page_bytes(n_kv_heads, head_dim, JF_E4M3);
+  a.vis = d_vis;
+  a.out = d_out;
+  a.out_plane = (size_t)(batch->n_rows + 15) / 16 * 16 * n_heads * head_dim;
+  a.o_part = (float*)d_ws;
+  a.ml_part = a.o_part + kv8_part_floats(a) * head_dim;
+  HIP_TRY(launch_attention_kv8(act_dtype, a, (hipStream_t)stream));
+  return JF_OK;
+}
+
+// ---- log probabilities -------------------------------------------------------------------
+static jf_status check_logits(int R, int V, int dtype, int64_t ld) {
+  if (dtype != JF_F32 && dtype != JF_BF16) return fail(JF_E_DTYPE, "dtype %d unsupported", dtype);
+  if (R < 0 || V < 1) return fail(JF_E_SHAPE, "need R >= 0 and V >= 1");
+  if (R > (1 << 22) || V > (1 << 30)) return fail(JF_E_CAPACITY, "R goes up to 2^22 and V to 2^30");
+  if (ld < V) return fail(JF_E_SHAPE, "row stride %lld is shorter than V = %d", (long long)ld, V);
+  return JF_OK;
+}
+
+extern "C" size_t jf_token_logprobs_ws_bytes(int32_t R, int32_t V, int32_t k) {
+  if (R < 1 || V < 1 || k < 0 || k > JF_MAX_TOP) return 0;
+  return logprob_parts(R, V) * (16 + (size_t)8 * k) + 256;
+}
+
+extern "C" jf_status jf_token_logprobs(int32_t R, int32_t V, int32_t dtype, const void* d_logits, int64_t ld,
+                                       const int32_t* d_tokens, int32_t k, float* d_logprob, float* d_entropy,
+                                       float* d_norm, int32_t* d_top_ids, float* d_top_logprob, void* d_ws,
+                                       jf_stream stream) {
+  jf_status s = check_logits(R, V, dtype, ld);
+  if (s != JF_OK) return s;
+  if (k < 0 || k > JF_MAX_TOP) return fail(JF_E_SHAPE, "k must be in [0, %d]", JF_MAX_TOP);
+  if (R == 0) return JF_OK;
+  if (!d_logits || !d_ws || (d_logprob && !d_tokens)) return fail(JF_E_INVAL, "null pointer argument");
+  if (!aligned16(d_ws)) return fail(JF_E_INVAL, "d_ws must start on a 16-byte boundary");
+  LogprobArgs a{};
+  a.R = R; a.V = V; a.k = d_top_ids || d_top_logprob ? k : 0;
+  a.x = d_logits; a.ld = (size_t)ld;
+  a.tokens = d_tokens;
+  a.logprob = d_logprob; a.entropy = d_entropy; a.norm = d_norm; a.top_logprob = d_top_logprob; a.top_ids = d_top_ids;
+  a.splits = logprob_splits(R, V);
+  a.part = (float*)d_ws;
+  a.top_part = (uint64_t*)(a.part + (size_t)R * a.splits * 4);
+  HIP_TRY(launch_logprobs(dtype, a, (hipStream_t)stream));
+  return JF_OK;
+}
+
+extern "C" jf_status jf_token_logprobs_grad(int32_t R, int32_t V, int32_t dtype, const void* d_logits, int64_t ld,
+                                            const int32_t* d_tokens, const float* d_norm, const float* d_entropy,
+                                            const float* d_g_logprob, const float* d_g_entropy, void* d_grad,
+                                            int64_t ld_grad, jf_stream stream) {
+  jf_status s = check_logits(R, V, dtype, ld);
+  if (s != JF_OK) return s;
+  if (ld_grad < V) return fail(JF_E_SHAPE, "row stride %lld is shorter than V = %d", (long long)ld_grad, V);
+  if (R == 0) return JF_OK;
+  if (!d_logits || !d_norm || !d_grad || (d_g_logprob && !d_tokens) || (d_g_entropy && !d_entropy))
+    return fail(JF_E_INVAL, "null pointer argument");
+  if (d_grad == d_logits && ld_grad != ld) return fail(JF_E_INVAL, "in place needs ld_grad = ld");
+  if (((int64_t)V + 4095) / 4096 * R > kMaxBlocks)
+    return fail(JF_E_CAPACITY, "R = %d rows of V = %d exceed one launch", R, V);
+  LogprobGradArgs a{};
+  a.R = R; a.V = V;
+  a.x = d_logits; a.ld = (size_t)ld; a.ld_g = (size_t)ld_grad;
+  a.tokens = d_g_logprob ? d_tokens : nullptr;
+  a.norm = d_norm; a.entropy = d_g_entropy ? d_entropy : nullptr;
+  a.g_logprob = d_g_logprob; a.g_entropy = d_g_entropy;
+  a.grad = d_grad;
+  HIP_TRY(launch_logprobs_grad(dtype, a, (hipStream_t)stream));
+  return JF_OK;
+}

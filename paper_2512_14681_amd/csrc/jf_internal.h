@@ -271,6 +271,94 @@ hipError_t launch_fill_int(int32_t* p, int n, int32_t v, hipStream_t stream);  /
 hipError_t launch_to_f32(int dtype, const void* src, float* dst, int n, hipStream_t stream);
 hipError_t launch_copy_int(int32_t* dst, const int32_t* src, hipStream_t stream);
 
+// ---- batches of sequences over one paged cache (jf_batch.h) ----
+constexpr int kFlagCapacity = 2, kFlagBadPage = 8;  // JF_FLAG_* of jf.h
+constexpr int kKvE4m3 = 2;                          // JF_E4M3 of jf.h
+struct BatchArgs {
+  int n_seqs, n_rows, max_rows, max_ctx, n_pages, stride;
+  const int32_t* row_start;  // [n_seqs + 1]
+  const int32_t* ctx;        // [n_seqs]
+  const int32_t* table;      // [n_seqs][stride]
+  int32_t* flags;            // or null
+};
+
+// kvcache.hip
+struct AppendArgs {
+  BatchArgs b;
+  int H, G, hd;
+  const void *q, *k, *v;     // rows [n_rows][ld]; q may be null
+  size_t ld_q, ld_k, ld_v;
+  int vec_q, vec_k, vec_v;   // every four elements from a multiple of 4 are aligned
+  const int32_t* pos;        // [n_rows], or null: a row's slot
+  double freq[64];           // turns per position of each pair (0: no rotation)
+  int rotate;
+  void* kv;
+  size_t page_bytes;
+  void* q_out;               // activation planes [n_rows][H][hd], q_plane apart
+  size_t q_plane;
+  int n_cache, n_q;          // workgroups of a sequence for the cache, for the queries
+};
+hipError_t launch_kv_append(int kv_dtype, int x_dtype, int act_dtype, AppendArgs& a, hipStream_t stream);
+struct ReadArgs {
+  BatchArgs b;
+  int G, hd;
+  const void* kv;
+  size_t page_bytes;
+  void *k, *v;               // rows [n_rows][ld]
+  size_t ld_k, ld_v;
+  int pages;
+};
+hipError_t launch_kv_read(int kv_dtype, int x_dtype, ReadArgs& a, hipStream_t stream);
+
+// attention_kv8.hip
+struct Kv8Args {
+  BatchArgs b;
+  int H, G, hd;
+  const void* q;             // activation planes [n_rows][H][hd]
+  size_t q_plane;
+  const uint8_t* kv;
+  size_t page_bytes;
+  const uint64_t* vis;       // [n_rows][kVisWords], or null (causal)
+  void* out;                 // activation planes, GEMM-input layout of [n_rows][H * hd]
+  size_t out_plane;
+  float* o_part;             // [splits][n_rows * H][hd]
+  float* ml_part;            // [splits][n_rows * H][2]
+  // the plan (kv8_plan)
+  int share;                 // 1: the waves of a workgroup take query tiles of their own, 0: they share the keys
+  int qt;                    // query tiles of a wave
+  int groups;                // workgroups along the query tiles
+  int chunk;                 // pages of a key split
+  int splits;
+};
+void kv8_plan(Kv8Args& a);   // from b, H, G, hd
+hipError_t launch_attention_kv8(int act_dtype, const Kv8Args& a, hipStream_t stream);
+
+// logprobs.hip
+constexpr int kMaxTop = 32;
+struct LogprobArgs {
+  int R, V, k;
+  const void* x;
+  size_t ld;
+  const int32_t* tokens;     // [R] or null
+  float *logprob, *entropy, *norm, *top_logprob;   // each may be null
+  int32_t* top_ids;          // may be null
+  float* part;               // [R][splits][4]
+  uint64_t* top_part;        // [R][splits][k]
+  int splits;
+};
+int logprob_splits(int R, int V);
+size_t logprob_parts(int R, int V);   // R' * logprob_splits(R', V) at most, for all R' <= R
+hipError_t launch_logprobs(int dtype, const LogprobArgs& a, hipStream_t stream);
+struct LogprobGradArgs {
+  int R, V;
+  const void* x;
+  size_t ld, ld_g;
+  const int32_t* tokens;
+  const float *norm, *entropy, *g_logprob, *g_entropy;
+  void* grad;
+};
+hipError_t launch_logprobs_grad(int dtype, const LogprobGradArgs& a, hipStream_t stream);
+
 // trajectory.hip
 hipError_t launch_traj_record(const int32_t* prev, const int32_t* g, int n, int rows, int32_t* out,
                               hipStream_t stream);

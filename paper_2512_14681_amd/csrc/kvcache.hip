@@ -1,0 +1,325 @@
+// Keys and values of a batch of sequences: appended to a paged cache with the
+// position rotation applied on the way (jf_kv_append), and read back
+// (jf_kv_read).
+//
+// Rotation: dims i and i + hd / 2 of a head turn by pos * base^(-2 i / hd).
+// The angle is formed in 64 bits as a number of turns, of which only the
+// fraction is kept, so that far positions lose nothing; sine and cosine are
+// taken in 32 bits.
+//
+// A workgroup takes one head of one page: it alone writes that head's codes
+// and scale there, so the scale needs no other workgroup.  The queries'
+// rotation runs in further workgroups of the same launch.
+#include <algorithm>
+
+#include "jf_batch.h"
+
+namespace jf {
+
+// Sine and cosine of four consecutive pairs at a position.
+__device__ __forceinline__ void angles4(const double* freq, int i, int pos, float (&cs)[4], float (&sn)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const double t = (double)pos * freq[i + e];
+    sincospif(2.f * (float)(t - rint(t)), &sn[e], &cs[e]);
+  }
+}
+
+template <typename T> __device__ __forceinline__ void store4(T* p, const float (&v)[4]);
+template <> __device__ __forceinline__ void store4<float>(float* p, const float (&v)[4]) {
+  *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+}
+template <> __device__ __forceinline__ void store4<bf16_t>(bf16_t* p, const float (&v)[4]) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+}
+
+constexpr int kQHeads = 4;  // heads that share a thread's sines and cosines
+
+// The queries: a thread rotates four pairs of up to kQHeads heads of a row.
+template <typename X, typename A, int HD>
+__device__ __forceinline__ void append_queries(const AppendArgs& a, const Seq& q, int block) {
+  constexpr int kChunks = HD / 8;
+  const int hb = (a.H + kQHeads - 1) / kQHeads;
+  const int item = block * 256 + threadIdx.x;
+  const int c = item % kChunks, h0 = item / kChunks % hb * kQHeads, i = item / kChunks / hb;
+  if (i >= q.n) return;
+  const int row = q.r0 + i;
+  float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
+  if (a.rotate) angles4(a.freq, 4 * c, a.pos ? a.pos[row] : q.C + i, cs, sn);
+  const X* x = reinterpret_cast<const X*>(a.q) + (size_t)row * a.ld_q;
+  A* out = reinterpret_cast<A*>(a.q_out) + (size_t)row * a.H * HD;
+#pragma unroll
+  for (int hh = 0; hh < kQHeads; ++hh) {
+    const int h = h0 + hh;
+    if (h >= a.H) break;
+    float u[4], w[4], y[4], z[4];
+    load4(x + (size_t)h * HD + 4 * c, a.vec_q, u);
+    load4(x + (size_t)h * HD + HD / 2 + 4 * c, a.vec_q, w);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      y[e] = a.rotate ? u[e] * cs[e] - w[e] * sn[e] : u[e];
+      z[e] = a.rotate ? w[e] * cs[e] + u[e] * sn[e] : w[e];
+    }
+    act_store4(out + (size_t)h * HD + 4 * c, a.q_plane, y);
+    act_store4(out + (size_t)h * HD + HD / 2 + 4 * c, a.q_plane, z);
+  }
+}
+
+template <int HD, typename T> struct AppendShared { T v[HD][kPage + 8]; };   // values transposed
+template <int HD> struct AppendShared<HD, uint8_t> {
+  uint32_t code[2][16 * HD];  // a head's key and value codes in the page's order
+  float amax[2][4];
+};
+
+// KV: float, bf16_t (pages of jf_model_load) or uint8_t (e4m3 pages).
+template <typename X, typename A, typename KV, int HD>
+__global__ void __launch_bounds__(256) k_kv_append(AppendArgs a) {
+  constexpr int kItems = HD / 32;  // a thread's items: four pairs of one token
+  __shared__ AppendShared<HD, KV> sh;
+  const int per = a.n_cache + a.n_q;
+  const int s = blockIdx.x / per, it = blockIdx.x % per;
+  Seq q;
+  if (!batch_seq(a.b, s, q)) return;
+  if (it >= a.n_cache) {
+    append_queries<X, A, HD>(a, q, it - a.n_cache);
+    return;
+  }
+  const int g = it % a.G, page = q.C / kPage + it / a.G;
+  const int t0 = max(q.C - page * kPage, 0);                 // first new token of the page
+  const int t1 = min(q.C + q.n - page * kPage, kPage);       // past the last one
+  if (t1 <= t0) return;
+  const int id = batch_page(a.b, q, page);
+  if (id < 0) return;
+  const int tid = threadIdx.x;
+  const int row0 = q.r0 + page * kPage - q.C;                // the row of the page's token 0
+
+  // the new keys (rotated) and values, in registers
+  float x[kItems][2][8];
+  float kmax = 0.f, vmax = 0.f;
+#pragma unroll
+  for (int n = 0; n < kItems; ++n) {
+    const int item = n * 256 + tid, c = item % (HD / 8), t = item / (HD / 8);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[n][0][e] = x[n][1][e] = 0.f;
+    if (t >= t0 && t < t1) {
+      const int row = row0 + t;
+      const X* kp = reinterpret_cast<const X*>(a.k) + (size_t)row * a.ld_k + (size_t)g * HD + 4 * c;
+      const X* vp = reinterpret_cast<const X*>(a.v) + (size_t)row * a.ld_v + (size_t)g * HD + 4 * c;
+      float u[4], w[4], p[4], r[4];
+      load4(kp, a.vec_k, u);
+      load4(kp + HD / 2, a.vec_k, w);
+      load4(vp, a.vec_v, p);
+      load4(vp + HD / 2, a.vec_v, r);
+      float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
+      if (a.rotate) angles4(a.freq, 4 * c, a.pos ? a.pos[row] : q.C + row - q.r0, cs, sn);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[n][0][e] = a.rotate ? u[e] * cs[e] - w[e] * sn[e] : u[e];
+        x[n][0][4 + e] = a.rotate ? w[e] * cs[e] + u[e] * sn[e] : w[e];
+        x[n][1][e] = p[e];
+        x[n][1][4 + e] = r[e];
+      }
+    }
+  }
+  char* base = reinterpret_cast<char*>(a.kv) + (size_t)id * a.page_bytes;
+
+  if constexpr (sizeof(KV) > 1) {
+    KV* kd = reinterpret_cast<KV*>(base) + (size_t)g * kPage * HD;
+    KV* vd = reinterpret_cast<KV*>(base) + (size_t)(a.G + g) * kPage * HD;
+#pragma unroll
+    for (int n = 0; n < kItems; ++n) {
+      const int item = n * 256 + tid, c = item % (HD / 8), t = item / (HD / 8);
+      if (t < t0 || t >= t1) continue;
+      store4<KV>(kd + (size_t)t * HD + 4 * c, {x[n][0][0], x[n][0][1], x[n][0][2], x[n][0][3]});
+      store4<KV>(kd + (size_t)t * HD + HD / 2 + 4 * c, {x[n][0][4], x[n][0][5], x[n][0][6], x[n][0][7]});
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sh.v[(e / 4) * (HD / 2) + 4 * c + e % 4][t] = from_f32<KV>(x[n][1][e]);
+    }
+    __syncthreads();
+    const int m = t1 - t0;
+    for (int i = tid; i < m * HD; i += 256) vd[(size_t)(i / m) * kPage + t0 + i % m] = sh.v[i / m][t0 + i % m];
+  } else {
+#pragma unroll
+    for (int n = 0; n < kItems; ++n)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        // infinities saturate and NaN stays NaN: neither sets the scale
+        const float ka = fabsf(x[n][0][e]), va = fabsf(x[n][1][e]);
+        kmax = ka < INFINITY ? fmaxf(kmax, ka) : kmax;
+        vmax = va < INFINITY ? fmaxf(vmax, va) : vmax;
+      }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      kmax = fmaxf(kmax, __shfl_xor(kmax, d));
+      vmax = fmaxf(vmax, __shfl_xor(vmax, d));
+    }
+    if ((tid & 63) == 0) {
+      sh.amax[0][tid >> 6] = kmax;
+      sh.amax[1][tid >> 6] = vmax;
+    }
+    __syncthreads();
+    float* scales = reinterpret_cast<float*>(base + (size_t)2 * a.G * kPage * HD) + 2 * g;
+    uint32_t* codes[2] = {reinterpret_cast<uint32_t*>(base + (size_t)g * kPage * HD),
+                          reinterpret_cast<uint32_t*>(base + (size_t)(a.G + g) * kPage * HD)};
+    int from[2];          // first token whose codes are written
+    float inv[2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const float amax = fmaxf(fmaxf(sh.amax[w][0], sh.amax[w][1]), fmaxf(sh.amax[w][2], sh.amax[w][3]));
+      const float need = f8_block_scale(amax);
+      const float old = t0 > 0 ? scales[w] : need;
+      const float sc = fmaxf(old, need);
+      inv[w] = 1.f / sc;  // a power of two: exact
+      from[w] = t0;
+      if (sc > old) {     // the kept tokens' codes on the larger scale
+        const float ratio = old * inv[w];
+        for (int i = tid; i < 16 * HD; i += 256) {
+          float v[4];
+          f8_unpack4(codes[w][i], v);
+          sh.code[w][i] = f8_pack4(v[0] * ratio, v[1] * ratio, v[2] * ratio, v[3] * ratio);
+        }
+        from[w] = 0;
+      }
+    }
+    __syncthreads();      // scales read, kept codes staged
+    if (tid == 0) {
+      scales[0] = 1.f / inv[0];
+      scales[1] = 1.f / inv[1];
+    }
+    uint8_t* kc = reinterpret_cast<uint8_t*>(sh.code[0]);
+    uint8_t* vc = reinterpret_cast<uint8_t*>(sh.code[1]);
+#pragma unroll
+    for (int n = 0; n < kItems; ++n) {
+      const int item = n * 256 + tid, c = item % (HD / 8), t = item / (HD / 8);
+      if (t < t0 || t >= t1) continue;
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const float* k4 = &x[n][0][4 * hf];
+        const float* v4 = &x[n][1][4 * hf];
+        const int i = hf * (HD / 2) + 4 * c;
+        *reinterpret_cast<uint32_t*>(kc + kv8_key_offset(t, i, HD)) =
+            f8_pack4(k4[0] * inv[0], k4[1] * inv[0], k4[2] * inv[0], k4[3] * inv[0]);
+        const uint32_t w = f8_pack4(v4[0] * inv[1], v4[1] * inv[1], v4[2] * inv[1], v4[3] * inv[1]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vc[kv8_value_offset(t, i + e)] = (uint8_t)(w >> (8 * e));
+      }
+    }
+    __syncthreads();
+    // Words of four dims of one token (keys), of four tokens of one dim
+    // (values); only the tokens written change.
+    for (int i = tid; i < 16 * HD; i += 256) {
+      const int lane = (i >> 2) & 63, b = (i >> 8) * 16 + (i & 3) * 4;
+      const int tk = (b / (HD / 4)) * 16 + (lane & 15);
+      if (tk >= from[0] && tk < t1) codes[0][i] = sh.code[0][i];
+      const int tv = (i & 3) * 16 + (lane >> 4) * 4;
+      if (tv >= from[1] && tv + 4 <= t1) {
+        codes[1][i] = sh.code[1][i];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (tv + e >= from[1] && tv + e < t1)
+            reinterpret_cast<uint8_t*>(codes[1] + i)[e] = (uint8_t)(sh.code[1][i] >> (8 * e));
+      }
+    }
+  }
+}
+
+// ---- reading back --------------------------------------------------------------------
+template <typename T> __device__ __forceinline__ float cached(const T* p) { return to_f32<T>(*p); }
+
+// A workgroup: one head of one page.  KV as above; X: float or bf16_t rows.
+template <typename X, typename KV, int HD>
+__global__ void __launch_bounds__(256) k_kv_read(ReadArgs a) {
+  __shared__ float sv[kPage][HD + 1];
+  const int per = a.pages * a.G;
+  const int s = blockIdx.x / per, it = blockIdx.x % per;
+  Seq q;
+  if (!batch_seq(a.b, s, q)) return;
+  const int g = it % a.G, page = q.C / kPage + it / a.G;
+  const int t0 = max(q.C - page * kPage, 0), t1 = min(q.C + q.n - page * kPage, kPage);
+  if (t1 <= t0) return;
+  const int id = batch_page(a.b, q, page);
+  if (id < 0) return;
+  const int tid = threadIdx.x;
+  const int row0 = q.r0 + page * kPage - q.C;
+  const char* base = reinterpret_cast<const char*>(a.kv) + (size_t)id * a.page_bytes;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    if (w) __syncthreads();
+    if constexpr (sizeof(KV) > 1) {
+      const KV* p = reinterpret_cast<const KV*>(base) + (size_t)(w ? a.G + g : g) * kPage * HD;
+      for (int i = tid; i < kPage * HD; i += 256) {
+        const int t = w ? i % kPage : i / HD, d = w ? i / kPage : i % HD;
+        if (t >= t0 && t < t1) sv[t][d] = to_f32<KV>(p[i]);
+      }
+    } else {
+      const uint32_t* p = reinterpret_cast<const uint32_t*>(base + (size_t)(w ? a.G + g : g) * kPage * HD);
+      const float sc = reinterpret_cast<const float*>(base + (size_t)2 * a.G * kPage * HD)[2 * g + w];
+      for (int i = tid; i < 16 * HD; i += 256) {
+        float v[4];
+        f8_unpack4(p[i], v);
+        const int lane = (i >> 2) & 63, b = (i >> 8) * 16 + (i & 3) * 4;
+        if (w == 0) {
+          const int t = (b / (HD / 4)) * 16 + (lane & 15), d = (lane >> 4) * (HD / 4) + b % (HD / 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sv[t][d + e] = v[e] * sc;
+        } else {
+          const int t = (i & 3) * 16 + (lane >> 4) * 4, d = (i >> 8) * 16 + (lane & 15);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sv[t + e][d] = v[e] * sc;
+        }
+      }
+    }
+    __syncthreads();
+    X* out = reinterpret_cast<X*>(w ? a.v : a.k);
+    const size_t ld = w ? a.ld_v : a.ld_k;
+    for (int i = tid; i < (t1 - t0) * HD; i += 256) {
+      const int t = t0 + i / HD, d = i % HD;
+      out[(size_t)(row0 + t) * ld + (size_t)g * HD + d] = from_f32<X>(sv[t][d]);
+    }
+  }
+}
+
+// ---- launches ------------------------------------------------------------------------
+// Pages that n consecutive slots can touch.
+static int pages_of(int n) { return (int)(((int64_t)n + kPage - 2) / kPage) + 1; }
+
+template <typename X, typename A, typename KV>
+static hipError_t append_hd(const AppendArgs& a, unsigned grid, hipStream_t st) {
+  if (a.hd == 32) k_kv_append<X, A, KV, 32><<<grid, 256, 0, st>>>(a);
+  else if (a.hd == 64) k_kv_append<X, A, KV, 64><<<grid, 256, 0, st>>>(a);
+  else k_kv_append<X, A, KV, 128><<<grid, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+template <typename X, typename A>
+static hipError_t append_kv(int kv, const AppendArgs& a, unsigned grid, hipStream_t st) {
+  if (kv == 0) return append_hd<X, A, float>(a, grid, st);
+  if (kv == 1) return append_hd<X, A, bf16_t>(a, grid, st);
+  return append_hd<X, A, uint8_t>(a, grid, st);
+}
+hipError_t launch_kv_append(int kv, int x, int act, AppendArgs& a, hipStream_t st) {
+  a.n_cache = pages_of(a.b.max_rows) * a.G;
+  a.n_q = a.q ? (int)(((int64_t)a.b.max_rows * ((a.H + kQHeads - 1) / kQHeads) * (a.hd / 8) + 255) / 256) : 0;
+  const unsigned n = (unsigned)(a.b.n_seqs * (a.n_cache + a.n_q));
+  if (x == 0) return act == 0 ? append_kv<float, float>(kv, a, n, st) : append_kv<float, bf16_t>(kv, a, n, st);
+  return act == 0 ? append_kv<bf16_t, float>(kv, a, n, st) : append_kv<bf16_t, bf16_t>(kv, a, n, st);
+}
+
+template <typename X, typename KV> static hipError_t read_hd(const ReadArgs& a, unsigned grid, hipStream_t st) {
+  if (a.hd == 32) k_kv_read<X, KV, 32><<<grid, 256, 0, st>>>(a);
+  else if (a.hd == 64) k_kv_read<X, KV, 64><<<grid, 256, 0, st>>>(a);
+  else k_kv_read<X, KV, 128><<<grid, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+template <typename X> static hipError_t read_kv(int kv, const ReadArgs& a, unsigned grid, hipStream_t st) {
+  if (kv == 0) return read_hd<X, float>(a, grid, st);
+  if (kv == 1) return read_hd<X, bf16_t>(a, grid, st);
+  return read_hd<X, uint8_t>(a, grid, st);
+}
+hipError_t launch_kv_read(int kv, int x, ReadArgs& a, hipStream_t st) {
+  a.pages = pages_of(a.b.max_rows);
+  const unsigned n = (unsigned)(a.b.n_seqs * a.pages * a.G);
+  return x == 0 ? read_kv<float>(kv, a, n, st) : read_kv<bf16_t>(kv, a, n, st);
+}
+
+}  // namespace jf

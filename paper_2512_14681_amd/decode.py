@@ -15,6 +15,8 @@ paper's procedures:
                             iterate of every block on the device (the
                             trajectories J of Sec. 2.1 that Jacobi Forcing
                             trains on).
+* ``score``              -- log probabilities, entropies and best alternatives
+                            of given tokens after a prompt (teacher forcing).
 """
 from __future__ import annotations
 
@@ -166,6 +168,40 @@ class Decoder:
             lengths[b] = j + 1
             C += n
         return d_traj, lengths
+
+    # ---- teacher forcing ------------------------------------------------------------
+    def score(self, prompt, tokens, k: int = 0):
+        """Log probabilities of given tokens after a prompt of two tokens or
+        more: returns (logprob [T], entropy [T], top_ids [T][k],
+        top_logprob [T][k]), position i being the model's distribution of
+        tokens[i] given prompt + tokens[:i].  The prompt without its last
+        token is prefilled; steps of up to max_rows rows feed the rest and
+        commit every row, and jf_token_logprobs reads their logits on the
+        device.  The cache then holds prompt + tokens[:-1]."""
+        t, m, V = self.t, self.m, self.V
+        prompt = np.asarray(prompt, dtype=np.int32)
+        tokens = np.asarray(tokens, dtype=np.int32)
+        if len(prompt) < 2 or len(tokens) < 1:
+            raise ValueError("score needs a prompt of two tokens or more and one token or more")
+        T, R = len(tokens), m.cfg.max_rows
+        self.prefill(prompt[:-1])
+        feed = t.as_tensor(np.concatenate([prompt[-1:], tokens[:-1]]), device="cuda")
+        d_tok = t.as_tensor(tokens, device="cuda")
+        f32 = dict(dtype=t.float32, device="cuda")
+        lp, ent, top = t.empty(T, **f32), t.empty(T, **f32), t.empty((T, k), **f32)
+        ids = t.empty((T, k), dtype=t.int32, device="cuda")
+        logits = t.empty((min(R, T), V), **f32)
+        ws = t.empty(jf.token_logprobs_ws_bytes(min(R, T), V, k), dtype=t.uint8, device="cuda")
+        for at in range(0, T, R):
+            n = min(R, T - at)
+            m.jf_jacobi_step(feed[at:at + n], n, 0, 0, self.d_argmax, self.d_result, self.d_next, logits)
+            # every fed row is committed, accepted or not (argument of the commit: a result of n rows)
+            self.d_result[0].fill_(n)
+            m.jf_commit_kv(None, self.d_result)
+            jf.token_logprobs(logits[:n], ws, d_tokens=d_tok[at:at + n], k=k, d_logprob=lp[at:at + n],
+                              d_entropy=ent[at:at + n], d_top_ids=ids[at:at + n], d_top_logprob=top[at:at + n],
+                              stream=m.stream)
+        return lp.cpu().numpy(), ent.cpu().numpy(), ids.cpu().numpy(), top.cpu().numpy()
 
     # ---- App. A Alg. 1 ------------------------------------------------------------
     def generate_multiblock(self, prompt, n: int, K: int, r: float, max_new: int,

@@ -17,13 +17,14 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libjf.so")
 
 JF_OK, JF_E_INVAL, JF_E_SHAPE, JF_E_CAPACITY, JF_E_DTYPE, JF_E_HIP, JF_E_STATE = 0, -1, -2, -3, -4, -5, -6
-JF_F32, JF_BF16 = 0, 1
+JF_F32, JF_BF16, JF_E4M3 = 0, 1, 2
 JF_ROLE_RA, JF_ROLE_CAND, JF_ROLE_PSEUDO = 0, 1, 2
 JF_MAX_SEGMENTS = 16
 JF_MAX_ROWS = 512      # rows of one step at most
 JF_STEP_COMMIT = 2     # jf_jacobi_step mode bit: commit the accepted rows in the step
 JF_VIS_WORDS = 8       # u64 words of a row's in-step visibility mask
-JF_FLAG_BAD_TOKEN, JF_FLAG_CAPACITY, JF_FLAG_SYNC = 1, 2, 4
+JF_FLAG_BAD_TOKEN, JF_FLAG_CAPACITY, JF_FLAG_SYNC, JF_FLAG_BAD_PAGE = 1, 2, 4, 8
+JF_MAX_TOP = 32        # alternatives of jf_token_logprobs at most
 JF_OPT_FUSED_ATTENTION = 1
 JF_MASK_NOISY_CONTEXT, JF_MASK_CLEAN_CONTEXT = 0, 1
 (JF_KERNEL_QKV, JF_KERNEL_ATTN, JF_KERNEL_O, JF_KERNEL_GATEUP, JF_KERNEL_DOWN, JF_KERNEL_LMHEAD,
@@ -71,6 +72,12 @@ class JfSegment(ctypes.Structure):
                 ("verify_from", ctypes.c_int32)]
 
 
+class JfBatch(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("max_rows", ctypes.c_int32),
+                ("max_ctx", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("table_stride", ctypes.c_int32),
+                ("d_row_start", ctypes.c_void_p), ("d_ctx", ctypes.c_void_p), ("d_page_table", ctypes.c_void_p)]
+
+
 class JfError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {msg}")
@@ -79,6 +86,7 @@ class JfError(RuntimeError):
 
 _LIB = None
 P, I32, U64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_size_t
+I64, F64, PB = ctypes.c_int64, ctypes.c_double, ctypes.POINTER(JfBatch)
 _SIGS = {
     "jf_query_sizes": (I32, [ctypes.POINTER(JfConfig), ctypes.POINTER(SZ), ctypes.POINTER(SZ), ctypes.POINTER(SZ)]),
     "jf_model_load": (I32, [ctypes.POINTER(JfConfig), ctypes.POINTER(P), I32, P, P, P, P, ctypes.POINTER(P)]),
@@ -104,6 +112,14 @@ _SIGS = {
     "jf_packed_forward": (I32, [P, P, I32, I32, I32, P, P, P]),
     "jf_trajectory_record": (I32, [P, P, I32, I32, P, P]),
     "jf_trajectory_select": (I32, [P, P, I32, I32, I32, I32, P, P, P, P]),
+    "jf_kv_page_bytes": (SZ, [I32, I32, I32]),
+    "jf_kv_append": (I32, [PB, I32, I32, I32, I32, I32, I32, P, I64, P, I64, P, I64, P, F64, P, P, P, P]),
+    "jf_kv_read": (I32, [PB, I32, I32, I32, I32, P, P, I64, P, I64, P, P]),
+    "jf_attention_kv8_ws_bytes": (SZ, [PB, I32, I32, I32]),
+    "jf_attention_kv8": (I32, [PB, I32, I32, I32, I32, P, P, P, P, P, P, P]),
+    "jf_token_logprobs_ws_bytes": (SZ, [I32, I32, I32]),
+    "jf_token_logprobs": (I32, [I32, I32, I32, P, I64, P, I32, P, P, P, P, P, P, P]),
+    "jf_token_logprobs_grad": (I32, [I32, I32, I32, P, I64, P, P, P, P, P, P, I64, P]),
 }
 EXPORTS = tuple(_SIGS)
 
@@ -264,3 +280,91 @@ def trajectory_select(d_traj, d_len, n_blocks, n, max_points, w, d_sel, d_t_num=
                       stream=None):
     check(lib().jf_trajectory_select(_ptr(d_traj), _ptr(d_len), int(n_blocks), int(n), int(max_points),
                                      int(w), _ptr(d_t_num), _ptr(d_sel), _ptr(d_unconv), _stream(stream)))
+
+
+# ---- batches of sequences over a paged cache (component calls, no model) --------------
+class Batch:
+    """A jf_batch over device int32 tensors (kept alive here): row_start [n_seqs + 1], ctx [n_seqs] and
+    page_table [n_seqs][stride], with the host's bounds."""
+
+    def __init__(self, row_start, ctx, page_table, n_rows, max_rows, max_ctx, n_pages):
+        self.tensors = (row_start, ctx, page_table)
+        for t in self.tensors:
+            if str(t.dtype) != "torch.int32" or not t.is_contiguous():
+                raise TypeError("row_start, ctx and page_table are contiguous int32 tensors")
+        n = ctx.numel()
+        if row_start.numel() != n + 1 or page_table.shape[0] != n:
+            raise ValueError(f"{n} sequences need {n + 1} row starts and {n} rows of the page table")
+        self.c = JfBatch(n, int(n_rows), int(max_rows), int(max_ctx), int(n_pages), int(page_table.shape[1]),
+                         row_start.data_ptr(), ctx.data_ptr(), page_table.data_ptr())
+        self.ref = ctypes.byref(self.c)
+
+
+def _rows(t):
+    """(jf_dtype, row stride in elements) of a [rows][columns] tensor of fp32 or bf16 whose rows are contiguous."""
+    code = {"torch.float32": JF_F32, "torch.bfloat16": JF_BF16}.get(str(t.dtype))
+    if code is None or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise TypeError("rows are 2-dimensional fp32 or bf16 tensors with contiguous rows")
+    return code, t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def kv_page_bytes(n_kv_heads, head_dim, kv_dtype):
+    return lib().jf_kv_page_bytes(int(n_kv_heads), int(head_dim), int(kv_dtype))
+
+
+def kv_append(batch, n_heads, n_kv_heads, head_dim, kv_dtype, d_kv, d_k, d_v, d_q=None, d_q_out=None,
+              act_dtype=JF_BF16, d_pos=None, rope_base=0.0, d_flags=None, stream=None):
+    x, ld_k = _rows(d_k)
+    xv, ld_v = _rows(d_v)
+    xq, ld_q = _rows(d_q) if d_q is not None else (x, 0)
+    if not x == xv == xq:
+        raise TypeError("queries, keys and values have one type")
+    check(lib().jf_kv_append(batch.ref, n_heads, n_kv_heads, head_dim, kv_dtype, x, act_dtype, _ptr(d_q), ld_q,
+                             _ptr(d_k), ld_k, _ptr(d_v), ld_v, _ptr(d_pos), rope_base, _ptr(d_kv), _ptr(d_q_out),
+                             _ptr(d_flags), _stream(stream)))
+
+
+def kv_read(batch, n_kv_heads, head_dim, kv_dtype, d_kv, d_k, d_v, d_flags=None, stream=None):
+    x, ld_k = _rows(d_k)
+    xv, ld_v = _rows(d_v)
+    if x != xv:
+        raise TypeError("keys and values have one type")
+    check(lib().jf_kv_read(batch.ref, n_kv_heads, head_dim, kv_dtype, x, _ptr(d_kv), _ptr(d_k), ld_k, _ptr(d_v), ld_v,
+                           _ptr(d_flags), _stream(stream)))
+
+
+def attention_kv8_ws_bytes(batch, n_heads, n_kv_heads, head_dim):
+    n = lib().jf_attention_kv8_ws_bytes(batch.ref, n_heads, n_kv_heads, head_dim)
+    if n == 0:
+        raise JfError(JF_E_SHAPE, lib().jf_last_error().decode())
+    return n
+
+
+def attention_kv8(batch, n_heads, n_kv_heads, head_dim, act_dtype, d_q, d_kv, d_out, d_ws, d_vis=None, d_flags=None,
+                  stream=None):
+    check(lib().jf_attention_kv8(batch.ref, n_heads, n_kv_heads, head_dim, act_dtype, _ptr(d_q), _ptr(d_kv),
+                                 _ptr(d_vis), _ptr(d_out), _ptr(d_ws), _ptr(d_flags), _stream(stream)))
+
+
+# ---- log probabilities (component calls, no model) -------------------------------------
+def token_logprobs_ws_bytes(R, V, k=0):
+    return lib().jf_token_logprobs_ws_bytes(int(R), int(V), int(k))
+
+
+def token_logprobs(d_logits, d_ws, d_tokens=None, k=0, d_logprob=None, d_entropy=None, d_norm=None, d_top_ids=None,
+                   d_top_logprob=None, stream=None):
+    x, ld = _rows(d_logits)
+    check(lib().jf_token_logprobs(d_logits.shape[0], d_logits.shape[1], x, _ptr(d_logits), ld, _ptr(d_tokens), k,
+                                  _ptr(d_logprob), _ptr(d_entropy), _ptr(d_norm), _ptr(d_top_ids),
+                                  _ptr(d_top_logprob), _ptr(d_ws), _stream(stream)))
+
+
+def token_logprobs_grad(d_logits, d_norm, d_grad, d_tokens=None, d_entropy=None, d_g_logprob=None, d_g_entropy=None,
+                        stream=None):
+    x, ld = _rows(d_logits)
+    xg, ld_g = _rows(d_grad)
+    if x != xg or d_grad.shape != d_logits.shape:
+        raise TypeError("the gradient has the logits' shape and type")
+    check(lib().jf_token_logprobs_grad(d_logits.shape[0], d_logits.shape[1], x, _ptr(d_logits), ld, _ptr(d_tokens),
+                                       _ptr(d_norm), _ptr(d_entropy), _ptr(d_g_logprob), _ptr(d_g_entropy),
+                                       _ptr(d_grad), ld_g, _stream(stream)))
