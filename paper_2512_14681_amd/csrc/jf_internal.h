@@ -324,8 +324,7 @@ struct Kv8Args {
   float* o_part;             // [splits][n_rows * H][hd]
   float* ml_part;            // [splits][n_rows * H][2]
   // the plan (kv8_plan)
-  int share;                 // 1: the waves of a workgroup take query tiles of their own, 0: they share the keys
-  int qt;                    // query tiles of a wave
+  int qt;                    // query tiles of a wave (0: one tile, whose keys the waves share)
   int groups;                // workgroups along the query tiles
   int chunk;                 // pages of a key split
   int splits;
