@@ -14,6 +14,7 @@
 // values' scales are applied relative to the largest one met so far; a page's
 // codes lose bits by that only 2^11 and more below it.
 #include <algorithm>
+#include <type_traits>
 
 #include "jf_batch.h"
 
@@ -96,6 +97,18 @@ template <> __device__ __forceinline__ void load_q8<float>(const float* p, size_
   v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
 
+// Values that all lanes share, kept in scalar registers.
+__device__ __forceinline__ int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float same(float v) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
+}
+// The bits of a power of two over those of one no smaller, as their ratio (0
+// below the normal range).
+__device__ __forceinline__ float power_ratio(int a, int b) {
+  const int d = a - b + 0x3F800000;
+  return __uint_as_float(d > 0 ? d : 0);
+}
+
 // Maximum over the four lanes that share a query (l, l ^ 16, l ^ 32, l ^ 48).
 __device__ __forceinline__ float query_max(float v) {
   const uint32_t u = __float_as_uint(v);
@@ -105,11 +118,12 @@ __device__ __forceinline__ float query_max(float v) {
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// Weights are 2^kWeightBits e^(s - m), and m follows a row's maximum only
-// when that has grown by more than 2^kSlack: most pages leave the sums and
-// outputs as they are.
-constexpr float kWeightBits = 12.f, kSlack = 3.f;
-constexpr int kWaves = 4;
+// Weights are 2^kWeightBits e^(s - m).  m follows a row's maximum only when a
+// lane's 16 weights of a page sum to more than kMostWeight, which fp16 still
+// holds: most pages look for no maximum and leave sums and outputs as they
+// are.
+constexpr float kWeightBits = 10.f, kMostWeight = 32768.f;
+constexpr int kWaves = 4, kXcds = 8;
 
 // QT tiles of 16 queries of one KV head in a wave.  Query j of the head group
 // is row j / grp, head j % grp of the group, so that a tile's queries have
@@ -123,12 +137,13 @@ template <typename A, int HD, int QT> struct Tiles {
   int qi[QT], qhd[QT];
   bool valid[QT];
   float m[QT], l[QT];
-  f32x4_t o[QT][NP];                  // in the units of the value scale `unit`
-  float unit, minus_one;
+  f32x4_t o[QT][NP];                  // in units of the value scale `unit`
+  int unit;                           // the bits of a power of two (0 before the first page)
+  float minus_one;
 
   __device__ __forceinline__ void init(const Kv8Args& a, const Seq& q, int g, int tile0) {
     const int grp = a.H / a.G, nq = grp * q.n, lane = threadIdx.x & 63, ql = lane & 15, kg = lane >> 4;
-    unit = 0.f;
+    unit = 0;
     minus_one = -1.f;
     asm("" : "+s"(minus_one));
 #pragma unroll
@@ -167,15 +182,19 @@ template <typename A, int HD, int QT> struct Tiles {
     }
   }
 
-  // Scores of a page; kf(kt, c): its keys 16 kt .., dims of matrix step c.
-  template <typename F> __device__ __forceinline__ void scores(F kf, f32x4_t (&st)[QT][4]) const {
+  // Scores of a page; piece(n): the lane's 16 key bytes of piece n.
+  template <typename F> __device__ __forceinline__ void scores(F piece, f32x4_t (&st)[QT][4]) const {
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt) {
+    for (int t = 0; t < QT; ++t)
 #pragma unroll
-      for (int t = 0; t < QT; ++t) st[t][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int kt = 0; kt < 4; ++kt) st[t][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < NS; ++c) {
-        const f16x8_t k = kf(kt, c);
+    for (int n = 0; n < NP; ++n) {
+      const u32x4_t w = piece(n);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int kt = (2 * n + h) / NS, c = (2 * n + h) % NS;
+        const f16x8_t k = f8_to_f16(w[2 * h], w[2 * h + 1], 1.f);
 #pragma unroll
         for (int t = 0; t < QT; ++t) mfma16(st[t][kt], k, qh[t][c]);
 #pragma unroll
@@ -202,76 +221,137 @@ template <typename A, int HD, int QT> struct Tiles {
     }
   }
 
-  // Scores to weights; key_scale: the page's.
-  __device__ __forceinline__ void softmax(const f32x4_t (&st)[QT][4], float key_scale, f16x8_t (&ph)[QT][2],
-                                          f16x8_t (&pl)[QT][2]) {
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      float x[16];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = st[t][e >> 2][e & 3];
-      const float f = cq[t] * key_scale;
-      float mx = x[0];
-#pragma unroll
-      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[e]);
-      mx = query_max(mx) * f;
-      if (__any(mx > m[t] + kSlack)) {
-        const float m_new = fmaxf(m[t], mx);
-        const float alpha = __builtin_amdgcn_exp2f(m[t] - (m_new == -INFINITY ? 0.f : m_new));
-        l[t] *= alpha;
-        m[t] = m_new;
-#pragma unroll
-        for (int d = 0; d < NP; ++d) o[t][d] *= alpha;
-      }
-      // nothing visible yet: weights 0
-      const float off = kWeightBits - (m[t] == -INFINITY ? 0.f : m[t]);
-      float sum = 0.f;
+  // Tile t's weights of a page with that key scale.
+  __device__ __forceinline__ void weights(int t, const f32x4_t (&st)[QT][4], float key_scale, f16x8_t (&ph)[2],
+                                          f16x8_t (&pl)[2]) {
+    const float f = cq[t] * key_scale;
+    float x[16], sum;
+    auto compute = [&](float off) {
+      sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], f, off));
+        x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[t][e >> 2][e & 3], f, off));
         sum += x[e];
       }
-      l[t] += sum;
-      split16(x, minus_one, ph[t][0], pl[t][0]);
-      split16(x + 8, minus_one, ph[t][1], pl[t][1]);
+    };
+    compute(kWeightBits - m[t]);  // nothing seen yet: infinity or NaN
+    if (__any(!(sum <= kMostWeight))) {
+      float mx = st[t][0][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, st[t][e >> 2][e & 3]);
+      const float m_new = fmaxf(m[t], query_max(mx) * f), m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m[t] - m_use);
+      l[t] *= alpha;
+      m[t] = m_new;
+#pragma unroll
+      for (int d = 0; d < NP; ++d) o[t][d] *= alpha;
+      compute(kWeightBits - m_use);
     }
+    l[t] += sum;
+    split16(x, minus_one, ph[0], pl[0]);
+    split16(x + 8, minus_one, ph[1], pl[1]);
   }
 
-  // A page's value scale: the outputs' unit becomes the larger of the two.
-  __device__ __forceinline__ float value_scale(float s) {
+  // A page's value scale relative to the outputs' unit, which becomes the
+  // larger of the two (both in scalar registers; powers of two divide by
+  // their exponents).
+  __device__ __forceinline__ float value_scale(float scale) {
+    const int s = same((int)__float_as_uint(scale));
     if (s > unit) {
-      const float f = unit / s;
+      const float f = power_ratio(unit, s);
 #pragma unroll
       for (int t = 0; t < QT; ++t)
 #pragma unroll
         for (int d = 0; d < NP; ++d) o[t][d] *= f;
       unit = s;
     }
-    return s / unit;
+    return power_ratio(s, unit);
   }
 
-  // Weighted values; vf(n, j): the page's dims 16 n .., keys of tiles 2 j and 2 j + 1.
+  // Weighted values; piece(n): the lane's 16 value bytes of piece n.
   template <typename F>
-  __device__ __forceinline__ void outputs(F vf, const f16x8_t (&ph)[QT][2], const f16x8_t (&pl)[QT][2]) {
+  __device__ __forceinline__ void outputs(F piece, float vscale, const f16x8_t (&ph)[QT][2], const f16x8_t (&pl)[QT][2]) {
 #pragma unroll
-    for (int n = 0; n < NP; ++n)
+    for (int n = 0; n < NP; ++n) {
+      const u32x4_t w = piece(n);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const f16x8_t v = vf(n, j);
+        const f16x8_t v = f8_to_f16(w[2 * j], w[2 * j + 1], vscale);
 #pragma unroll
         for (int t = 0; t < QT; ++t) mfma16(o[t][n], v, ph[t][j]);
 #pragma unroll
         for (int t = 0; t < QT; ++t) mfma16(o[t][n], v, pl[t][j]);
       }
+    }
+  }
+
+  // The same two for pieces that come from LDS, in a fixed order: a piece's
+  // reads run two pieces ahead, its conversions beside the matrix
+  // instructions of the piece before, and no matrix instruction follows the
+  // one that it adds to.  mul(n, i, k) is matrix instruction i of piece n on
+  // its operands k.  (The compiler's own order waits for each read.)
+  template <typename F, typename M> __device__ __forceinline__ static void feed(F piece, float scale, M mul) {
+    u32x4_t w[3];
+    F16x8 k[2][2];
+    auto convert = [&](int n, int u) {  // conversion u of piece n
+      const int h = u >> 2, i = u & 3;
+      const uint32_t d = w[n % 3][2 * h + (i >> 1)];
+      k[n & 1][h].p[i] = i & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(d, scale, true)
+                               : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(d, scale, false);
+    };
+    w[0] = piece(0);
+    if (NP > 1) w[1] = piece(1);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) convert(0, u);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < NP; ++n) {
+      if (n + 2 < NP) w[(n + 2) % 3] = piece(n + 2);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < 4 * QT; ++i) {
+        mul(n, i, k[n & 1]);
+        if (n + 1 < NP)
+#pragma unroll
+          for (int u = 0; u < 2 / QT; ++u) convert(n + 1, i * (2 / QT) + u);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  template <typename F> __device__ __forceinline__ void scores_fed(F piece, f32x4_t (&st)[QT][4]) const {
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) st[t][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    feed(piece, 1.f, [&](int n, int i, const F16x8 (&k)[2]) {
+      const int h = i / (2 * QT), lo = i % (2 * QT) / QT, t = i % QT, kt = (2 * n + h) / NS, c = (2 * n + h) % NS;
+      mfma16(st[t][kt], k[h].v, lo ? qlo[t][c] : qh[t][c]);
+    });
+  }
+  template <typename F>
+  __device__ __forceinline__ void outputs_fed(F piece, float vscale, const f16x8_t (&ph)[QT][2],
+                                              const f16x8_t (&pl)[QT][2]) {
+    feed(piece, vscale, [&](int n, int i, const F16x8 (&k)[2]) {
+      const int j = i / (2 * QT), lo = i % (2 * QT) / QT, t = i % QT;
+      mfma16(o[t][n], k[j].v, lo ? pl[t][j] : ph[t][j]);
+    });
   }
 
   // NaN for the queries that see a NaN among the values that ones(n) marks
   // with the code of 1.
   template <typename F>
   __device__ __forceinline__ void poison(const Kv8Args& a, const Seq& q, int p, F ones) {
-    uint64_t sees[QT];
+    f16x8_t b[QT][2];  // 1 for the keys that a query sees
 #pragma unroll
-    for (int t = 0; t < QT; ++t) sees[t] = seen(a, q, t, p);
+    for (int t = 0; t < QT; ++t) {
+      const uint64_t sees = seen(a, q, t, p);
+      const uint32_t half[2] = {(uint32_t)sees, (uint32_t)(sees >> 32)};
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[t][j][e] = (half[j] >> (16 * (e >> 2) + (e & 3))) & 1 ? 1.f : 0.f;
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int n = 0; n < NP; ++n) {
       const u32x4_t w = ones(n);
@@ -279,16 +359,11 @@ template <typename A, int HD, int QT> struct Tiles {
       for (int t = 0; t < QT; ++t) {
         f32x4_t hit = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          f16x8_t b;
+        for (int j = 0; j < 2; ++j) mfma16(hit, f8_to_f16(w[2 * j], w[2 * j + 1], 1.f), b[t][j]);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) b[e] = (sees[t] >> (16 * (2 * j + (e >> 2)) + (e & 3))) & 1 ? 1.f : 0.f;
-          mfma16(hit, f8_to_f16(w[2 * j], w[2 * j + 1], 1.f), b);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (hit[i] > 0.f) o[t][n][i] = NAN;
+        for (int i = 0; i < 4; ++i) o[t][n][i] = hit[i] > 0.f ? NAN : o[t][n][i];
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 
@@ -354,64 +429,72 @@ __global__ void __launch_bounds__(256, 2) k_attention_kv8_few(Kv8Args a) {
   const int pages = (q.C + q.n + kPage - 1) / kPage;
   const int p0 = split * a.chunk, p1 = min(p0 + a.chunk, pages);
   if (p0 >= pages) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ql = lane & 15, kg = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = same((int)threadIdx.x >> 6), ql = lane & 15, kg = lane >> 4;
   T w;
 
-  int id = -1;
+  // Page ids: this page's, the next one's and (on its way) the one after; a
+  // bad one becomes page 0, of which nothing is used.
+  auto entry = [&](int p) { return q.table[min(p, p1 - 1)]; };  // no branch: it would wait for every load
   u32x4_t kr[NP], vr[NP];
-  float2 sc;
-  const uint8_t* page = nullptr;
-  auto find = [&](int p) {  // the wave's first valid page from p on
-    id = -1;
-    for (; p < p1; p += kWaves)
-      if ((id = __builtin_amdgcn_readfirstlane(batch_page(a.b, q, p))) >= 0) break;
-    return p;
-  };
-  auto load_keys = [&] {
-    page = a.kv + (size_t)id * a.page_bytes;
+  float2 sc = {1.f, 1.f};
+  const uint8_t* page = a.kv;
+  auto load_keys = [&](int id) {
+    page = a.kv + (size_t)max(id, 0) * a.page_bytes;
 #pragma unroll
     for (int n = 0; n < NP; ++n) kr[n] = load16<true>(page + (size_t)g * kPage * HD + n * 1024 + lane * 16);
     sc = reinterpret_cast<const float2*>(page + (size_t)2 * a.G * kPage * HD)[g];
   };
-  int p = find(p0 + wave);
-  if (p < p1) load_keys();
+  int p = p0 + wave, id = 0, after = 0;
+  if (p < p1) {
+    const int first = entry(p);
+    after = entry(p + kWaves);
+    id = batch_page_id(a.b, same(first));
+    load_keys(id);
+  }
   w.init(a, q, g, 0);
-  while (p < p1) {
+  // Page p; kEdge: it holds slots that not every row sees.
+  auto step = [&](auto edge) {
+    constexpr bool kEdge = decltype(edge)::value;
+    const int next = batch_page_id(a.b, same(after));
+    after = entry(p + 2 * kWaves);
 #pragma unroll
     for (int n = 0; n < NP; ++n) vr[n] = load16<true>(page + (size_t)(a.G + g) * kPage * HD + n * 1024 + lane * 16);
     f32x4_t st[1][4];
-    w.scores([&](int kt, int c) {
-      const int i = kt * (HD / 16) + 2 * c;
-      return f8_to_f16(kr[i >> 2][i & 3], kr[i >> 2][(i & 3) + 1], 1.f);
-    }, st);
-    const int now = p;
-    const float2 scale = sc;
-    p = find(p + kWaves);
-    if (p < p1) load_keys();
-    const float vscale = w.value_scale(scale.y);
-    f16x8_t ph[1][2], pl[1][2];
-    const bool edge = (now + 1) * kPage > q.C;  // holds slots that not every row sees
-    if (edge) w.mask(a, q, now, st);
-    w.softmax(st, scale.x, ph, pl);
-    if (edge) {
-      // 0 times NaN is NaN: NaN codes are taken out, and the rows that see one get it back
-      bool any = false;
+    w.scores([&](int n) { return kr[n]; }, st);
+    const float2 scale = {same(sc.x), same(sc.y)};
+    if (p + kWaves < p1) load_keys(next);
+    if (id >= 0) {  // a bad page's slots are seen by nobody
+      const float vscale = w.value_scale(scale.y);
+      f16x8_t ph[1][2], pl[1][2];
+      if constexpr (kEdge) {
+        w.mask(a, q, p, st);
+        // 0 times NaN is NaN: NaN codes are taken out, and the rows that see one get it back
+        bool any = false;
 #pragma unroll
-      for (int n = 0; n < NP; ++n) any |= has_nans(vr[n]);
-      if (__any(any)) {
-        w.poison(a, q, now, [&](int n) { return nan_ones(vr[n]); });
+        for (int n = 0; n < NP; ++n) any |= has_nans(vr[n]);
+        if (__any(any)) {
+          w.poison(a, q, p, [&](int n) { return nan_ones(vr[n]); });
 #pragma unroll
-        for (int n = 0; n < NP; ++n) vr[n] = without_nans(vr[n]);
+          for (int n = 0; n < NP; ++n) vr[n] = without_nans(vr[n]);
+        }
       }
+      w.weights(0, st, scale.x, ph[0], pl[0]);
+      w.outputs([&](int n) { return vr[n]; }, vscale, ph, pl);
     }
-    w.outputs([&](int n, int j) { return f8_to_f16(vr[n][2 * j], vr[n][2 * j + 1], vscale); }, ph, pl);
-  }
+    id = next;
+    p += kWaves;
+  };
+  const int whole = min(q.C / kPage, p1);
+#pragma unroll 1
+  while (p < whole) step(std::false_type{});
+#pragma unroll 1
+  while (p < p1) step(std::true_type{});
   w.finish();
 
 #pragma unroll
   for (int n = 0; n < NP; ++n)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s_o[wave][ql][16 * n + 4 * kg + i] = w.o[0][n][i] * w.unit;
+    for (int i = 0; i < 4; ++i) s_o[wave][ql][16 * n + 4 * kg + i] = w.o[0][n][i] * __uint_as_float(w.unit);
   if (kg == 0) {
     s_m[wave][ql] = w.m[0];
     s_l[wave][ql] = w.l[0];
@@ -438,23 +521,27 @@ __global__ void __launch_bounds__(256, 2) k_attention_kv8_few(Kv8Args a) {
 }
 
 // More tiles: QT of its own for each wave.  Workgroup: KV head, 4 QT tiles,
-// key split.  A page is turned to fp16 once for all of them, on its way into
-// one of two LDS buffers: the next page's loads are in flight during a page's
-// work, and one barrier separates two pages.
+// key split.  A page's codes go from memory to one of two LDS buffers without
+// passing registers, while the page before is worked on; the waves read them
+// as operands and turn them to fp16 (as fp16 in LDS the writes alone, 32 KB a
+// page at the 31 bytes a cycle that they reach, took a quarter of the time).
 template <typename A, int HD, int QT>
 __global__ void __launch_bounds__(256, 2) k_attention_kv8_many(Kv8Args a) {
   using T = Tiles<A, HD, QT>;
-  constexpr int NS = T::NS, NP = T::NP;
-  constexpr int kItems = 2 * NP / kWaves;      // 16-byte pieces of a page for each thread
-  __shared__ f16x8_t s_kv[2][4 * NP][64];      // operands: keys kt NS + c, then values 2 NP + 2 n + j
-  __shared__ int s_nan[2];                     // page + 1 whose values hold a NaN that not every row sees
+  constexpr int NP = T::NP;
+  constexpr int kItems = 2 * NP / kWaves;      // 1 KB pieces of a page that each wave brings
+  __shared__ u32x4_t s_kv[2][2 * NP][64];      // pieces: keys, then values
   const int grp = a.H / a.G;
-  const int s = blockIdx.x / (a.G * a.groups), g = blockIdx.x / a.groups % a.G, group = blockIdx.x % a.groups;
-  const int split = blockIdx.y;
+  // Workgroups go around the 8 XCDs in order: each gets a run of consecutive
+  // work, so that the groups that read the same pages share an L2.
+  const int work = blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds;
+  const int group = work % a.groups, split = work / a.groups % a.splits, g = work / (a.groups * a.splits) % a.G;
+  const int s = work / (a.groups * a.splits * a.G);
+  if (s >= a.b.n_seqs) return;
   Seq q;
   if (!batch_seq(a.b, s, q)) return;
   const int nq = grp * q.n;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, kg = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = same((int)threadIdx.x >> 6), kg = lane >> 4;
   if (group * kWaves * QT * 16 >= nq) return;
   const int pages = (q.C + q.n + kPage - 1) / kPage;
   const int p0 = split * a.chunk;
@@ -467,111 +554,147 @@ __global__ void __launch_bounds__(256, 2) k_attention_kv8_many(Kv8Args a) {
     mine = min(mine, (q.C + last_wave / grp) / kPage + 1);
     p1 = min(p1, (q.C + last / grp) / kPage + 1);
   }
-  if (threadIdx.x < 2) s_nan[threadIdx.x] = 0;
   T w;
   w.init(a, q, g, tile0);
 
-  u32x4_t raw[kItems];
-  float2 sc = {0.f, 0.f};
-  const uint8_t* page = nullptr;
-  auto load = [&](int p) {  // the first valid page from p on
-    int id = -1;
-    for (; p < p1; ++p)
-      if ((id = __builtin_amdgcn_readfirstlane(batch_page(a.b, q, p))) >= 0) break;
-    if (id >= 0) {
-      page = a.kv + (size_t)id * a.page_bytes;
-#pragma unroll
-      for (int i = 0; i < kItems; ++i) {
-        const int piece = i * kWaves + wave;   // keys 0 .. NP - 1, then values
-        raw[i] = load16<false>(page + (size_t)(piece < NP ? g : a.G + g) * kPage * HD + (piece % NP) * 1024 + lane * 16);
-      }
-      sc = reinterpret_cast<const float2*>(page + (size_t)2 * a.G * kPage * HD)[g];
-    }
-    return p;
-  };
-  auto store = [&](int buf, int p, float vscale) {
+  // Page ids: the next page's and (on its way) the one after; a bad one
+  // becomes page 0, of which nothing is used.
+  auto entry = [&](int p) { return q.table[min(p, p1 - 1)]; };  // no branch: it would wait for every load
+  float2 sc = {1.f, 1.f};
+  const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)reinterpret_cast<char*>(s_kv) +
+                        wave * 1024;
+  auto load = [&](int buf, int id) {  // a page on its way into a buffer, and its scales
+    const uint8_t* page = a.kv + (size_t)max(id, 0) * a.page_bytes;
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
       const int piece = i * kWaves + wave;
-      if (piece >= NP && (p + 1) * kPage > q.C && __any(has_nans(raw[i]))) {
-        raw[i] = without_nans(raw[i]);
-        s_nan[buf] = p + 1;
-      }
-      const float f = piece < NP ? 1.f : vscale;
-      s_kv[buf][2 * piece][lane] = f8_to_f16(raw[i][0], raw[i][1], f);
-      s_kv[buf][2 * piece + 1][lane] = f8_to_f16(raw[i][2], raw[i][3], f);
+      dma_1k<false>(reinterpret_cast<const char*>(page) + ((piece < NP ? g : a.G + g) * kPage * HD + piece % NP * 1024),
+                    lane * 16, ring + (buf * 2 * NP + i * kWaves) * 1024);
     }
+    sc = reinterpret_cast<const float2*>(page + (size_t)2 * a.G * kPage * HD)[g];
   };
-  __syncthreads();  // s_nan
-  int p = load(p0), buf = 0;
-  float vscale = 0.f, key_scale = 0.f;
-  const uint8_t* base = nullptr;
-  if (p < p1) {
-    vscale = w.value_scale(sc.y);
-    key_scale = sc.x;
-    base = page;
-    store(0, p, vscale);
+  int buf = 0, id = 0, after = 0;
+  if (p0 < p1) {
+    const int first = entry(p0);
+    after = entry(p0 + 1);
+    id = batch_page_id(a.b, same(first));
+    load(0, id);
   }
-  __syncthreads();
-  while (p < p1) {
-    const int next = load(p + 1);
-    if (p < mine) {
-      f32x4_t st[QT][4];
-      w.scores([&](int kt, int c) { return s_kv[buf][kt * NS + c][lane]; }, st);
-      f16x8_t ph[QT][2], pl[QT][2];
-      if ((p + 1) * kPage > q.C) w.mask(a, q, p, st);
-      w.softmax(st, key_scale, ph, pl);
-      if (s_nan[buf] == p + 1)
-        w.poison(a, q, p, [&](int n) {
-          return nan_ones(load16<false>(base + (size_t)(a.G + g) * kPage * HD + n * 1024 + lane * 16));
-        });
-      w.outputs([&](int n, int j) { return s_kv[buf][2 * NP + 2 * n + j][lane]; }, ph, pl);
-    }
-    if (next < p1) {
-      vscale = w.value_scale(sc.y);
-      key_scale = sc.x;
-      base = page;
-      store(buf ^ 1, next, vscale);
-    }
+  // Page p; kEdge: it holds slots that not every row sees.
+  auto step = [&](auto edge, int p) {
+    constexpr bool kEdge = decltype(edge)::value;
+    // every wave's pieces of page p have arrived, and its work on the page before is done
+    wait_vm<0>();
     __syncthreads();
-    p = next;
+    const float key_scale = same(sc.x), vscale = w.value_scale(sc.y);
+    const bool work = id >= 0 && p < mine;   // a bad page's slots are seen by nobody
+    const int next = batch_page_id(a.b, same(after));
+    if (p + 1 < p1) load(buf ^ 1, next);
+    after = entry(p + 2);
+    if (work) {
+      auto key = [&](int n) { return s_kv[buf][n][lane]; };
+      auto value = [&](int n) { return s_kv[buf][NP + n][lane]; };
+      f32x4_t st[QT][4];
+      w.scores_fed(key, st);
+      if constexpr (kEdge) w.mask(a, q, p, st);
+      f16x8_t ph[QT][2], pl[QT][2];
+#pragma unroll
+      for (int t = 0; t < QT; ++t) w.weights(t, st, key_scale, ph[t], pl[t]);
+      if constexpr (kEdge) {
+        // 0 times NaN is NaN: NaN codes are taken out, and the rows that see one get it back
+        bool any = false;
+#pragma unroll
+        for (int n = 0; n < NP; ++n) any |= has_nans(value(n));
+        if (__any(any)) {
+          w.poison(a, q, p, [&](int n) { return nan_ones(value(n)); });
+          w.outputs_fed([&](int n) { return without_nans(value(n)); }, vscale, ph, pl);
+        } else {
+          w.outputs_fed(value, vscale, ph, pl);
+        }
+      } else {
+        w.outputs_fed(value, vscale, ph, pl);
+      }
+    }
+    id = next;
     buf ^= 1;
-  }
+  };
+  int p = p0;
+#pragma unroll 1
+  for (const int whole = min(q.C / kPage, p1); p < whole; ++p) step(std::false_type{}, p);
+#pragma unroll 1
+  for (; p < p1; ++p) step(std::true_type{}, p);
   w.finish();
 #pragma unroll
   for (int t = 0; t < QT; ++t)
     if (w.valid[t])
 #pragma unroll
       for (int n = 0; n < NP; ++n) {
-        float v[4] = {w.o[t][n][0] * w.unit, w.o[t][n][1] * w.unit, w.o[t][n][2] * w.unit, w.o[t][n][3] * w.unit};
+        const float unit = __uint_as_float(w.unit);
+        float v[4] = {w.o[t][n][0] * unit, w.o[t][n][1] * unit, w.o[t][n][2] * unit, w.o[t][n][3] * unit};
         put_outputs<A>(a, q.r0 + w.qi[t], w.qhd[t], split, 16 * n + 4 * kg, w.m[t], w.l[t], v);
       }
 }
 
-// Merges the key splits of a sequence, four dims of one row and head a
-// thread, in split order.
-template <typename A>
+// Merges a row's key splits, four dims of one row and head a thread.  SG
+// threads share an item, each taking every SG-th split, at most kMaxSplits /
+// SG of them with all loads in flight at once, and join in LDS.  Splits are
+// added in the same order whatever the timing.
+constexpr int kMaxSplits = 64;
+template <typename A, int SG>
 __global__ void __launch_bounds__(256) k_attention_kv8_merge(Kv8Args a, int blocks) {
+  constexpr int kEach = SG == 1 ? 8 : kMaxSplits / SG;
+  __shared__ float s_part[SG > 1 ? 256 : 1][6];
   const int s = blockIdx.x / blocks;
   Seq q;
   if (!batch_seq(a.b, s, q)) return;
-  const int chunks = a.hd / 4;
-  const int item = blockIdx.x % blocks * 256 + threadIdx.x;
-  const int dim = item % chunks * 4, h = item / chunks % a.H, i = item / chunks / a.H;
-  if (i >= q.n) return;
-  const int row = q.r0 + i;
+  const int chunks = a.hd / 4, per = 256 / (chunks * SG);  // items of a workgroup
+  const int tid = threadIdx.x, dim = tid % chunks * 4, group = tid / chunks % SG;
+  const int item = blockIdx.x % blocks * per + tid / (chunks * SG);
+  const bool valid = item < q.n * a.H;
+  const int h = valid ? item % a.H : 0, row = q.r0 + (valid ? item / a.H : 0);
   const int n = ((q.C + q.n + kPage - 1) / kPage + a.chunk - 1) / a.chunk;
   const size_t stride = (size_t)a.b.n_rows * a.H, at = (size_t)row * a.H + h;
-  float m = -INFINITY;
-  for (int k = 0; k < n; ++k) m = fmaxf(m, a.ml_part[(k * stride + at) * 2]);
-  float l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int k = 0; k < n; ++k) {
-    const float2 ml = *reinterpret_cast<const float2*>(a.ml_part + (k * stride + at) * 2);
-    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
-    const float4 o = *reinterpret_cast<const float4*>(a.o_part + (k * stride + at) * a.hd + dim);
-    l += ml.y * f;
-    v[0] += o.x * f; v[1] += o.y * f; v[2] += o.z * f; v[3] += o.w * f;
+  float2 ml[kEach];
+  float4 o[kEach];
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int k = group + j * SG;
+    ml[j] = make_float2(-INFINITY, 0.f);
+    o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (k < n) {
+      ml[j] = *reinterpret_cast<const float2*>(a.ml_part + (k * stride + at) * 2);
+      o[j] = *reinterpret_cast<const float4*>(a.o_part + (k * stride + at) * a.hd + dim);
+    }
   }
+  float m = -INFINITY, l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) m = fmaxf(m, ml[j].x);
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const float f = ml[j].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[j].x - m);
+    l += ml[j].y * f;
+    v[0] += o[j].x * f; v[1] += o[j].y * f; v[2] += o[j].z * f; v[3] += o[j].w * f;
+  }
+  if constexpr (SG > 1) {
+    float* p = s_part[tid];
+    p[0] = m; p[1] = l; p[2] = v[0]; p[3] = v[1]; p[4] = v[2]; p[5] = v[3];
+    __syncthreads();
+    if (group) return;
+    const float* g = s_part[tid];  // the groups' parts are chunks threads apart
+    float mm = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < SG; ++j) mm = fmaxf(mm, g[j * chunks * 6]);
+    l = v[0] = v[1] = v[2] = v[3] = 0.f;
+#pragma unroll
+    for (int j = 0; j < SG; ++j) {
+      const float* x = g + j * chunks * 6;
+      const float f = x[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[0] - mm);
+      l += x[1] * f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += x[2 + e] * f;
+    }
+  }
+  if (!valid) return;
   const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] = inv == 0.f ? 0.f : v[e] * inv;
@@ -579,42 +702,49 @@ __global__ void __launch_bounds__(256) k_attention_kv8_merge(Kv8Args a, int bloc
 }
 
 // ---- launch --------------------------------------------------------------------------
-constexpr int kMaxSplits = 64;
 
-#ifndef WB_FEW
-#define WB_FEW 1024
-#define WB_MANY 512
-#define CH_FEW 4
-#define CH_MANY 4
-#endif
+// One tile: up to 20 pages in one workgroup a head, which saves the merge (1
+// row after 1024 keys 9.7 us, split five ways 6.0 and 3.2 for the merge);
+// beyond, 512 workgroups of 4 to 24 pages (64 ragged sequences of up to 8192:
+// 24 pages 57.6 us, 64 pages 61.7).  More tiles: as many splits as fill the
+// chip's 512 places, of 8 pages or more (192 rows after 2048 keys: 8 pages
+// 29.2 and 6.4 us for the merge, 4 pages 30.5 and 13), or of 4 where these
+// leave most of the chip free (16 rows after 1024 keys: 17.2 against 23.9 us).
 void kv8_plan(Kv8Args& a) {
   const int tiles = (int)(((int64_t)a.H / a.G * a.b.max_rows + 15) / 16);
   a.qt = tiles == 1 ? 0 : tiles <= kWaves ? 1 : 2;
   a.groups = a.qt == 0 ? 1 : (tiles + kWaves * a.qt - 1) / (kWaves * a.qt);
   const int pages = (a.b.max_ctx + kPage - 1) / kPage;
   const int64_t base = (int64_t)a.b.n_seqs * a.G * a.groups;
-  const int wb = a.qt == 0 ? WB_FEW : WB_MANY, ch = a.qt == 0 ? CH_FEW : CH_MANY;
-  const int64_t want = std::min<int64_t>(std::max<int64_t>((wb + base - 1) / base, 1), kMaxSplits);
-  a.chunk = std::max<int>((int)((pages + want - 1) / want), ch);
-  if (a.qt == 0) a.chunk = (a.chunk + kWaves - 1) / kWaves * kWaves;
+  if (a.qt == 0) {
+    const int64_t c = (base * pages / 512 + 2) / 4 * 4;
+    a.chunk = pages <= 20 ? pages : (int)std::min<int64_t>(std::max<int64_t>(c, 4), 24);
+  } else {
+    const int64_t want = std::max<int64_t>(512 / base, 1);
+    a.chunk = std::max<int>((int)((pages + want - 1) / want), base * pages <= 1024 ? 4 : 8);
+  }
+  a.chunk = std::max(a.chunk, (pages + kMaxSplits - 1) / kMaxSplits);
   a.splits = (pages + a.chunk - 1) / a.chunk;
 }
 
 template <typename A, int HD>
-static void attention_qt(const Kv8Args& a, dim3 grid, hipStream_t st) {
-  if (a.qt == 0) k_attention_kv8_few<A, HD><<<grid, 256, 0, st>>>(a);
-  else if (a.qt == 1) k_attention_kv8_many<A, HD, 1><<<grid, 256, 0, st>>>(a);
-  else k_attention_kv8_many<A, HD, 2><<<grid, 256, 0, st>>>(a);
+static void attention_qt(const Kv8Args& a, hipStream_t st) {
+  const dim3 few((unsigned)(a.b.n_seqs * a.G), (unsigned)a.splits);
+  const unsigned many = (unsigned)((a.b.n_seqs * a.G * a.groups * a.splits + kXcds - 1) / kXcds * kXcds);
+  if (a.qt == 0) k_attention_kv8_few<A, HD><<<few, 256, 0, st>>>(a);
+  else if (a.qt == 1) k_attention_kv8_many<A, HD, 1><<<many, 256, 0, st>>>(a);
+  else k_attention_kv8_many<A, HD, 2><<<many, 256, 0, st>>>(a);
 }
 template <typename A> static hipError_t attention_act(const Kv8Args& a, hipStream_t st) {
-  const dim3 grid((unsigned)(a.b.n_seqs * a.G * a.groups), (unsigned)a.splits);
-  if (a.hd == 32) attention_qt<A, 32>(a, grid, st);
-  else if (a.hd == 64) attention_qt<A, 64>(a, grid, st);
-  else attention_qt<A, 128>(a, grid, st);
+  if (a.hd == 32) attention_qt<A, 32>(a, st);
+  else if (a.hd == 64) attention_qt<A, 64>(a, st);
+  else attention_qt<A, 128>(a, st);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  const int blocks = (a.b.max_rows * a.H * (a.hd / 4) + 255) / 256;
-  k_attention_kv8_merge<A><<<(unsigned)(a.b.n_seqs * blocks), 256, 0, st>>>(a, blocks);
+  const int per = 256 / (a.hd / 4 * (a.splits > 8 ? 8 : 1));
+  const int blocks = (a.b.max_rows * a.H + per - 1) / per;
+  if (a.splits > 8) k_attention_kv8_merge<A, 8><<<(unsigned)(a.b.n_seqs * blocks), 256, 0, st>>>(a, blocks);
+  else k_attention_kv8_merge<A, 1><<<(unsigned)(a.b.n_seqs * blocks), 256, 0, st>>>(a, blocks);
   return hipGetLastError();
 }
 hipError_t launch_attention_kv8(int act, const Kv8Args& a, hipStream_t st) {

@@ -96,9 +96,6 @@ template <int MT, int NT, int WM, int WN, int KB> struct MrCfg {
   static constexpr int ACC = mr_acc(MT, NT);
 };
 
-template <int N> __device__ __forceinline__ void wait_vm() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
 // Waits until at most `a` (<= A) stages of C loads each are outstanding.
 template <int C, int A> __device__ __forceinline__ void wait_stages(int a) {
   if constexpr (A == 0) {
@@ -108,22 +105,6 @@ template <int C, int A> __device__ __forceinline__ void wait_stages(int a) {
     else wait_stages<C, A - 1>(a);
   }
 }
-// One 1 KB piece from global memory to LDS without passing registers: lane
-// l's 16 bytes at src + lane16 go to LDS byte dst + 16 l (M0 holds dst; one
-// wait state between its write and the load).  Written as the instruction:
-// the compiler would take every LDS read for a reader of every such load in
-// flight and wait for all of them.  The ring's waits below order them.
-// kStream: the weights of a launch whose blocks share none are read once,
-// with the streaming hint.
-template <bool kStream> __device__ __forceinline__ void dma_1k(const char* src, int lane16, uint32_t dst) {
-  if constexpr (kStream)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(dst), "v"(lane16), "s"(src)
-                 : "memory", "m0");
-  else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(lane16), "s"(src)
-                 : "memory", "m0");
-}
-
 template <int MT, int NT> struct MrFrags {
   uint4 x[MT][2];  // hi, lo
   uint4 w[NT];

@@ -967,6 +967,7 @@ static jf_status check_batch(const jf_batch* b, int n_heads, int n_kv_heads, int
     return fail(JF_E_CAPACITY, "max_ctx %d needs more than table_stride %d pages", b->max_ctx, b->table_stride);
   if (b->max_rows > b->max_ctx) return fail(JF_E_CAPACITY, "max_rows %d exceeds max_ctx %d", b->max_rows, b->max_ctx);
   *none = b->n_seqs == 0 || b->n_rows == 0 || b->max_rows == 0;
+  if (!*none && b->n_pages == 0) return fail(JF_E_CAPACITY, "the pool has no pages");
   if (!*none && (!b->d_row_start || !b->d_ctx || !b->d_page_table)) return fail(JF_E_INVAL, "null array in the batch");
   *out = BatchArgs{b->n_seqs, b->n_rows,      b->max_rows, b->max_ctx,      b->n_pages,
                    b->table_stride, b->d_row_start, b->d_ctx,    b->d_page_table, d_flags};
@@ -1055,6 +1056,8 @@ extern "C" jf_status jf_kv_read(const jf_batch* batch, int32_t n_kv_heads, int32
   a.page_bytes = jf_kv_page_bytes(n_kv_heads, head_dim, kv_dtype);
   a.k = d_k; a.v = d_v;
   a.ld_k = (size_t)ld_k; a.ld_v = (size_t)ld_v;
+  const size_t esz = x_dtype == JF_BF16 ? 2 : 4;
+  a.vec_k = vector4(d_k, ld_k, esz); a.vec_v = vector4(d_v, ld_v, esz);
   HIP_TRY(launch_kv_read(kv_dtype, x_dtype, a, (hipStream_t)stream));
   return JF_OK;
 }
@@ -1072,7 +1075,7 @@ static jf_status kv8_args(const jf_batch* batch, int n_heads, int n_kv_heads, in
   a->H = n_heads; a->G = n_kv_heads; a->hd = head_dim;
   kv8_plan(*a);
   s = check_blocks(std::max<int64_t>((int64_t)n_kv_heads * a->groups * a->splits,
-                                     ((int64_t)batch->max_rows * n_heads * (head_dim / 4) + 255) / 256),
+                                     ((int64_t)batch->max_rows * n_heads * (head_dim / 4) * 8 + 255) / 256),
                    batch->n_seqs);
   return s;
 }

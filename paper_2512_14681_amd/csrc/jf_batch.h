@@ -26,14 +26,14 @@ __device__ __forceinline__ bool batch_seq(const BatchArgs& b, int s, Seq& q) {
   return ok && r1 > r0;
 }
 
-// The physical page of a sequence's page p; -1 (with JF_FLAG_BAD_PAGE raised)
-// if the table names none of the pool's.
-__device__ __forceinline__ int batch_page(const BatchArgs& b, const Seq& q, int p) {
-  const int id = q.table[p];
+// A page table entry's page; -1 (with JF_FLAG_BAD_PAGE raised) if it names
+// none of the pool's.
+__device__ __forceinline__ int batch_page_id(const BatchArgs& b, int id) {
   if ((unsigned)id < (unsigned)b.n_pages) return id;
   if (b.flags) atomicOr(b.flags, kFlagBadPage);
   return -1;
 }
+__device__ __forceinline__ int batch_page(const BatchArgs& b, const Seq& q, int p) { return batch_page_id(b, q.table[p]); }
 
 // ---- 8-bit pages ------------------------------------------------------------------
 // Codes of the keys [G][64 hd], of the values [G][64 hd], then the scales

@@ -93,6 +93,26 @@ __device__ __forceinline__ void mfma(f32x4_t& acc, const Frag<float>& a, const F
   acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.hi.w, b.hi.w, acc, 0, 0, 0);
 }
 
+// ---- global memory to LDS ----------------------------------------------------
+template <int N> __device__ __forceinline__ void wait_vm() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// One 1 KB piece from global memory to LDS without passing registers: lane
+// l's 16 bytes at src + lane16 go to LDS byte dst + 16 l (M0 holds dst; one
+// wait state between its write and the load).  Written as the instruction:
+// the compiler would take every LDS read for a reader of every such load in
+// flight and wait for all of them.  The reader's
+// waits order them.
+// kStream: data that is read once, with the streaming hint.
+template <bool kStream> __device__ __forceinline__ void dma_1k(const char* src, int lane16, uint32_t dst) {
+  if constexpr (kStream)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(dst), "v"(lane16), "s"(src)
+                 : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(lane16), "s"(src)
+                 : "memory", "m0");
+}
+
 // ---- activations -----------------------------------------------------------------
 // A bf16 model computes activations in fp32 and stores each one as two bf16
 // planes, hi = bf16(v) and lo = bf16(v - hi) (plane stride in elements); the

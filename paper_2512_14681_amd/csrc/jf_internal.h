@@ -306,6 +306,7 @@ struct ReadArgs {
   size_t page_bytes;
   void *k, *v;               // rows [n_rows][ld]
   size_t ld_k, ld_v;
+  int vec_k, vec_v;          // every four elements from a multiple of 4 are aligned
   int pages;
 };
 hipError_t launch_kv_read(int kv_dtype, int x_dtype, ReadArgs& a, hipStream_t stream);

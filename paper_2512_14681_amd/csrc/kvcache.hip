@@ -44,30 +44,37 @@ __device__ __forceinline__ void append_queries(const AppendArgs& a, const Seq& q
   const int c = item % kChunks, h0 = item / kChunks % hb * kQHeads, i = item / kChunks / hb;
   if (i >= q.n) return;
   const int row = q.r0 + i;
-  float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
-  if (a.rotate) angles4(a.freq, 4 * c, a.pos ? a.pos[row] : q.C + i, cs, sn);
+  const int pos = a.pos ? a.pos[row] : q.C + i;
   const X* x = reinterpret_cast<const X*>(a.q) + (size_t)row * a.ld_q;
   A* out = reinterpret_cast<A*>(a.q_out) + (size_t)row * a.H * HD;
+  // all loads before the first store, which they could not pass
+  float u[kQHeads][4], w[kQHeads][4];
+#pragma unroll
+  for (int hh = 0; hh < kQHeads; ++hh) {
+    const int h = min(h0 + hh, a.H - 1);
+    load4(x + (size_t)h * HD + 4 * c, a.vec_q, u[hh]);
+    load4(x + (size_t)h * HD + HD / 2 + 4 * c, a.vec_q, w[hh]);
+  }
+  float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
+  if (a.rotate) angles4(a.freq, 4 * c, pos, cs, sn);
 #pragma unroll
   for (int hh = 0; hh < kQHeads; ++hh) {
     const int h = h0 + hh;
     if (h >= a.H) break;
-    float u[4], w[4], y[4], z[4];
-    load4(x + (size_t)h * HD + 4 * c, a.vec_q, u);
-    load4(x + (size_t)h * HD + HD / 2 + 4 * c, a.vec_q, w);
+    float y[4], z[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      y[e] = a.rotate ? u[e] * cs[e] - w[e] * sn[e] : u[e];
-      z[e] = a.rotate ? w[e] * cs[e] + u[e] * sn[e] : w[e];
+      y[e] = a.rotate ? u[hh][e] * cs[e] - w[hh][e] * sn[e] : u[hh][e];
+      z[e] = a.rotate ? w[hh][e] * cs[e] + u[hh][e] * sn[e] : w[hh][e];
     }
     act_store4(out + (size_t)h * HD + 4 * c, a.q_plane, y);
     act_store4(out + (size_t)h * HD + HD / 2 + 4 * c, a.q_plane, z);
   }
 }
 
-template <int HD, typename T> struct AppendShared { T v[HD][kPage + 8]; };   // values transposed
+template <int HD, typename T> struct AppendShared { alignas(16) T v[HD][kPage + 16 / sizeof(T)]; };   // values transposed
 template <int HD> struct AppendShared<HD, uint8_t> {
-  uint32_t code[2][16 * HD];  // a head's key and value codes in the page's order
+  alignas(16) uint32_t code[2][16 * HD];  // a head's key and value codes in the page's order
   float amax[2][4];
 };
 
@@ -88,12 +95,11 @@ __global__ void __launch_bounds__(256) k_kv_append(AppendArgs a) {
   const int t0 = max(q.C - page * kPage, 0);                 // first new token of the page
   const int t1 = min(q.C + q.n - page * kPage, kPage);       // past the last one
   if (t1 <= t0) return;
-  const int id = batch_page(a.b, q, page);
-  if (id < 0) return;
+  const int entry = q.table[page];                           // looked at when the rows are on their way
   const int tid = threadIdx.x;
   const int row0 = q.r0 + page * kPage - q.C;                // the row of the page's token 0
 
-  // the new keys (rotated) and values, in registers
+  // the new keys and values, in registers
   float x[kItems][2][8];
   float kmax = 0.f, vmax = 0.f;
 #pragma unroll
@@ -105,19 +111,27 @@ __global__ void __launch_bounds__(256) k_kv_append(AppendArgs a) {
       const int row = row0 + t;
       const X* kp = reinterpret_cast<const X*>(a.k) + (size_t)row * a.ld_k + (size_t)g * HD + 4 * c;
       const X* vp = reinterpret_cast<const X*>(a.v) + (size_t)row * a.ld_v + (size_t)g * HD + 4 * c;
-      float u[4], w[4], p[4], r[4];
-      load4(kp, a.vec_k, u);
-      load4(kp + HD / 2, a.vec_k, w);
-      load4(vp, a.vec_v, p);
-      load4(vp + HD / 2, a.vec_v, r);
-      float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
-      if (a.rotate) angles4(a.freq, 4 * c, a.pos ? a.pos[row] : q.C + row - q.r0, cs, sn);
+      load4(kp, a.vec_k, reinterpret_cast<float(&)[4]>(x[n][0][0]));
+      load4(kp + HD / 2, a.vec_k, reinterpret_cast<float(&)[4]>(x[n][0][4]));
+      load4(vp, a.vec_v, reinterpret_cast<float(&)[4]>(x[n][1][0]));
+      load4(vp + HD / 2, a.vec_v, reinterpret_cast<float(&)[4]>(x[n][1][4]));
+    }
+  }
+  const int id = batch_page_id(a.b, entry);
+  if (id < 0) return;
+  if (a.rotate) {
+#pragma unroll
+    for (int n = 0; n < kItems; ++n) {
+      const int item = n * 256 + tid, c = item % (HD / 8), t = item / (HD / 8);
+      if (t < t0 || t >= t1) continue;
+      const int row = row0 + t;
+      float cs[4], sn[4];
+      angles4(a.freq, 4 * c, a.pos ? a.pos[row] : q.C + row - q.r0, cs, sn);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        x[n][0][e] = a.rotate ? u[e] * cs[e] - w[e] * sn[e] : u[e];
-        x[n][0][4 + e] = a.rotate ? w[e] * cs[e] + u[e] * sn[e] : w[e];
-        x[n][1][e] = p[e];
-        x[n][1][4 + e] = r[e];
+        const float u = x[n][0][e], w = x[n][0][4 + e];
+        x[n][0][e] = u * cs[e] - w * sn[e];
+        x[n][0][4 + e] = w * cs[e] + u * sn[e];
       }
     }
   }
@@ -136,9 +150,20 @@ __global__ void __launch_bounds__(256) k_kv_append(AppendArgs a) {
       for (int e = 0; e < 8; ++e) sh.v[(e / 4) * (HD / 2) + 4 * c + e % 4][t] = from_f32<KV>(x[n][1][e]);
     }
     __syncthreads();
-    const int m = t1 - t0;
-    for (int i = tid; i < m * HD; i += 256) vd[(size_t)(i / m) * kPage + t0 + i % m] = sh.v[i / m][t0 + i % m];
+    // 16 bytes along the tokens of a dim where all of them are new
+    constexpr int N = 16 / (int)sizeof(KV);
+    for (int i = tid; i < HD * (kPage / N); i += 256) {
+      const int d = i / (kPage / N), t = i % (kPage / N) * N;
+      KV* p = vd + (size_t)d * kPage + t;
+      if (t >= t0 && t + N <= t1) {
+        *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(&sh.v[d][t]);
+      } else {
+        for (int e = max(t0 - t, 0); e < min(t1 - t, N); ++e) p[e] = sh.v[d][t + e];
+      }
+    }
   } else {
+    float* scales = reinterpret_cast<float*>(base + (size_t)2 * a.G * kPage * HD) + 2 * g;
+    const float held[2] = {scales[0], scales[1]};
 #pragma unroll
     for (int n = 0; n < kItems; ++n)
 #pragma unroll
@@ -158,7 +183,6 @@ __global__ void __launch_bounds__(256) k_kv_append(AppendArgs a) {
       sh.amax[1][tid >> 6] = vmax;
     }
     __syncthreads();
-    float* scales = reinterpret_cast<float*>(base + (size_t)2 * a.G * kPage * HD) + 2 * g;
     uint32_t* codes[2] = {reinterpret_cast<uint32_t*>(base + (size_t)g * kPage * HD),
                           reinterpret_cast<uint32_t*>(base + (size_t)(a.G + g) * kPage * HD)};
     int from[2];          // first token whose codes are written
@@ -167,7 +191,7 @@ __global__ void __launch_bounds__(256) k_kv_append(AppendArgs a) {
     for (int w = 0; w < 2; ++w) {
       const float amax = fmaxf(fmaxf(sh.amax[w][0], sh.amax[w][1]), fmaxf(sh.amax[w][2], sh.amax[w][3]));
       const float need = f8_block_scale(amax);
-      const float old = t0 > 0 ? scales[w] : need;
+      const float old = t0 > 0 ? held[w] : need;
       const float sc = fmaxf(old, need);
       inv[w] = 1.f / sc;  // a power of two: exact
       from[w] = t0;
@@ -205,6 +229,19 @@ __global__ void __launch_bounds__(256) k_kv_append(AppendArgs a) {
       }
     }
     __syncthreads();
+    if (from[0] == 0 && from[1] == 0 && t1 == kPage) {  // a whole page
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int i = 0; i < HD / 64; ++i)
+          reinterpret_cast<uint4*>(codes[w])[i * 256 + tid] = reinterpret_cast<const uint4*>(sh.code[w])[i * 256 + tid];
+      if constexpr (HD < 64)
+        if (tid < 128)
+#pragma unroll
+          for (int w = 0; w < 2; ++w)
+            reinterpret_cast<uint4*>(codes[w])[tid] = reinterpret_cast<const uint4*>(sh.code[w])[tid];
+      return;
+    }
     // Words of four dims of one token (keys), of four tokens of one dim
     // (values); only the tokens written change.
     for (int i = tid; i < 16 * HD; i += 256) {
@@ -225,12 +262,23 @@ __global__ void __launch_bounds__(256) k_kv_append(AppendArgs a) {
 }
 
 // ---- reading back --------------------------------------------------------------------
-template <typename T> __device__ __forceinline__ float cached(const T* p) { return to_f32<T>(*p); }
+template <typename X> __device__ __forceinline__ void put4(X* p, bool vec, const float (&v)[4]) {
+  if (vec) {
+    store4<X>(p, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = from_f32<X>(v[e]);
+  }
+}
 
 // A workgroup: one head of one page.  KV as above; X: float or bf16_t rows.
+// What is transposed in the page (values; all codes) passes through LDS: 16
+// bytes a load, all of them in flight at once; four dims of a token a store.
 template <typename X, typename KV, int HD>
 __global__ void __launch_bounds__(256) k_kv_read(ReadArgs a) {
-  __shared__ float sv[kPage][HD + 1];
+  constexpr int N = 16 / (int)sizeof(KV);                 // elements of 16 bytes
+  constexpr int kRow = kPage + N;                         // a dim's tokens in LDS
+  __shared__ alignas(16) KV sh[sizeof(KV) > 1 ? HD * kRow : 2 * HD * kPage];
   const int per = a.pages * a.G;
   const int s = blockIdx.x / per, it = blockIdx.x % per;
   Seq q;
@@ -243,40 +291,57 @@ __global__ void __launch_bounds__(256) k_kv_read(ReadArgs a) {
   const int tid = threadIdx.x;
   const int row0 = q.r0 + page * kPage - q.C;
   const char* base = reinterpret_cast<const char*>(a.kv) + (size_t)id * a.page_bytes;
+  const KV* kp = reinterpret_cast<const KV*>(base) + (size_t)g * kPage * HD;
+  const KV* vp = reinterpret_cast<const KV*>(base) + (size_t)(a.G + g) * kPage * HD;
+  float scale[2] = {1.f, 1.f};
+  if constexpr (sizeof(KV) > 1) {
+#pragma unroll 4
+    for (int i = tid; i < HD * (kPage / N); i += 256) {
+      const int d = i / (kPage / N), t = i % (kPage / N) * N;
+      if (t < t1 && t + N > t0)
+        *reinterpret_cast<uint4*>(sh + d * kRow + t) = *reinterpret_cast<const uint4*>(vp + (size_t)d * kPage + t);
+    }
+  } else {
+    const float2 sc = reinterpret_cast<const float2*>(base + (size_t)2 * a.G * kPage * HD)[g];
+    scale[0] = sc.x;
+    scale[1] = sc.y;
+    constexpr int kEach = (4 * HD + 255) / 256;           // a thread's 16 bytes of the 64 hd of each kind
+    uint4 r[2][kEach];
 #pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    if (w) __syncthreads();
+    for (int i = 0; i < kEach; ++i)
+      if (i * 256 + tid < 4 * HD) {
+        r[0][i] = reinterpret_cast<const uint4*>(kp)[i * 256 + tid];
+        r[1][i] = reinterpret_cast<const uint4*>(vp)[i * 256 + tid];
+      }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (i * 256 + tid < 4 * HD) {
+        reinterpret_cast<uint4*>(sh)[i * 256 + tid] = r[0][i];
+        reinterpret_cast<uint4*>(sh + HD * kPage)[i * 256 + tid] = r[1][i];
+      }
+  }
+  __syncthreads();
+  for (int i = tid; i < (t1 - t0) * (HD / 4); i += 256) {
+    const int t = t0 + i / (HD / 4), d = i % (HD / 4) * 4;
+    float k[4], v[4];
     if constexpr (sizeof(KV) > 1) {
-      const KV* p = reinterpret_cast<const KV*>(base) + (size_t)(w ? a.G + g : g) * kPage * HD;
-      for (int i = tid; i < kPage * HD; i += 256) {
-        const int t = w ? i % kPage : i / HD, d = w ? i / kPage : i % HD;
-        if (t >= t0 && t < t1) sv[t][d] = to_f32<KV>(p[i]);
-      }
+      load4(kp + (size_t)t * HD + d, true, k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = to_f32<KV>(sh[(d + e) * kRow + t]);
     } else {
-      const uint32_t* p = reinterpret_cast<const uint32_t*>(base + (size_t)(w ? a.G + g : g) * kPage * HD);
-      const float sc = reinterpret_cast<const float*>(base + (size_t)2 * a.G * kPage * HD)[2 * g + w];
-      for (int i = tid; i < 16 * HD; i += 256) {
-        float v[4];
-        f8_unpack4(p[i], v);
-        const int lane = (i >> 2) & 63, b = (i >> 8) * 16 + (i & 3) * 4;
-        if (w == 0) {
-          const int t = (b / (HD / 4)) * 16 + (lane & 15), d = (lane >> 4) * (HD / 4) + b % (HD / 4);
+      f8_unpack4(*reinterpret_cast<const uint32_t*>(sh + kv8_key_offset(t, d, HD)), k);
+      uint32_t w = 0;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sv[t][d + e] = v[e] * sc;
-        } else {
-          const int t = (i & 3) * 16 + (lane >> 4) * 4, d = (i >> 8) * 16 + (lane & 15);
+      for (int e = 0; e < 4; ++e) w |= (uint32_t)sh[HD * kPage + kv8_value_offset(t, d + e)] << (8 * e);
+      f8_unpack4(w, v);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sv[t + e][d] = v[e] * sc;
-        }
+      for (int e = 0; e < 4; ++e) {
+        k[e] *= scale[0];
+        v[e] *= scale[1];
       }
     }
-    __syncthreads();
-    X* out = reinterpret_cast<X*>(w ? a.v : a.k);
-    const size_t ld = w ? a.ld_v : a.ld_k;
-    for (int i = tid; i < (t1 - t0) * HD; i += 256) {
-      const int t = t0 + i / HD, d = i % HD;
-      out[(size_t)(row0 + t) * ld + (size_t)g * HD + d] = from_f32<X>(sv[t][d]);
-    }
+    put4(reinterpret_cast<X*>(a.k) + (size_t)(row0 + t) * a.ld_k + (size_t)g * HD + d, a.vec_k, k);
+    put4(reinterpret_cast<X*>(a.v) + (size_t)(row0 + t) * a.ld_v + (size_t)g * HD + d, a.vec_v, v);
   }
 }
 

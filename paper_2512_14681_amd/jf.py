@@ -282,30 +282,82 @@ def trajectory_select(d_traj, d_len, n_blocks, n, max_points, w, d_sel, d_t_num=
                                      int(w), _ptr(d_t_num), _ptr(d_sel), _ptr(d_unconv), _stream(stream)))
 
 
-# ---- batches of sequences over a paged cache (component calls, no model) --------------
+# ---- batches of sequences over a paged cache, log probabilities (component calls) -----
+_DTYPES = {}
+
+
+def _types():
+    """{torch dtype: jf_dtype} of rows, and int32; torch is imported at the first use."""
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: JF_F32, torch.bfloat16: JF_BF16})
+        global _I32, _F32, _current_device, _current_stream
+        _I32, _F32 = torch.int32, torch.float32
+        _current_device, _current_stream = torch.cuda.current_device, torch.cuda.current_stream
+    return _DTYPES
+
+
+def _at(dev, t):
+    """Address of a tensor on the current GPU; None stays None."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        raise ValueError(f"a tensor is on {t.device}, the call runs on GPU {dev}")
+    return t.data_ptr()
+
+
+def _vec(dev, t, dtype, n):
+    """Address of a contiguous tensor of n elements or more."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+        raise TypeError(f"expected a contiguous {dtype} tensor of {n} elements, got {tuple(t.shape)} of {t.dtype}")
+    return _at(dev, t)
+
+
+def _rows(t):
+    """(jf_dtype, row stride in elements) of a [rows][columns] tensor of fp32 or bf16 whose rows are contiguous."""
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        code = _types().get(t.dtype)
+    if code is None or t.dim() != 2:
+        raise TypeError("rows are 2-dimensional fp32 or bf16 tensors")
+    ld, step = t.stride()
+    if step != 1 and t.size(1) > 1:
+        raise TypeError("a row's elements lie side by side")
+    if ld < t.size(1) and t.size(0) <= 1:   # the stride of a single row says nothing
+        ld = t.size(1)
+    return code, ld
+
+
+def _on(stream):
+    return (stream if stream is not None else _current_stream()).cuda_stream
+
+
 class Batch:
     """A jf_batch over device int32 tensors (kept alive here): row_start [n_seqs + 1], ctx [n_seqs] and
     page_table [n_seqs][stride], with the host's bounds."""
 
     def __init__(self, row_start, ctx, page_table, n_rows, max_rows, max_ctx, n_pages):
+        _types()
         self.tensors = (row_start, ctx, page_table)
         for t in self.tensors:
-            if str(t.dtype) != "torch.int32" or not t.is_contiguous():
+            if t.dtype is not _I32 or not t.is_contiguous():
                 raise TypeError("row_start, ctx and page_table are contiguous int32 tensors")
         n = ctx.numel()
-        if row_start.numel() != n + 1 or page_table.shape[0] != n:
+        if row_start.numel() != n + 1 or page_table.dim() != 2 or page_table.shape[0] != n:
             raise ValueError(f"{n} sequences need {n + 1} row starts and {n} rows of the page table")
-        self.c = JfBatch(n, int(n_rows), int(max_rows), int(max_ctx), int(n_pages), int(page_table.shape[1]),
+        if not ctx.get_device() == row_start.get_device() == page_table.get_device():
+            raise ValueError("row_start, ctx and page_table are on one device")
+        self.device, self.n_rows = ctx.get_device(), int(n_rows)
+        self.c = JfBatch(n, self.n_rows, int(max_rows), int(max_ctx), int(n_pages), int(page_table.shape[1]),
                          row_start.data_ptr(), ctx.data_ptr(), page_table.data_ptr())
         self.ref = ctypes.byref(self.c)
 
-
-def _rows(t):
-    """(jf_dtype, row stride in elements) of a [rows][columns] tensor of fp32 or bf16 whose rows are contiguous."""
-    code = {"torch.float32": JF_F32, "torch.bfloat16": JF_BF16}.get(str(t.dtype))
-    if code is None or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise TypeError("rows are 2-dimensional fp32 or bf16 tensors with contiguous rows")
-    return code, t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    def on(self, dev):
+        if self.device != dev:
+            raise ValueError(f"the batch is on device {self.device}, the call runs on GPU {dev}")
+        return self.ref
 
 
 def kv_page_bytes(n_kv_heads, head_dim, kv_dtype):
@@ -319,9 +371,12 @@ def kv_append(batch, n_heads, n_kv_heads, head_dim, kv_dtype, d_kv, d_k, d_v, d_
     xq, ld_q = _rows(d_q) if d_q is not None else (x, 0)
     if not x == xv == xq:
         raise TypeError("queries, keys and values have one type")
-    check(lib().jf_kv_append(batch.ref, n_heads, n_kv_heads, head_dim, kv_dtype, x, act_dtype, _ptr(d_q), ld_q,
-                             _ptr(d_k), ld_k, _ptr(d_v), ld_v, _ptr(d_pos), rope_base, _ptr(d_kv), _ptr(d_q_out),
-                             _ptr(d_flags), _stream(stream)))
+    dev = _current_device()
+    status = lib().jf_kv_append(batch.on(dev), n_heads, n_kv_heads, head_dim, kv_dtype, x, act_dtype, _at(dev, d_q),
+                                ld_q, _at(dev, d_k), ld_k, _at(dev, d_v), ld_v, _vec(dev, d_pos, _I32, batch.n_rows),
+                                rope_base, _at(dev, d_kv), _at(dev, d_q_out), _vec(dev, d_flags, _I32, 1), _on(stream))
+    if status:
+        check(status)
 
 
 def kv_read(batch, n_kv_heads, head_dim, kv_dtype, d_kv, d_k, d_v, d_flags=None, stream=None):
@@ -329,8 +384,11 @@ def kv_read(batch, n_kv_heads, head_dim, kv_dtype, d_kv, d_k, d_v, d_flags=None,
     xv, ld_v = _rows(d_v)
     if x != xv:
         raise TypeError("keys and values have one type")
-    check(lib().jf_kv_read(batch.ref, n_kv_heads, head_dim, kv_dtype, x, _ptr(d_kv), _ptr(d_k), ld_k, _ptr(d_v), ld_v,
-                           _ptr(d_flags), _stream(stream)))
+    dev = _current_device()
+    status = lib().jf_kv_read(batch.on(dev), n_kv_heads, head_dim, kv_dtype, x, _at(dev, d_kv), _at(dev, d_k), ld_k,
+                              _at(dev, d_v), ld_v, _vec(dev, d_flags, _I32, 1), _on(stream))
+    if status:
+        check(status)
 
 
 def attention_kv8_ws_bytes(batch, n_heads, n_kv_heads, head_dim):
@@ -342,11 +400,15 @@ def attention_kv8_ws_bytes(batch, n_heads, n_kv_heads, head_dim):
 
 def attention_kv8(batch, n_heads, n_kv_heads, head_dim, act_dtype, d_q, d_kv, d_out, d_ws, d_vis=None, d_flags=None,
                   stream=None):
-    check(lib().jf_attention_kv8(batch.ref, n_heads, n_kv_heads, head_dim, act_dtype, _ptr(d_q), _ptr(d_kv),
-                                 _ptr(d_vis), _ptr(d_out), _ptr(d_ws), _ptr(d_flags), _stream(stream)))
+    _types()
+    dev = _current_device()
+    status = lib().jf_attention_kv8(batch.on(dev), n_heads, n_kv_heads, head_dim, act_dtype, _at(dev, d_q),
+                                    _at(dev, d_kv), _at(dev, d_vis), _at(dev, d_out), _at(dev, d_ws),
+                                    _vec(dev, d_flags, _I32, 1), _on(stream))
+    if status:
+        check(status)
 
 
-# ---- log probabilities (component calls, no model) -------------------------------------
 def token_logprobs_ws_bytes(R, V, k=0):
     return lib().jf_token_logprobs_ws_bytes(int(R), int(V), int(k))
 
@@ -354,9 +416,14 @@ def token_logprobs_ws_bytes(R, V, k=0):
 def token_logprobs(d_logits, d_ws, d_tokens=None, k=0, d_logprob=None, d_entropy=None, d_norm=None, d_top_ids=None,
                    d_top_logprob=None, stream=None):
     x, ld = _rows(d_logits)
-    check(lib().jf_token_logprobs(d_logits.shape[0], d_logits.shape[1], x, _ptr(d_logits), ld, _ptr(d_tokens), k,
-                                  _ptr(d_logprob), _ptr(d_entropy), _ptr(d_norm), _ptr(d_top_ids),
-                                  _ptr(d_top_logprob), _ptr(d_ws), _stream(stream)))
+    R, V = d_logits.shape
+    dev = _current_device()
+    status = lib().jf_token_logprobs(R, V, x, _at(dev, d_logits), ld, _vec(dev, d_tokens, _I32, R), k,
+                                     _vec(dev, d_logprob, _F32, R), _vec(dev, d_entropy, _F32, R),
+                                     _vec(dev, d_norm, _F32, 2 * R), _vec(dev, d_top_ids, _I32, R * k),
+                                     _vec(dev, d_top_logprob, _F32, R * k), _at(dev, d_ws), _on(stream))
+    if status:
+        check(status)
 
 
 def token_logprobs_grad(d_logits, d_norm, d_grad, d_tokens=None, d_entropy=None, d_g_logprob=None, d_g_entropy=None,
@@ -365,6 +432,11 @@ def token_logprobs_grad(d_logits, d_norm, d_grad, d_tokens=None, d_entropy=None,
     xg, ld_g = _rows(d_grad)
     if x != xg or d_grad.shape != d_logits.shape:
         raise TypeError("the gradient has the logits' shape and type")
-    check(lib().jf_token_logprobs_grad(d_logits.shape[0], d_logits.shape[1], x, _ptr(d_logits), ld, _ptr(d_tokens),
-                                       _ptr(d_norm), _ptr(d_entropy), _ptr(d_g_logprob), _ptr(d_g_entropy),
-                                       _ptr(d_grad), ld_g, _stream(stream)))
+    R, V = d_logits.shape
+    dev = _current_device()
+    status = lib().jf_token_logprobs_grad(R, V, x, _at(dev, d_logits), ld, _vec(dev, d_tokens, _I32, R),
+                                          _vec(dev, d_norm, _F32, 2 * R), _vec(dev, d_entropy, _F32, R),
+                                          _vec(dev, d_g_logprob, _F32, R), _vec(dev, d_g_entropy, _F32, R),
+                                          _at(dev, d_grad), ld_g, _on(stream))
+    if status:
+        check(status)

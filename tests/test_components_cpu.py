@@ -47,7 +47,7 @@ BAD_BATCHES = [
     (dict(n_seqs=-1), jf.JF_E_INVAL), (dict(n_rows=-1), jf.JF_E_INVAL), (dict(n_pages=-1), jf.JF_E_INVAL),
     (dict(max_ctx=129), jf.JF_E_CAPACITY), (dict(max_rows=129), jf.JF_E_CAPACITY),
     (dict(max_ctx=(1 << 30) + 1, table_stride=1 << 30), jf.JF_E_CAPACITY),
-    (dict(d_row_start=None), jf.JF_E_INVAL), (dict(d_ctx=None), jf.JF_E_INVAL),
+    (dict(n_pages=0), jf.JF_E_CAPACITY), (dict(d_row_start=None), jf.JF_E_INVAL), (dict(d_ctx=None), jf.JF_E_INVAL),
     (dict(d_page_table=None), jf.JF_E_INVAL),
 ]
 
@@ -170,9 +170,29 @@ def test_binding_checks_its_tensors():
         jf.Batch(torch.zeros(3), torch.zeros(2, **i32), torch.zeros(2, 1, **i32), 4, 2, 64, 1)
     with pytest.raises(ValueError):
         jf.Batch(torch.zeros(2, **i32), torch.zeros(2, **i32), torch.zeros(2, 1, **i32), 4, 2, 64, 1)
+    with pytest.raises(ValueError):
+        jf.Batch(torch.zeros(3, **i32), torch.zeros(2, **i32), torch.zeros(2, **i32), 4, 2, 64, 1)
     with pytest.raises(TypeError):
         jf.token_logprobs(torch.zeros(4, 8, dtype=torch.float16), None)
     with pytest.raises(TypeError):
         jf.token_logprobs(torch.zeros(8, 4).t(), None)
     with pytest.raises(TypeError):
         jf.token_logprobs_grad(torch.zeros(4, 8), None, torch.zeros(4, 8, dtype=torch.bfloat16))
+
+
+def test_binding_refuses_tensors_elsewhere(monkeypatch):
+    """Host tensors, short vectors and other types never reach the library as addresses."""
+    import torch
+    jf._types()
+    monkeypatch.setattr(jf, "_current_device", lambda: 0)
+    x, i32 = torch.zeros(4, 8), dict(dtype=torch.int32)
+    with pytest.raises(ValueError, match="on cpu"):
+        jf.token_logprobs(x, torch.zeros(1024, dtype=torch.uint8))
+    with pytest.raises(TypeError, match="int32"):
+        jf._vec(0, torch.zeros(4, dtype=torch.int64), torch.int32, 4)
+    for bad in (torch.zeros(3), torch.zeros(8)[::2], torch.zeros(4, dtype=torch.bfloat16)):
+        with pytest.raises((TypeError, ValueError)):
+            jf._vec(0, bad, torch.float32, 4)
+    b = jf.Batch(torch.zeros(3, **i32), torch.zeros(2, **i32), torch.zeros(2, 1, **i32), 4, 2, 64, 1)
+    with pytest.raises(ValueError, match="batch is on"):
+        jf.kv_read(b, 1, 32, jf.JF_BF16, x, torch.zeros(4, 32), torch.zeros(4, 32))
