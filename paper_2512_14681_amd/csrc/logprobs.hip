@@ -4,12 +4,13 @@
 // One pass over a row's logits x with m = max x, s = sum e^(x - m) and
 // u = sum e^(x - m) (x - m), all in fp32 and relative to the running maximum:
 //   log p_t = (x_t - m) - log s,   entropy = log s - u / s.
-// The alternatives are the k largest 64-bit keys (value, then lowest index);
-// a wave keeps its k best sorted over its lanes.  Bound by memory without
-// alternatives (512 rows of 152064 fp32 logits 56 us, 5.6 TB/s, kept in the
-// caches for the gradient; 50 us if loaded as read once, which calls with
-// alternatives do), by the vector unit with them (64 rows in bf16: k = 0 8 us,
-// k = 8 15 us).
+// The alternatives are the k largest 64-bit keys (value, then lowest index).
+// Bound by memory without alternatives (512 rows of 152064 fp32 logits 56 us,
+// 5.6 TB/s, kept in the caches for the gradient; 50 us if loaded as read once,
+// which calls with alternatives do), by the vector unit with them where the
+// rows are few (64 rows in bf16: k = 0 8 us, k = 8 13 us; 400 rows in fp32 and
+// k = 8 46 us, 5.2 TB/s).  A row is split until there are about four
+// workgroups a compute unit; a second launch joins (4 us).
 #include <algorithm>
 
 #include "jf_device.h"
@@ -94,34 +95,6 @@ __device__ __forceinline__ float key_value(uint64_t k) {
   return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
 }
 
-// A wave's best keys, largest first, one a lane (0: none).
-struct TopList {
-  uint64_t key, kth;  // this lane's; the k-th best (every lane)
-  float least;        // the k-th best's value: nothing below it is looked at
-  int k;
-  __device__ __forceinline__ void init(int k_) { key = kth = 0; least = -INFINITY; k = k_; }
-  // Puts one key (the same in every lane) in its place.
-  __device__ __forceinline__ void insert(uint64_t c) {
-    const int lane = threadIdx.x & 63;
-    const int at = __popcll(__ballot(key > c));
-    const uint64_t up = from_lane_below(key);
-    key = lane < at ? key : (lane == at ? c : up);
-    kth = from_lane(key, k - 1);
-    least = kth ? key_value(kth) : -INFINITY;
-  }
-  // Offers one element a lane.
-  __device__ __forceinline__ void offer(float v, int col) {
-    if (!__any(v >= least && v > -INFINITY)) return;
-    const uint64_t c = v > -INFINITY ? argmax_key(v, (uint32_t)col) : 0;
-    uint64_t left = __ballot(c > kth);
-    while (left) {
-      const uint64_t x = from_lane(c, __builtin_ctzll(left));
-      left &= left - 1;
-      if (x > kth) insert(x);
-    }
-  }
-};
-
 // Keys larger than `key` among n in LDS (zeros up to the next multiple of 8):
 // its place in their order.
 __device__ __forceinline__ int key_rank(const uint64_t* keys, int n, uint64_t key) {
@@ -132,56 +105,118 @@ __device__ __forceinline__ int key_rank(const uint64_t* keys, int n, uint64_t ke
   return rank;
 }
 
-// A wave's first tile.  The k-th largest of its 64 lanes' maxima has k
-// elements at or above it, so the k best are among those that reach it (few
-// more than k unless they sit in few lanes): these are put side by side in
-// LDS and ranked by counting.  The threshold is searched bit by bit in the
-// upper half of the ordered values only: a little lower, which admits a few
-// more.  false: more than kCand of them, nothing done.
+// A wave's best keys.  It collects candidates side by side in LDS, elements
+// above a value that k earlier ones reach, and ranks them by counting when
+// they are too many and at the end, so that most tiles cost a comparison an
+// element (kept sorted over the lanes instead, key by key, 64 rows of 152064
+// bf16 logits took 15.2 us for k = 8 and 20.7 for k = 20, now 13.2 and 17.4).
 constexpr int kCand = 128;
-template <typename T>
-__device__ __forceinline__ bool top_first(TopList& top, const float (&x)[kTileElems], float mx, int base, int tid,
-                                          uint64_t* cand, uint64_t* best) {
-  const int lane = tid & 63;
-  const uint32_t u = __float_as_uint(mx), om = mx > -INFINITY ? ((u & 0x80000000u) ? ~u : (u | 0x80000000u)) : 0;
-  uint32_t t = 0;
-#pragma unroll
-  for (int b = 31; b >= 16; --b) {
-    const uint32_t with = t | 1u << b;
-    t = __popcll(__ballot(om >= with)) >= top.k ? with : t;
+template <typename T> struct TopList {
+  uint64_t* cand;  // kCand of this wave
+  uint64_t* best;  // kMaxTop of this wave: scratch
+  int k, n;
+  float least;     // k candidates reach it (-inf: not known of k)
+  __device__ __forceinline__ void init(int k_, uint64_t* cand_, uint64_t* best_) {
+    k = k_; cand = cand_; best = best_;
+    n = 0;
+    least = -INFINITY;
   }
-  // 0: fewer than k lanes hold anything, and everything finite is a candidate
-  const float least = t ? key_value((uint64_t)t << 32) : -INFINITY;
+  static __device__ __forceinline__ void fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
+  // This lane's of the k best candidates in order (0: none), which alone stay.
+  __device__ __forceinline__ uint64_t rank() {
+    const int lane = threadIdx.x & 63;
+    if (lane < 8 && n + lane < kCand) cand[n + lane] = 0;
+    if (lane < kMaxTop) best[lane] = 0;
+    fence();
 #pragma unroll
-  for (int h = 0; h < kCand; h += 64) cand[h + lane] = 0;
-  if (lane < kMaxTop) best[lane] = 0;
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  int n = 0;
-#pragma unroll
-  for (int j = 0; j < kTileElems; ++j) {
-    const bool in = x[j] >= least && x[j] > -INFINITY;
-    const uint64_t mask = __ballot(in);
-    if (mask) {
-      const int at = n + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
-      if (in && at < kCand) cand[at] = argmax_key(x[j], (uint32_t)tile_col<T>(base, tid, j));
-      n += __popcll(mask);
-    }
+    for (int h = 0; h < kCand; h += 64)
+      if (h + lane < n) {
+        const uint64_t key = cand[h + lane];
+        const int at = key_rank(cand, n, key);
+        if (at < k) best[at] = key;
+      }
+    fence();
+    const uint64_t key = lane < k ? best[lane] : 0;
+    keep(key);
+    return key;
   }
-  if (n > kCand) return false;
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  // The candidates become these: the k best in order, one a lane.
+  __device__ __forceinline__ void keep(uint64_t key) {
+    const int lane = threadIdx.x & 63;
+    n = __popcll(__ballot(lane < k && key));
+    if (lane < k) cand[lane] = key;
+    const uint64_t kth = from_lane(key, k - 1);
+    if (kth) least = key_value(kth);
+    fence();
+  }
+  // Adds the elements for which in(value); false (and nothing added) if they do not fit.
+  template <typename F>
+  __device__ __forceinline__ bool add(const float (&x)[kTileElems], int base, int tid, F in) {
+    int to = n;
 #pragma unroll
-  for (int h = 0; h < kCand; h += 64)
-    if (h + lane < n) {
-      const uint64_t key = cand[h + lane];
-      const int rank = key_rank(cand, n, key);
-      if (rank < top.k) best[rank] = key;
+    for (int j = 0; j < kTileElems; ++j) {
+      const bool it = in(x[j]);
+      const uint64_t mask = __ballot(it);
+      if (mask) {
+        const int at = to + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+        if (it && at < kCand) cand[at] = argmax_key(x[j], (uint32_t)tile_col<T>(base, tid, j));
+        to += __popcll(mask);
+      }
     }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  top.key = lane < top.k ? best[lane] : 0;
-  top.kth = best[top.k - 1];
-  top.least = top.kth ? key_value(top.kth) : -INFINITY;
-  return true;
-}
+    if (to > kCand) return false;
+    n = to;
+    return true;
+  }
+  // A value that k of the tile's elements reach (-inf: not known of k): the
+  // k-th largest of the lanes' maxima, searched bit by bit in the upper half
+  // of the ordered values only; a little lower, which admits a few more.
+  __device__ __forceinline__ float reached(float mx) const {
+    const uint32_t u = __float_as_uint(mx), om = mx > -INFINITY ? ((u & 0x80000000u) ? ~u : (u | 0x80000000u)) : 0;
+    uint32_t t = 0;
+#pragma unroll
+    for (int b = 31; b >= 16; --b) {
+      const uint32_t with = t | 1u << b;
+      t = __popcll(__ballot(om >= with)) >= k ? with : t;
+    }
+    return t ? key_value((uint64_t)t << 32) : -INFINITY;
+  }
+  // A tile's elements, mx their maximum in this lane.  Tiles come by rising
+  // column, so an element that only equals `least` comes after k others.
+  __device__ __forceinline__ void offer(const float (&x)[kTileElems], float mx, int base, int tid) {
+    if (!__any(mx > least)) return;
+    if (n >= 2 * k) {  // a better `least` (400 rows of fp32, 13 tiles a split: 46 us, 54 without)
+      rank();
+      if (!__any(mx > least)) return;
+    }
+    const float above = least;
+    if (n && add(x, base, tid, [&](float v) { return v > above; })) return;
+    if (n) rank();
+    const float low = fmaxf(reached(mx), least);
+    if (add(x, base, tid, [&](float v) { return v >= low && v > -INFINITY; })) {
+      least = low;
+      return;
+    }
+    // the best sit in few lanes, or many are equal: one by one into the sorted list
+    const int lane = tid & 63;
+    uint64_t key = lane < n ? cand[lane] : 0, kth = from_lane(key, k - 1);
+#pragma unroll
+    for (int j = 0; j < kTileElems; ++j) {
+      const uint64_t c = x[j] >= low && x[j] > -INFINITY ? argmax_key(x[j], (uint32_t)tile_col<T>(base, tid, j)) : 0;
+      uint64_t left = __ballot(c > kth);
+      while (left) {
+        const uint64_t y = from_lane(c, __builtin_ctzll(left));
+        left &= left - 1;
+        if (y <= kth) continue;
+        const int at = __popcll(__ballot(key > y));
+        const uint64_t up = from_lane_below(key);
+        key = lane < at ? key : (lane == at ? y : up);
+        kth = from_lane(key, k - 1);
+      }
+    }
+    keep(key);
+  }
+};
 
 struct Stat { float m, s, u; };
 // The statistics of two sets together.
@@ -228,8 +263,8 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int per) {
   const T* row = reinterpret_cast<const T*>(a.x) + (size_t)r * a.ld;
   const int v0 = split * per, v1 = min(a.V, v0 + per);
   Stat st = {-INFINITY, 0.f, 0.f};
-  TopList top;
-  top.init(a.k);
+  TopList<T> top;
+  if constexpr (TOP) top.init(a.k, s_cand[wave], s_top[wave]);
   float next[kTileElems];
   load_tile<T, TOP>(row, v0, tid, v1, next);
   for (int base = v0; base < v1; base += kTile) {
@@ -252,19 +287,14 @@ __global__ void __launch_bounds__(256) k_logprobs(LogprobArgs a, int per) {
       st.u = __builtin_fmaf(e, fmaxf(d, -1e4f), st.u);  // max: 0 * inf
     }
     if constexpr (TOP) {
-      if (base > v0 || !top_first<T>(top, x, mt, base, tid, s_cand[wave], s_top[wave])) {
-        if (__any(mt >= top.least)) {
-#pragma unroll
-          for (int j = 0; j < kTileElems; ++j) top.offer(x[j], tile_col<T>(base, tid, j));
-        }
-      }
+      top.offer(x, mt, base, tid);
     }
   }
 #pragma unroll
   for (int d = 1; d < 64; d *= 2)
     st = join(st, Stat{__shfl_xor(st.m, d), __shfl_xor(st.s, d), __shfl_xor(st.u, d)});
   if (lane == 0) s_st[wave] = st;
-  if (TOP && lane < kMaxTop) s_top[wave][lane] = lane < a.k ? top.key : 0;
+  if constexpr (TOP) top.rank();  // into s_top[wave]
   __syncthreads();
   st = join(join(s_st[0], s_st[1]), join(s_st[2], s_st[3]));
   uint64_t* best = s_cand[0];

@@ -136,6 +136,19 @@ def test_ties_and_orders(tj, order):
     check(tj, x, [1, V - 1], 7, torch.bfloat16, pad=3)
 
 
+@pytest.mark.parametrize("k", [1, 8, 32])
+def test_alternatives_over_many_steps(tj, k):
+    """Rows that are not split: their best come from any step, from many, or are equal across steps."""
+    rng = np.random.default_rng(k)
+    R, V = 1024, 12388
+    x = rng.integers(-8, 9, (R, V)) / 2.0  # many equal values
+    x[::4] = rng.standard_normal((R // 4, V)) + np.arange(V) / 4096.0
+    x[1::4] += 4.0 * (np.arange(V) // 4096 % 2)
+    x[2::4, 4096:] -= 32.0
+    x[3::8] = np.where(rng.random((R // 8, V)) < 0.001, x[3::8], -np.inf)
+    check(tj, x, rng.integers(-1, V, R), k, tj[0].float32)
+
+
 def test_outputs_are_optional(tj):
     torch, jf = tj
     x = torch.randn(5, 300, device="cuda")
