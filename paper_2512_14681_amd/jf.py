@@ -9,6 +9,7 @@ one ABI call that enqueues HIP kernels.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -23,6 +24,7 @@ JF_MAX_SEGMENTS = 16
 JF_MAX_ROWS = 512      # rows of one step at most
 JF_STEP_COMMIT = 2     # jf_jacobi_step mode bit: commit the accepted rows in the step
 JF_VIS_WORDS = 8       # u64 words of a row's in-step visibility mask
+JF_PAGE = 64           # cache slots of a page
 JF_FLAG_BAD_TOKEN, JF_FLAG_CAPACITY, JF_FLAG_SYNC, JF_FLAG_BAD_PAGE = 1, 2, 4, 8
 JF_MAX_TOP = 32        # alternatives of jf_token_logprobs at most
 JF_OPT_FUSED_ATTENTION = 1
@@ -315,18 +317,30 @@ def _vec(dev, t, dtype, n):
     return _at(dev, t)
 
 
-def _rows(t):
-    """(jf_dtype, row stride in elements) of a [rows][columns] tensor of fp32 or bf16 whose rows are contiguous."""
+def _buf(dev, t, n):
+    """Address of a contiguous tensor of n bytes or more."""
+    if t is None:
+        return None
+    if t.nbytes < n or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous tensor of {n} bytes, got {tuple(t.shape)} of {t.dtype}")
+    return _at(dev, t)
+
+
+def _rows(t, least=0, width=1):
+    """(jf_dtype, row stride in elements) of a [rows][columns] tensor of fp32 or bf16 whose rows are contiguous,
+    `least` of them or more with `width` columns or more."""
     code = _DTYPES.get(t.dtype)
     if code is None:
         code = _types().get(t.dtype)
     if code is None or t.dim() != 2:
         raise TypeError("rows are 2-dimensional fp32 or bf16 tensors")
-    ld, step = t.stride()
-    if step != 1 and t.size(1) > 1:
+    (n, w), (ld, step) = t.shape, t.stride()
+    if step != 1 and w > 1:
         raise TypeError("a row's elements lie side by side")
-    if ld < t.size(1) and t.size(0) <= 1:   # the stride of a single row says nothing
-        ld = t.size(1)
+    if n < least or w < width:
+        raise ValueError(f"expected {least} rows of {width} columns, got {n} of {w}")
+    if n <= 1 and ld < w:   # the stride of a single row says nothing
+        ld = w
     return code, ld
 
 
@@ -349,10 +363,11 @@ class Batch:
             raise ValueError(f"{n} sequences need {n + 1} row starts and {n} rows of the page table")
         if not ctx.get_device() == row_start.get_device() == page_table.get_device():
             raise ValueError("row_start, ctx and page_table are on one device")
-        self.device, self.n_rows = ctx.get_device(), int(n_rows)
+        self.device, self.n_rows, self.n_pages = ctx.get_device(), int(n_rows), int(n_pages)
         self.c = JfBatch(n, self.n_rows, int(max_rows), int(max_ctx), int(n_pages), int(page_table.shape[1]),
                          row_start.data_ptr(), ctx.data_ptr(), page_table.data_ptr())
         self.ref = ctypes.byref(self.c)
+        self.ws = {}    # {(n_heads, n_kv_heads, head_dim): bytes of attention_kv8's workspace}
 
     def on(self, dev):
         if self.device != dev:
@@ -364,51 +379,74 @@ def kv_page_bytes(n_kv_heads, head_dim, kv_dtype):
     return lib().jf_kv_page_bytes(int(n_kv_heads), int(head_dim), int(kv_dtype))
 
 
+def _pool_bytes(batch, n_kv_heads, head_dim, kv_dtype):
+    """batch.n_pages of kv_page_bytes (without the call, half a microsecond)."""
+    n = 2 * JF_PAGE * n_kv_heads * head_dim
+    if kv_dtype == JF_E4M3:
+        return batch.n_pages * ((n + 8 * n_kv_heads + 127) // 128 * 128)
+    return batch.n_pages * n * (4 if kv_dtype == JF_F32 else 2)
+
+
 def kv_append(batch, n_heads, n_kv_heads, head_dim, kv_dtype, d_kv, d_k, d_v, d_q=None, d_q_out=None,
               act_dtype=JF_BF16, d_pos=None, rope_base=0.0, d_flags=None, stream=None):
-    x, ld_k = _rows(d_k)
-    xv, ld_v = _rows(d_v)
-    xq, ld_q = _rows(d_q) if d_q is not None else (x, 0)
+    n, w = batch.n_rows, n_kv_heads * head_dim
+    x, ld_k = _rows(d_k, n, w)
+    xv, ld_v = _rows(d_v, n, w)
+    xq, ld_q = _rows(d_q, n, n_heads * head_dim) if d_q is not None else (x, 0)
     if not x == xv == xq:
         raise TypeError("queries, keys and values have one type")
     dev = _current_device()
     status = lib().jf_kv_append(batch.on(dev), n_heads, n_kv_heads, head_dim, kv_dtype, x, act_dtype, _at(dev, d_q),
-                                ld_q, _at(dev, d_k), ld_k, _at(dev, d_v), ld_v, _vec(dev, d_pos, _I32, batch.n_rows),
-                                rope_base, _at(dev, d_kv), _at(dev, d_q_out), _vec(dev, d_flags, _I32, 1), _on(stream))
+                                ld_q, _at(dev, d_k), ld_k, _at(dev, d_v), ld_v, _vec(dev, d_pos, _I32, n), rope_base,
+                                _buf(dev, d_kv, _pool_bytes(batch, n_kv_heads, head_dim, kv_dtype)),
+                                _buf(dev, d_q_out, 4 * n * n_heads * head_dim),  # fp32, or two bf16 planes
+                                _vec(dev, d_flags, _I32, 1), _on(stream))
     if status:
         check(status)
 
 
 def kv_read(batch, n_kv_heads, head_dim, kv_dtype, d_kv, d_k, d_v, d_flags=None, stream=None):
-    x, ld_k = _rows(d_k)
-    xv, ld_v = _rows(d_v)
+    n, w = batch.n_rows, n_kv_heads * head_dim
+    x, ld_k = _rows(d_k, n, w)
+    xv, ld_v = _rows(d_v, n, w)
     if x != xv:
         raise TypeError("keys and values have one type")
     dev = _current_device()
-    status = lib().jf_kv_read(batch.on(dev), n_kv_heads, head_dim, kv_dtype, x, _at(dev, d_kv), _at(dev, d_k), ld_k,
+    status = lib().jf_kv_read(batch.on(dev), n_kv_heads, head_dim, kv_dtype, x,
+                              _buf(dev, d_kv, _pool_bytes(batch, n_kv_heads, head_dim, kv_dtype)), _at(dev, d_k), ld_k,
                               _at(dev, d_v), ld_v, _vec(dev, d_flags, _I32, 1), _on(stream))
     if status:
         check(status)
 
 
+def _kv8_ws_bytes(batch, shape):
+    n = batch.ws.get(shape)
+    if n is None:
+        n = batch.ws[shape] = lib().jf_attention_kv8_ws_bytes(batch.ref, *shape)
+    return n
+
+
 def attention_kv8_ws_bytes(batch, n_heads, n_kv_heads, head_dim):
-    n = lib().jf_attention_kv8_ws_bytes(batch.ref, n_heads, n_kv_heads, head_dim)
+    n = _kv8_ws_bytes(batch, (n_heads, n_kv_heads, head_dim))
     if n == 0:
-        raise JfError(JF_E_SHAPE, lib().jf_last_error().decode())
+        raise JfError(JF_E_SHAPE, "no batch or heads that jf_attention_kv8 takes")
     return n
 
 
 def attention_kv8(batch, n_heads, n_kv_heads, head_dim, act_dtype, d_q, d_kv, d_out, d_ws, d_vis=None, d_flags=None,
                   stream=None):
-    _types()
-    dev = _current_device()
-    status = lib().jf_attention_kv8(batch.on(dev), n_heads, n_kv_heads, head_dim, act_dtype, _at(dev, d_q),
-                                    _at(dev, d_kv), _at(dev, d_vis), _at(dev, d_out), _at(dev, d_ws),
+    dev, n = _current_device(), batch.n_rows
+    rows = 4 * n * n_heads * head_dim   # bytes: fp32, or two bf16 planes
+    status = lib().jf_attention_kv8(batch.on(dev), n_heads, n_kv_heads, head_dim, act_dtype, _buf(dev, d_q, rows),
+                                    _buf(dev, d_kv, _pool_bytes(batch, n_kv_heads, head_dim, JF_E4M3)),
+                                    _buf(dev, d_vis, n * 8 * JF_VIS_WORDS), _buf(dev, d_out, rows),
+                                    _buf(dev, d_ws, _kv8_ws_bytes(batch, (n_heads, n_kv_heads, head_dim))),
                                     _vec(dev, d_flags, _I32, 1), _on(stream))
     if status:
         check(status)
 
 
+@functools.lru_cache(4096)
 def token_logprobs_ws_bytes(R, V, k=0):
     return lib().jf_token_logprobs_ws_bytes(int(R), int(V), int(k))
 
@@ -421,7 +459,8 @@ def token_logprobs(d_logits, d_ws, d_tokens=None, k=0, d_logprob=None, d_entropy
     status = lib().jf_token_logprobs(R, V, x, _at(dev, d_logits), ld, _vec(dev, d_tokens, _I32, R), k,
                                      _vec(dev, d_logprob, _F32, R), _vec(dev, d_entropy, _F32, R),
                                      _vec(dev, d_norm, _F32, 2 * R), _vec(dev, d_top_ids, _I32, R * k),
-                                     _vec(dev, d_top_logprob, _F32, R * k), _at(dev, d_ws), _on(stream))
+                                     _vec(dev, d_top_logprob, _F32, R * k),
+                                     _buf(dev, d_ws, token_logprobs_ws_bytes(R, V, k)), _on(stream))
     if status:
         check(status)
 

@@ -196,3 +196,34 @@ def test_binding_refuses_tensors_elsewhere(monkeypatch):
     b = jf.Batch(torch.zeros(3, **i32), torch.zeros(2, **i32), torch.zeros(2, 1, **i32), 4, 2, 64, 1)
     with pytest.raises(ValueError, match="batch is on"):
         jf.kv_read(b, 1, 32, jf.JF_BF16, x, torch.zeros(4, 32), torch.zeros(4, 32))
+
+
+def test_binding_refuses_short_tensors(monkeypatch):
+    """Fewer rows than the batch has, narrow rows, small pools and strided outputs never reach the library."""
+    import torch
+    jf._types()
+    monkeypatch.setattr(jf, "_current_device", lambda: -1)   # what host tensors answer
+    i32 = dict(dtype=torch.int32)
+    G, hd, n = 2, 32, 4
+    for kv, dtype in ((jf.JF_F32, torch.float32), (jf.JF_BF16, torch.bfloat16), (jf.JF_E4M3, torch.uint8)):
+        b = jf.Batch(torch.zeros(3, **i32), torch.zeros(2, **i32), torch.zeros(2, 1, **i32), n, 2, 64, 3)
+        assert jf._pool_bytes(b, G, hd, kv) == 3 * jf.kv_page_bytes(G, hd, kv)
+        pool = torch.zeros(jf._pool_bytes(b, G, hd, kv) // torch.zeros(1, dtype=dtype).element_size(), dtype=dtype)
+        rows, q = torch.zeros(n, G * hd), torch.zeros(n, 4 * hd)
+        out = torch.zeros(n, 4, hd)
+        ok = dict(d_kv=pool, d_k=rows, d_v=rows, d_q=q, d_q_out=out)
+        for bad in (dict(d_k=rows[1:]), dict(d_v=rows[:, 1:]), dict(d_q=q[:3]), dict(d_q=q[:, :96]),
+                    dict(d_kv=pool[:-1]), dict(d_q_out=out[1:]), dict(d_q_out=out.transpose(0, 1))):
+            with pytest.raises(ValueError, match="expected"):
+                jf.kv_append(b, 4, G, hd, kv, act_dtype=jf.JF_F32, **{**ok, **bad})
+        for bad in (dict(d_k=rows[1:]), dict(d_v=rows[:, 1:]), dict(d_kv=pool[:-1])):
+            with pytest.raises(ValueError, match="expected"):
+                jf.kv_read(b, G, hd, kv, **{**{k: ok[k] for k in ("d_kv", "d_k", "d_v")}, **bad})
+    ok = dict(d_q=out, d_kv=pool, d_out=out, d_ws=None, d_vis=torch.zeros(n, jf.JF_VIS_WORDS, dtype=torch.int64))
+    for bad in (dict(d_q=out[1:]), dict(d_kv=pool[:-1]), dict(d_out=out[1:]), dict(d_vis=ok["d_vis"][1:]),
+                dict(d_q=out.transpose(0, 1)), dict(d_ws=torch.zeros(jf.attention_kv8_ws_bytes(b, 4, G, hd) // 4 - 1))):
+        with pytest.raises(ValueError, match="expected"):
+            jf.attention_kv8(b, 4, G, hd, jf.JF_F32, **{**ok, **bad})
+    x = torch.zeros(3, 5000)
+    with pytest.raises(ValueError, match="expected"):
+        jf.token_logprobs(x, torch.zeros(jf.token_logprobs_ws_bytes(3, 5000, 4) - 1, dtype=torch.uint8), k=4)
