@@ -109,16 +109,16 @@ __device__ __forceinline__ int key_rank(const uint64_t* keys, int n, uint64_t ke
 // above a value that k earlier ones reach, and ranks them by counting when
 // they are too many and at the end, so that most tiles cost a comparison an
 // element (kept sorted over the lanes instead, key by key, 64 rows of 152064
-// bf16 logits took 15.2 us for k = 8 and 20.7 for k = 20, now 13.2 and 17.4).
+// bf16 logits took 15.2 us for k = 8 and 20.7 for k = 20, now 12.6 and 16.3).
 constexpr int kCand = 128;
 template <typename T> struct TopList {
-  uint64_t* cand;  // kCand of this wave
+  uint64_t* cand;  // kCand of this wave: `sorted` keys, then pairs of value and column
   uint64_t* best;  // kMaxTop of this wave: scratch
-  int k, n;
+  int k, n, sorted;
   float least;     // k candidates reach it (-inf: not known of k)
   __device__ __forceinline__ void init(int k_, uint64_t* cand_, uint64_t* best_) {
     k = k_; cand = cand_; best = best_;
-    n = 0;
+    n = sorted = 0;
     least = -INFINITY;
   }
   static __device__ __forceinline__ void fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
@@ -126,15 +126,21 @@ template <typename T> struct TopList {
   // This lane's of the k best candidates in order (0: none), which alone stay.
   __device__ __forceinline__ uint64_t rank() {
     const int lane = threadIdx.x & 63;
-    if (lane < 8 && n + lane < kCand) cand[n + lane] = 0;
     if (lane < kMaxTop) best[lane] = 0;
+    uint64_t mine[kCand / 64];
+#pragma unroll
+    for (int h = 0; h < kCand / 64; ++h) {
+      const int i = 64 * h + lane;
+      const uint64_t c = cand[i];
+      mine[h] = i >= n ? 0 : (i < sorted ? c : argmax_key(__uint_as_float((uint32_t)(c >> 32)), (uint32_t)c));
+      cand[i] = mine[h];
+    }
     fence();
 #pragma unroll
-    for (int h = 0; h < kCand; h += 64)
-      if (h + lane < n) {
-        const uint64_t key = cand[h + lane];
-        const int at = key_rank(cand, n, key);
-        if (at < k) best[at] = key;
+    for (int h = 0; h < kCand / 64; ++h)
+      if (mine[h]) {
+        const int at = key_rank(cand, n, mine[h]);
+        if (at < k) best[at] = mine[h];
       }
     fence();
     const uint64_t key = lane < k ? best[lane] : 0;
@@ -144,13 +150,13 @@ template <typename T> struct TopList {
   // The candidates become these: the k best in order, one a lane.
   __device__ __forceinline__ void keep(uint64_t key) {
     const int lane = threadIdx.x & 63;
-    n = __popcll(__ballot(lane < k && key));
+    n = sorted = __popcll(__ballot(lane < k && key));
     if (lane < k) cand[lane] = key;
     const uint64_t kth = from_lane(key, k - 1);
     if (kth) least = key_value(kth);
     fence();
   }
-  // Adds the elements for which in(value); false (and nothing added) if they do not fit.
+  // Adds the elements for which in(value), as they are; false (and nothing added) if they do not fit.
   template <typename F>
   __device__ __forceinline__ bool add(const float (&x)[kTileElems], int base, int tid, F in) {
     int to = n;
@@ -160,7 +166,8 @@ template <typename T> struct TopList {
       const uint64_t mask = __ballot(it);
       if (mask) {
         const int at = to + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
-        if (it && at < kCand) cand[at] = argmax_key(x[j], (uint32_t)tile_col<T>(base, tid, j));
+        if (it && at < kCand)
+          cand[at] = (uint64_t)__float_as_uint(x[j]) << 32 | (uint32_t)tile_col<T>(base, tid, j);
         to += __popcll(mask);
       }
     }
@@ -189,12 +196,12 @@ template <typename T> struct TopList {
       rank();
       if (!__any(mx > least)) return;
     }
-    const float above = least;
+    const float above = least;  // -inf admits the finite ones
     if (n && add(x, base, tid, [&](float v) { return v > above; })) return;
     if (n) rank();
-    const float low = fmaxf(reached(mx), least);
-    if (add(x, base, tid, [&](float v) { return v >= low && v > -INFINITY; })) {
-      least = low;
+    const float reach = fmaxf(reached(mx), least), low = fmaxf(reach, -3.402823466e38f);  // only finite ones
+    if (add(x, base, tid, [&](float v) { return v >= low; })) {
+      least = reach;
       return;
     }
     // the best sit in few lanes, or many are equal: one by one into the sorted list
@@ -202,7 +209,7 @@ template <typename T> struct TopList {
     uint64_t key = lane < n ? cand[lane] : 0, kth = from_lane(key, k - 1);
 #pragma unroll
     for (int j = 0; j < kTileElems; ++j) {
-      const uint64_t c = x[j] >= low && x[j] > -INFINITY ? argmax_key(x[j], (uint32_t)tile_col<T>(base, tid, j)) : 0;
+      const uint64_t c = x[j] >= low ? argmax_key(x[j], (uint32_t)tile_col<T>(base, tid, j)) : 0;
       uint64_t left = __ballot(c > kth);
       while (left) {
         const uint64_t y = from_lane(c, __builtin_ctzll(left));
