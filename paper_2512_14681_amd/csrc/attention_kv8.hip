@@ -520,16 +520,16 @@ __global__ void __launch_bounds__(256, 2) k_attention_kv8_few(Kv8Args a) {
     }
 }
 
-// More tiles: QT of its own for each wave.  Workgroup: KV head, 4 QT tiles,
-// key split.  A page's codes go from memory to one of two LDS buffers without
+// More tiles: QT of its own for each of W waves.  Workgroup: KV head, W QT
+// tiles, key split.  A page's codes go from memory to one of two LDS buffers without
 // passing registers, while the page before is worked on; the waves read them
 // as operands and turn them to fp16 (as fp16 in LDS the writes alone, 32 KB a
 // page at the 31 bytes a cycle that they reach, took a quarter of the time).
-template <typename A, int HD, int QT>
-__global__ void __launch_bounds__(256, 2) k_attention_kv8_many(Kv8Args a) {
+template <typename A, int HD, int QT, int W>
+__global__ void __launch_bounds__(64 * W, 2) k_attention_kv8_many(Kv8Args a) {
   using T = Tiles<A, HD, QT>;
   constexpr int NP = T::NP;
-  constexpr int kItems = 2 * NP / kWaves;      // 1 KB pieces of a page that each wave brings
+  constexpr int kItems = 2 * NP / W;      // 1 KB pieces of a page that each wave brings
   __shared__ u32x4_t s_kv[2][2 * NP][64];      // pieces: keys, then values
   const int grp = a.H / a.G;
   // Workgroups go around the 8 XCDs in order: each gets a run of consecutive
@@ -542,15 +542,15 @@ __global__ void __launch_bounds__(256, 2) k_attention_kv8_many(Kv8Args a) {
   if (!batch_seq(a.b, s, q)) return;
   const int nq = grp * q.n;
   const int lane = threadIdx.x & 63, wave = same((int)threadIdx.x >> 6), kg = lane >> 4;
-  if (group * kWaves * QT * 16 >= nq) return;
+  if (group * W * QT * 16 >= nq) return;
   const int pages = (q.C + q.n + kPage - 1) / kPage;
   const int p0 = split * a.chunk;
   int p1 = min(p0 + a.chunk, pages);
   if (p0 >= pages) return;
-  const int tile0 = (group * kWaves + wave) * QT;
+  const int tile0 = (group * W + wave) * QT;
   int mine = tile0 * 16 < nq ? p1 : p0;        // the wave's tiles need pages [p0, mine)
   if (!a.vis) {                                // causal: no slot past the last row
-    const int last_wave = min((tile0 + QT) * 16, nq) - 1, last = min((group + 1) * kWaves * QT * 16, nq) - 1;
+    const int last_wave = min((tile0 + QT) * 16, nq) - 1, last = min((group + 1) * W * QT * 16, nq) - 1;
     mine = min(mine, (q.C + last_wave / grp) / kPage + 1);
     p1 = min(p1, (q.C + last / grp) / kPage + 1);
   }
@@ -567,9 +567,9 @@ __global__ void __launch_bounds__(256, 2) k_attention_kv8_many(Kv8Args a) {
     const uint8_t* page = a.kv + (size_t)max(id, 0) * a.page_bytes;
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-      const int piece = i * kWaves + wave;
+      const int piece = i * W + wave;
       dma_1k<false>(reinterpret_cast<const char*>(page) + ((piece < NP ? g : a.G + g) * kPage * HD + piece % NP * 1024),
-                    lane * 16, ring + (buf * 2 * NP + i * kWaves) * 1024);
+                    lane * 16, ring + (buf * 2 * NP + i * W) * 1024);
     }
     sc = reinterpret_cast<const float2*>(page + (size_t)2 * a.G * kPage * HD)[g];
   };
@@ -707,20 +707,25 @@ __global__ void __launch_bounds__(256) k_attention_kv8_merge(Kv8Args a, int bloc
 // row after 1024 keys 9.7 us, split five ways 6.0 and 3.2 for the merge);
 // beyond, 512 workgroups of 4 to 24 pages (64 ragged sequences of up to 8192:
 // 24 pages 57.6 us, 64 pages 61.7).  More tiles: as many splits as fill the
-// chip's 512 places, of 8 pages or more (192 rows after 2048 keys: 8 pages
+// chip's 2048 places for waves, of 8 pages or more (192 rows after 2048 keys: 8 pages
 // 29.2 and 6.4 us for the merge, 4 pages 30.5 and 13), or of 4 where these
 // leave most of the chip free (16 rows after 1024 keys: 17.2 against 23.9 us).
+// Two tiles have workgroups of two waves, twice as many, as two more would
+// only load (64 sequences of 4 rows after up to 4000 keys: 41.8 against 57.6
+// us; three and four tiles as two waves of two 64.7 and 67.0, as four of one
+// 62.1 and 63.9).
 void kv8_plan(Kv8Args& a) {
   const int tiles = (int)(((int64_t)a.H / a.G * a.b.max_rows + 15) / 16);
   a.qt = tiles == 1 ? 0 : tiles <= kWaves ? 1 : 2;
-  a.groups = a.qt == 0 ? 1 : (tiles + kWaves * a.qt - 1) / (kWaves * a.qt);
+  a.waves = tiles == 2 ? 2 : kWaves;
+  a.groups = a.qt == 0 ? 1 : (tiles + a.waves * a.qt - 1) / (a.waves * a.qt);
   const int pages = (a.b.max_ctx + kPage - 1) / kPage;
   const int64_t base = (int64_t)a.b.n_seqs * a.G * a.groups;
   if (a.qt == 0) {
     const int64_t c = (base * pages / 512 + 2) / 4 * 4;
     a.chunk = pages <= 20 ? pages : (int)std::min<int64_t>(std::max<int64_t>(c, 4), 24);
   } else {
-    const int64_t want = std::max<int64_t>(512 / base, 1);
+    const int64_t want = std::max<int64_t>(512 * kWaves / a.waves / base, 1);
     a.chunk = std::max<int>((int)((pages + want - 1) / want), base * pages <= 1024 ? 4 : 8);
   }
   a.chunk = std::max(a.chunk, (pages + kMaxSplits - 1) / kMaxSplits);
@@ -732,8 +737,9 @@ static void attention_qt(const Kv8Args& a, hipStream_t st) {
   const dim3 few((unsigned)(a.b.n_seqs * a.G), (unsigned)a.splits);
   const unsigned many = (unsigned)((a.b.n_seqs * a.G * a.groups * a.splits + kXcds - 1) / kXcds * kXcds);
   if (a.qt == 0) k_attention_kv8_few<A, HD><<<few, 256, 0, st>>>(a);
-  else if (a.qt == 1) k_attention_kv8_many<A, HD, 1><<<many, 256, 0, st>>>(a);
-  else k_attention_kv8_many<A, HD, 2><<<many, 256, 0, st>>>(a);
+  else if (a.waves == 2) k_attention_kv8_many<A, HD, 1, 2><<<many, 128, 0, st>>>(a);
+  else if (a.qt == 1) k_attention_kv8_many<A, HD, 1, 4><<<many, 256, 0, st>>>(a);
+  else k_attention_kv8_many<A, HD, 2, 4><<<many, 256, 0, st>>>(a);
 }
 template <typename A> static hipError_t attention_act(const Kv8Args& a, hipStream_t st) {
   if (a.hd == 32) attention_qt<A, 32>(a, st);

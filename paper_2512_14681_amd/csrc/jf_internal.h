@@ -326,6 +326,7 @@ struct Kv8Args {
   float* ml_part;            // [splits][n_rows * H][2]
   // the plan (kv8_plan)
   int qt;                    // query tiles of a wave (0: one tile, whose keys the waves share)
+  int waves;                 // waves of a workgroup
   int groups;                // workgroups along the query tiles
   int chunk;                 // pages of a key split
   int splits;

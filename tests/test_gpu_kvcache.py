@@ -382,6 +382,14 @@ def test_attention_many_rows_and_long_prefixes(tj, hd, G, grp, act, ctx, rows, k
     attention_case(tj, hd, G, grp, act, ctx, rows, kind, seed=hd + rows[0])
 
 
+@pytest.mark.parametrize("hd,G,grp,act", [(128, 4, 7, "bf16"), (64, 2, 8, "f32"), (32, 1, 8, "bf16")])
+@pytest.mark.parametrize("ctx,rows,kind", [([0], [4], "causal"), ([900, 0, 63, 130], [4, 1, 0, 3], "tree"),
+                                           ([5000, 64], [3, 4], "any"), ([60, 61, 62], [4, 4, 4], "causal")])
+def test_attention_of_short_drafts(tj, hd, G, grp, act, ctx, rows, kind):
+    """17 to 32 queries of a KV head, some sequences with fewer."""
+    attention_case(tj, hd, G, grp, act, ctx, rows, kind, seed=grp + len(ctx))
+
+
 @pytest.mark.parametrize("qstd", [0.0, 1e-30, 8.0, 1e4])
 def test_attention_scores_of_any_size(tj, qstd):
     """From queries of zero (the mean of the values) to scores of which one takes all."""
