@@ -707,13 +707,14 @@ __global__ void __launch_bounds__(256) k_attention_kv8_merge(Kv8Args a, int bloc
 // row after 1024 keys 9.7 us, split five ways 6.0 and 3.2 for the merge);
 // beyond, 512 workgroups of 4 to 24 pages (64 ragged sequences of up to 8192:
 // 24 pages 57.6 us, 64 pages 61.7).  More tiles: as many splits as fill the
-// chip's 2048 places for waves, of 8 pages or more (192 rows after 2048 keys: 8 pages
+// chip's places (two workgroups of four waves a compute unit with two tiles a
+// wave; three with one, whose registers allow it: 64 sequences of 6 rows after
+// up to 4000 keys 54.1 us, 62.9 with two), of 8 pages or more (192 rows after 2048 keys: 8 pages
 // 29.2 and 6.4 us for the merge, 4 pages 30.5 and 13), or of 4 where these
 // leave most of the chip free (16 rows after 1024 keys: 17.2 against 23.9 us).
-// Two tiles have workgroups of two waves, twice as many, as two more would
-// only load (64 sequences of 4 rows after up to 4000 keys: 41.8 against 57.6
-// us; three and four tiles as two waves of two 64.7 and 67.0, as four of one
-// 62.1 and 63.9).
+// Two tiles have workgroups of two waves, four a compute unit, as two more
+// waves would only load (the same with 4 rows: 41.8 against 57.6 us; three and
+// four tiles as two waves of two 64.7 and 67.0, as four of one 62.1 and 63.9).
 void kv8_plan(Kv8Args& a) {
   const int tiles = (int)(((int64_t)a.H / a.G * a.b.max_rows + 15) / 16);
   a.qt = tiles == 1 ? 0 : tiles <= kWaves ? 1 : 2;
@@ -725,7 +726,8 @@ void kv8_plan(Kv8Args& a) {
     const int64_t c = (base * pages / 512 + 2) / 4 * 4;
     a.chunk = pages <= 20 ? pages : (int)std::min<int64_t>(std::max<int64_t>(c, 4), 24);
   } else {
-    const int64_t want = std::max<int64_t>(512 * kWaves / a.waves / base, 1);
+    const int places = a.waves == 2 ? 1024 : a.qt == 1 ? 768 : 512;
+    const int64_t want = std::max<int64_t>(places / base, 1);
     a.chunk = std::max<int>((int)((pages + want - 1) / want), base * pages <= 1024 ? 4 : 8);
   }
   a.chunk = std::max(a.chunk, (pages + kMaxSplits - 1) / kMaxSplits);
