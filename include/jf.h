@@ -401,7 +401,7 @@ jf_status jf_trajectory_select(const int32_t *d_traj, const int32_t *d_len,
  * JF_FLAG_CAPACITY is raised; a page table entry outside [0, n_pages) raises
  * JF_FLAG_BAD_PAGE and its tokens are skipped.  d_flags (optional, one int32)
  * gets these bits ORed in; the caller clears it.  n_seqs, n_rows or max_rows
- * = 0 does nothing.  n_seqs times the workgroups that max_rows and max_ctx
+ * = 0 does nothing; n_pages = 0 otherwise is JF_E_CAPACITY.  n_seqs times the workgroups that max_rows and max_ctx
  * call for must stay within 2^22 (JF_E_CAPACITY). */
 typedef struct {
   int32_t n_seqs, n_rows, max_rows, max_ctx, n_pages, table_stride;

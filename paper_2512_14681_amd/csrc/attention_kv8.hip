@@ -415,9 +415,10 @@ template <bool ONCE> __device__ __forceinline__ u32x4_t load16(const uint8_t* p)
 }
 
 // One query tile (few rows: bound by the cache's bytes).  Workgroup: KV head,
-// tile, key split; the waves take every fourth page straight into registers,
-// the next page's keys in flight from when this one's scores are done, and
-// merge in LDS.
+// key split; the waves take every fourth page straight into registers, as
+// nobody shares it, the next page's keys in flight from when this one's scores
+// are done, and merge in LDS.  64 sequences of up to 8192 tokens, 28 query and
+// 4 KV heads of 128 dims: 57.4 us, 5.7 TB/s.
 template <typename A, int HD>
 __global__ void __launch_bounds__(256, 2) k_attention_kv8_few(Kv8Args a) {
   using T = Tiles<A, HD, 1>;
@@ -525,6 +526,11 @@ __global__ void __launch_bounds__(256, 2) k_attention_kv8_few(Kv8Args a) {
 // passing registers, while the page before is worked on; the waves read them
 // as operands and turn them to fp16 (as fp16 in LDS the writes alone, 32 KB a
 // page at the 31 bytes a cycle that they reach, took a quarter of the time).
+// 512 rows after up to 8000 keys, heads as above: 135 us, 122 GFLOP issued at
+// 0.90 PFLOP/s.  Bound by issue: a wave's 128 matrix instructions a page take
+// 2050 cycles, its 350 vector instructions 1800, and the two waves of a SIMD
+// overlap these only in part.  (Half pages in a pipeline, one half's
+// exponentials beside the other's matrix work, ran out of registers: 143 us.)
 template <typename A, int HD, int QT, int W>
 __global__ void __launch_bounds__(64 * W, 2) k_attention_kv8_many(Kv8Args a) {
   using T = Tiles<A, HD, QT>;
@@ -706,15 +712,17 @@ __global__ void __launch_bounds__(256) k_attention_kv8_merge(Kv8Args a, int bloc
 // One tile: up to 20 pages in one workgroup a head, which saves the merge (1
 // row after 1024 keys 9.7 us, split five ways 6.0 and 3.2 for the merge);
 // beyond, 512 workgroups of 4 to 24 pages (64 ragged sequences of up to 8192:
-// 24 pages 57.6 us, 64 pages 61.7).  More tiles: as many splits as fill the
-// chip's places (two workgroups of four waves a compute unit with two tiles a
-// wave; three with one, whose registers allow it: 64 sequences of 6 rows after
-// up to 4000 keys 54.1 us, 62.9 with two), of 8 pages or more (192 rows after 2048 keys: 8 pages
-// 29.2 and 6.4 us for the merge, 4 pages 30.5 and 13), or of 4 where these
-// leave most of the chip free (16 rows after 1024 keys: 17.2 against 23.9 us).
-// Two tiles have workgroups of two waves, four a compute unit, as two more
-// waves would only load (the same with 4 rows: 41.8 against 57.6 us; three and
-// four tiles as two waves of two 64.7 and 67.0, as four of one 62.1 and 63.9).
+// 24 pages 57.6 us, 64 pages 61.7).
+// More tiles: as many splits as fill the chip's places, of 8 pages or more
+// (192 rows after 2048 keys: 8 pages 29.2 us and 6.4 for the merge, 4 pages
+// 30.5 and 13), or of 4 where these leave most of the chip free (16 rows after
+// 1024 keys: 17.2 against 23.9 us).  A compute unit has places for two
+// workgroups of four waves with two tiles a wave, and for three with one tile,
+// whose registers allow it (64 sequences of 6 rows after up to 4000 keys 54.1
+// us, 62.9 with two).  Two tiles have workgroups of two waves, four a compute
+// unit, as two more waves would only load (the same with 4 rows 41.8 us, 57.6
+// with four waves); three and four tiles as two waves of two tiles would take
+// 64.7 and 67.0 us, as four of one 62.1 and 63.9.
 void kv8_plan(Kv8Args& a) {
   const int tiles = (int)(((int64_t)a.H / a.G * a.b.max_rows + 15) / 16);
   a.qt = tiles == 1 ? 0 : tiles <= kWaves ? 1 : 2;
