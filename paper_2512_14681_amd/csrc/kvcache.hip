@@ -12,7 +12,7 @@
 //
 // Both are bound by memory for many rows and by three dependent loads (the
 // sequence, its page table entry, the page) for few.  Append: 14458 rows of 16
-// + 2 x 4 heads of 128 dims in fp32 to an e4m3 cache 61.6 us, 310 MB at 5.0
+// + 2 x 4 heads of 128 dims in fp32 to an e4m3 cache 63 us, 310 MB at 4.9
 // TB/s; one row 4.8 us, 64 sequences of one row 9.7 us.  Read: the 14458 rows
 // to bf16 14.5 us, 44 MB at 3.1 TB/s; the last pages of 64 sequences 6.8 us.
 #include <algorithm>
