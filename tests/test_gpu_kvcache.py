@@ -477,6 +477,29 @@ def test_pages_beyond_32_bit_offsets(tj):
     assert float(outs[0][0].abs().sum()) > 0
 
 
+@pytest.mark.parametrize("hd", [32, 64, 128])
+def test_read_into_rows_on_8_byte_boundaries(tj, hd):
+    """bf16 rows whose starts are multiples of 8 bytes, not of 16, and of 4: the values are those of plain rows."""
+    torch, jf = tj
+    G, C, n = 3, 50, 90
+    S = Seqs(tj, [C], [n])
+    pool = torch.zeros(S.n_pages, jf.kv_page_bytes(G, hd, jf.JF_E4M3), dtype=torch.uint8, device="cuda")
+    first = jf.Batch(torch.tensor([0, C + n], dtype=torch.int32).cuda(), torch.zeros(1, dtype=torch.int32).cuda(), S.d_table,
+                     C + n, C + n, 64 * S.d_table.shape[1], S.n_pages)
+    x = torch.randn(C + n, 2, G * hd, device="cuda")
+    jf.kv_append(first, G, G, hd, jf.JF_E4M3, pool, x[:, 0], x[:, 1])
+    want = [torch.empty(n, G * hd, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    jf.kv_read(S.batch, G, hd, jf.JF_E4M3, pool, *want)
+    assert bool((want[0] != 0).any()) and bool((want[1] != 0).any())
+    for pad, at in ((4, 4), (4, 0), (1, 2)):
+        flat = torch.full((2, n * (G * hd + pad) + at), 9.0, dtype=torch.bfloat16, device="cuda")
+        rows = [f[at:].view(n, G * hd + pad) for f in flat]
+        jf.kv_read(S.batch, G, hd, jf.JF_E4M3, pool, rows[0][:, :G * hd], rows[1][:, :G * hd])
+        for r, w in zip(rows, want):
+            assert bool((r[:, :G * hd] == w).all()) and bool((r[:, G * hd:] == 9).all())
+        assert bool((flat[:, :at] == 9).all())
+
+
 def test_shared_prefix_pages(tj):
     """Two sequences whose first pages are the same: each sees them, and appends to its own last page."""
     torch, jf = tj
@@ -579,3 +602,42 @@ def test_captured_calls_follow_the_devices_lengths(tj):
             torch.cuda.synchronize()
             assert bool((out == eo).all()) and bool((out2 == eo).all()) and bool((pool == epool).all()), i
     assert float(out.abs().sum()) > 0
+
+
+def test_calls_on_two_streams_at_once(tj):
+    """Streams that are named, not current, each with its own workspace: what the calls give alone."""
+    torch, jf = tj
+    G, grp, hd, C = 2, 4, 64, 1500
+    H = G * grp
+    sets = []
+    for seed, rows in ((1, 1), (2, 70)):
+        S = Seqs(tj, [C, 300], [rows, rows], seed=seed)
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+        pool = torch.randint(0, 100, (S.n_pages, jf.kv_page_bytes(G, hd, jf.JF_E4M3)), dtype=torch.uint8, device="cuda",
+                             generator=g)
+        n = 2 * G * 64 * hd
+        pool[:, n:n + 8 * G] = torch.ones(2 * G).view(torch.uint8).cuda()
+        x = torch.randn(S.R, (H + 2 * G) * hd, device="cuda", generator=g)
+        q = torch.empty(1, S.R, H, hd, device="cuda")
+        out = torch.zeros(1, (S.R + 15) // 16 * 16 * H * hd, device="cuda")
+        ws = torch.empty(jf.attention_kv8_ws_bytes(S.batch, H, G, hd), dtype=torch.uint8, device="cuda")
+        sets.append((S, pool, x, q, out, ws))
+
+    def one(S, pool, x, q, out, ws, stream):
+        jf.kv_append(S.batch, H, G, hd, jf.JF_E4M3, pool, x[:, H * hd:(H + G) * hd], x[:, (H + G) * hd:],
+                     d_q=x[:, :H * hd], d_q_out=q, act_dtype=jf.JF_F32, rope_base=1e4, stream=stream)
+        jf.attention_kv8(S.batch, H, G, hd, jf.JF_F32, q, pool, out, ws, stream=stream)
+    alone = []
+    for a in sets:
+        one(*a, None)
+        alone.append((a[4].clone(), a[1].clone()))
+        a[4].zero_()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(20):                     # the rows once more into the same slots: the same pages
+        for a, st in zip(sets, streams):
+            one(*a, st)
+    torch.cuda.synchronize()
+    for a, (o, pool) in zip(sets, alone):
+        assert bool((a[4] == o).all()) and bool((a[1] == pool).all()) and float(o.abs().sum()) > 0

@@ -231,6 +231,26 @@ def test_gradient_of_special_rows(tj):
     assert (o[3, ::2] == 0).all() and abs(o[3, 1] - (1 - 1 / 50)) < 2.0 ** -20 and abs(o[3, 3] + 1 / 50) < 2.0 ** -20
 
 
+def test_rows_beyond_32_bit_offsets(tj):
+    """Rows 2^31 + 8 elements apart, the gradient in place: what rows side by side give."""
+    torch, jf = tj
+    R, V, k, ld = 3, 5003, 5, (1 << 31) + 8
+    x = torch.randn(R, V, device="cuda").to(torch.bfloat16)
+    flat = torch.zeros((R - 1) * ld + V + 64, dtype=torch.bfloat16, device="cuda")
+    far = flat.as_strided((R, V), (ld, 1))
+    far.copy_(x)
+    tok = torch.tensor([1, 5002, -1], dtype=torch.int32, device="cuda")
+    g = torch.tensor([1.0, -2.0, 0.5], device="cuda")
+    outs = []
+    for t in (x, far):
+        lp, ent, norm, ids, top, _ = run(tj, t, tok.cpu().numpy(), k)
+        jf.token_logprobs_grad(t, norm, t, d_tokens=tok, d_entropy=ent, d_g_logprob=g, d_g_entropy=g)
+        outs.append((lp, ent, norm, ids, top, t))
+    for a, b in zip(*outs):
+        assert bool((a == b).all())
+    assert float(x.float().abs().sum()) > 0 and bool((flat[V:ld] == 0).all()) and bool((flat[-64:] == 0).all())
+
+
 def test_captured(tj):
     """Both calls captured on a stream of their own, replayed with new logits between eager work."""
     torch, jf = tj
