@@ -125,20 +125,20 @@ __device__ __forceinline__ float query_max(float v) {
 constexpr float kWeightBits = 10.f, kMostWeight = 32768.f;
 constexpr int kWaves = 4, kXcds = 8;
 
-// QT tiles of 16 queries of one KV head in a wave.  Query j of the head group
-// is row j / grp, head j % grp of the group, so that a tile's queries have
+// A wave's tile: 16 queries of one KV head.  Query j of the head group is row
+// j / grp, head j % grp of the group, so that a tile's queries have
 // neighbouring rows.  Lane l holds query l % 16; of a page's scores it has
 // keys 16 t + 4 kg + i (kg = l / 16), of the outputs dims 16 n + 4 kg + i.
-template <typename A, int HD, int QT> struct Tiles {
+template <typename A, int HD> struct Tile {
   static constexpr int NS = HD / 32;  // matrix steps along the head
   static constexpr int NP = HD / 16;  // 1 KB pieces of a page's keys (and values)
-  f16x8_t qh[QT][NS], qlo[QT][NS];
-  float cq[QT];                       // score units: 2^(row's exponent) log2(e) / sqrt(hd)
-  int qi[QT], qhd[QT];
-  bool valid[QT];
-  float m[QT], l[QT];
-  f32x4_t o[QT][NP];                  // in units of the value scale `unit`
-  int unit;                           // the bits of a power of two (0 before the first page)
+  f16x8_t qh[NS], qlo[NS];
+  float cq;         // score units: 2^(row's exponent) log2(e) / sqrt(hd)
+  int qi, qhd;      // the lane's query: row in the sequence, head
+  bool valid;
+  float m, l;
+  f32x4_t o[NP];    // in units of the value scale `unit`
+  int unit;         // the bits of a power of two (0 before the first page)
   float minus_one;
 
   __device__ __forceinline__ void init(const Kv8Args& a, const Seq& q, int g, int tile0) {
@@ -146,48 +146,43 @@ template <typename A, int HD, int QT> struct Tiles {
     unit = 0;
     minus_one = -1.f;
     asm("" : "+s"(minus_one));
+    const int j = tile0 * 16 + ql;
+    valid = j < nq;
+    qi = valid ? j / grp : 0;
+    qhd = g * grp + (valid ? j - qi * grp : 0);
+    float v[NS][8], amax = 0.f;
+    const A* p = reinterpret_cast<const A*>(a.q) + ((size_t)(q.r0 + qi) * a.H + qhd) * HD + kg * (HD / 4);
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      const int j = (tile0 + t) * 16 + ql;
-      valid[t] = j < nq;
-      qi[t] = valid[t] ? j / grp : 0;
-      qhd[t] = g * grp + (valid[t] ? j - qi[t] * grp : 0);
-      float v[NS][8], amax = 0.f;
-      const A* p = reinterpret_cast<const A*>(a.q) + ((size_t)(q.r0 + qi[t]) * a.H + qhd[t]) * HD + kg * (HD / 4);
+    for (int c = 0; c < NS; ++c) {
+      load_q8<A>(p + 8 * c, a.q_plane, v[c]);
 #pragma unroll
-      for (int c = 0; c < NS; ++c) {
-        load_q8<A>(p + 8 * c, a.q_plane, v[c]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(v[c][e]));
-      }
-      amax = query_max(amax);
-      // an infinite row stays as it is (and its output becomes NaN)
-      int ex = 0;
-      if (amax > 0.f && amax < INFINITY) {
-        (void)frexpf(amax, &ex);
-        ex = max(ex - 1, -100);
-      }
-      const float down = ldexpf(1.f, -ex);
-      cq[t] = ldexpf(1.4426950408889634f / sqrtf((float)HD), ex);
-#pragma unroll
-      for (int c = 0; c < NS; ++c) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[c][e] *= down;
-        split16(v[c], minus_one, qh[t][c], qlo[t][c]);
-      }
-      m[t] = -INFINITY;
-      l[t] = 0.f;
-#pragma unroll
-      for (int d = 0; d < NP; ++d) o[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(v[c][e]));
     }
+    amax = query_max(amax);
+    // an infinite row stays as it is (and its output becomes NaN)
+    int ex = 0;
+    if (amax > 0.f && amax < INFINITY) {
+      (void)frexpf(amax, &ex);
+      ex = max(ex - 1, -100);
+    }
+    const float down = ldexpf(1.f, -ex);
+    cq = ldexpf(1.4426950408889634f / sqrtf((float)HD), ex);
+#pragma unroll
+    for (int c = 0; c < NS; ++c) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[c][e] *= down;
+      split16(v[c], minus_one, qh[c], qlo[c]);
+    }
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int d = 0; d < NP; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
 
   // Scores of a page; piece(n): the lane's 16 key bytes of piece n.
-  template <typename F> __device__ __forceinline__ void scores(F piece, f32x4_t (&st)[QT][4]) const {
+  template <typename F> __device__ __forceinline__ void scores(F piece, f32x4_t (&st)[4]) const {
 #pragma unroll
-    for (int t = 0; t < QT; ++t)
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt) st[t][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int kt = 0; kt < 4; ++kt) st[kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int n = 0; n < NP; ++n) {
       const u32x4_t w = piece(n);
@@ -195,59 +190,54 @@ template <typename A, int HD, int QT> struct Tiles {
       for (int h = 0; h < 2; ++h) {
         const int kt = (2 * n + h) / NS, c = (2 * n + h) % NS;
         const f16x8_t k = f8_to_f16(w[2 * h], w[2 * h + 1], 1.f);
-#pragma unroll
-        for (int t = 0; t < QT; ++t) mfma16(st[t][kt], k, qh[t][c]);
-#pragma unroll
-        for (int t = 0; t < QT; ++t) mfma16(st[t][kt], k, qlo[t][c]);
+        mfma16(st[kt], k, qh[c]);
+        mfma16(st[kt], k, qlo[c]);
       }
     }
   }
 
-  // The slots of page p that tile t's queries see, this lane's keys at bits 16 t' + i.
-  __device__ __forceinline__ uint64_t seen(const Kv8Args& a, const Seq& q, int t, int p) const {
-    return seen_bits(a.vis ? a.vis + (size_t)(q.r0 + qi[t]) * kVisWords : nullptr, qi[t], q.n, p * kPage - q.C) >>
+  // The slots of page p that the lane's query sees, this lane's keys at bits 16 t + i.
+  __device__ __forceinline__ uint64_t seen(const Kv8Args& a, const Seq& q, int p) const {
+    return seen_bits(a.vis ? a.vis + (size_t)(q.r0 + qi) * kVisWords : nullptr, qi, q.n, p * kPage - q.C) >>
            (4 * ((threadIdx.x & 63) >> 4));
   }
 
   // -inf for the slots of page p that a query does not see.
-  __device__ __forceinline__ void mask(const Kv8Args& a, const Seq& q, int p, f32x4_t (&st)[QT][4]) const {
+  __device__ __forceinline__ void mask(const Kv8Args& a, const Seq& q, int p, f32x4_t (&st)[4]) const {
+    const uint64_t sees = seen(a, q, p);
+    const uint32_t half[2] = {(uint32_t)sees, (uint32_t)(sees >> 32)};
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      const uint64_t sees = seen(a, q, t, p);
-      const uint32_t half[2] = {(uint32_t)sees, (uint32_t)(sees >> 32)};
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        st[t][e >> 2][e & 3] = (half[e >> 3] >> (16 * ((e >> 2) & 1) + (e & 3))) & 1 ? st[t][e >> 2][e & 3] : -INFINITY;
-    }
+    for (int e = 0; e < 16; ++e)
+      st[e >> 2][e & 3] = (half[e >> 3] >> (16 * ((e >> 2) & 1) + (e & 3))) & 1 ? st[e >> 2][e & 3] : -INFINITY;
   }
 
-  // Tile t's weights of a page with that key scale.
-  __device__ __forceinline__ void weights(int t, const f32x4_t (&st)[QT][4], float key_scale, f16x8_t (&ph)[2],
+  // Weights of a page with that key scale.
+  __device__ __forceinline__ void weights(const f32x4_t (&st)[4], float key_scale, f16x8_t (&ph)[2],
                                           f16x8_t (&pl)[2]) {
-    const float f = cq[t] * key_scale;
+    const float f = cq * key_scale;
     float x[16], sum;
     auto compute = [&](float off) {
       sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[t][e >> 2][e & 3], f, off));
+        x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e >> 2][e & 3], f, off));
         sum += x[e];
       }
     };
-    compute(kWeightBits - m[t]);  // nothing seen yet: infinity or NaN
+    compute(kWeightBits - m);  // nothing seen yet: infinity or NaN
     if (__any(!(sum <= kMostWeight))) {
-      float mx = st[t][0][0];
+      float mx = st[0][0];
 #pragma unroll
-      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, st[t][e >> 2][e & 3]);
-      const float m_new = fmaxf(m[t], query_max(mx) * f), m_use = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(m[t] - m_use);
-      l[t] *= alpha;
-      m[t] = m_new;
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, st[e >> 2][e & 3]);
+      const float m_new = fmaxf(m, query_max(mx) * f), m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m - m_use);
+      l *= alpha;
+      m = m_new;
 #pragma unroll
-      for (int d = 0; d < NP; ++d) o[t][d] *= alpha;
+      for (int d = 0; d < NP; ++d) o[d] *= alpha;
       compute(kWeightBits - m_use);
     }
-    l[t] += sum;
+    l += sum;
     split16(x, minus_one, ph[0], pl[0]);
     split16(x + 8, minus_one, ph[1], pl[1]);
   }
@@ -260,9 +250,7 @@ template <typename A, int HD, int QT> struct Tiles {
     if (s > unit) {
       const float f = power_ratio(unit, s);
 #pragma unroll
-      for (int t = 0; t < QT; ++t)
-#pragma unroll
-        for (int d = 0; d < NP; ++d) o[t][d] *= f;
+      for (int d = 0; d < NP; ++d) o[d] *= f;
       unit = s;
     }
     return power_ratio(s, unit);
@@ -270,26 +258,25 @@ template <typename A, int HD, int QT> struct Tiles {
 
   // Weighted values; piece(n): the lane's 16 value bytes of piece n.
   template <typename F>
-  __device__ __forceinline__ void outputs(F piece, float vscale, const f16x8_t (&ph)[QT][2], const f16x8_t (&pl)[QT][2]) {
+  __device__ __forceinline__ void outputs(F piece, float vscale, const f16x8_t (&ph)[2], const f16x8_t (&pl)[2]) {
 #pragma unroll
     for (int n = 0; n < NP; ++n) {
       const u32x4_t w = piece(n);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const f16x8_t v = f8_to_f16(w[2 * j], w[2 * j + 1], vscale);
-#pragma unroll
-        for (int t = 0; t < QT; ++t) mfma16(o[t][n], v, ph[t][j]);
-#pragma unroll
-        for (int t = 0; t < QT; ++t) mfma16(o[t][n], v, pl[t][j]);
+        mfma16(o[n], v, ph[j]);
+        mfma16(o[n], v, pl[j]);
       }
     }
   }
 
   // The same two for pieces that come from LDS, in a fixed order: a piece's
   // reads run two pieces ahead, its conversions beside the matrix
-  // instructions of the piece before, and no matrix instruction follows the
-  // one that it adds to.  mul(n, i, k) is matrix instruction i of piece n on
-  // its operands k.  (The compiler's own order waits for each read.)
+  // instructions of the piece before.  mul(n, i, k) is matrix instruction i of
+  // piece n on its operands k.  (The compiler's own order waits for each read.
+  // That an instruction adds to the result of the one before costs nothing:
+  // two results in turn took the same time.)
   template <typename F, typename M> __device__ __forceinline__ static void feed(F piece, float scale, M mul) {
     u32x4_t w[3];
     F16x8 k[2][2];
@@ -309,31 +296,29 @@ template <typename A, int HD, int QT> struct Tiles {
       if (n + 2 < NP) w[(n + 2) % 3] = piece(n + 2);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < 4 * QT; ++i) {
+      for (int i = 0; i < 4; ++i) {
         mul(n, i, k[n & 1]);
         if (n + 1 < NP)
 #pragma unroll
-          for (int u = 0; u < 2 / QT; ++u) convert(n + 1, i * (2 / QT) + u);
+          for (int u = 0; u < 2; ++u) convert(n + 1, 2 * i + u);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
-  template <typename F> __device__ __forceinline__ void scores_fed(F piece, f32x4_t (&st)[QT][4]) const {
+  template <typename F> __device__ __forceinline__ void scores_fed(F piece, f32x4_t (&st)[4]) const {
 #pragma unroll
-    for (int t = 0; t < QT; ++t)
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt) st[t][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int kt = 0; kt < 4; ++kt) st[kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     feed(piece, 1.f, [&](int n, int i, const F16x8 (&k)[2]) {
-      const int h = i / (2 * QT), lo = i % (2 * QT) / QT, t = i % QT, kt = (2 * n + h) / NS, c = (2 * n + h) % NS;
-      mfma16(st[t][kt], k[h].v, lo ? qlo[t][c] : qh[t][c]);
+      const int h = i / 2, lo = i % 2, kt = (2 * n + h) / NS, c = (2 * n + h) % NS;
+      mfma16(st[kt], k[h].v, lo ? qlo[c] : qh[c]);
     });
   }
   template <typename F>
-  __device__ __forceinline__ void outputs_fed(F piece, float vscale, const f16x8_t (&ph)[QT][2],
-                                              const f16x8_t (&pl)[QT][2]) {
+  __device__ __forceinline__ void outputs_fed(F piece, float vscale, const f16x8_t (&ph)[2],
+                                              const f16x8_t (&pl)[2]) {
     feed(piece, vscale, [&](int n, int i, const F16x8 (&k)[2]) {
-      const int j = i / (2 * QT), lo = i % (2 * QT) / QT, t = i % QT;
-      mfma16(o[t][n], k[j].v, lo ? pl[t][j] : ph[t][j]);
+      const int j = i / 2, lo = i % 2;
+      mfma16(o[n], k[j].v, lo ? pl[j] : ph[j]);
     });
   }
 
@@ -341,38 +326,29 @@ template <typename A, int HD, int QT> struct Tiles {
   // with the code of 1.
   template <typename F>
   __device__ __forceinline__ void poison(const Kv8Args& a, const Seq& q, int p, F ones) {
-    f16x8_t b[QT][2];  // 1 for the keys that a query sees
+    f16x8_t b[2];  // 1 for the keys that a query sees
+    const uint64_t sees = seen(a, q, p);
+    const uint32_t half[2] = {(uint32_t)sees, (uint32_t)(sees >> 32)};
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      const uint64_t sees = seen(a, q, t, p);
-      const uint32_t half[2] = {(uint32_t)sees, (uint32_t)(sees >> 32)};
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) b[t][j][e] = (half[j] >> (16 * (e >> 2) + (e & 3))) & 1 ? 1.f : 0.f;
-    }
+      for (int e = 0; e < 8; ++e) b[j][e] = (half[j] >> (16 * (e >> 2) + (e & 3))) & 1 ? 1.f : 0.f;
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int n = 0; n < NP; ++n) {
       const u32x4_t w = ones(n);
+      f32x4_t hit = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        f32x4_t hit = {0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < 2; ++j) mfma16(hit, f8_to_f16(w[2 * j], w[2 * j + 1], 1.f), b[j]);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) mfma16(hit, f8_to_f16(w[2 * j], w[2 * j + 1], 1.f), b[t][j]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[t][n][i] = hit[i] > 0.f ? NAN : o[t][n][i];
-      }
+      for (int i = 0; i < 4; ++i) o[n][i] = hit[i] > 0.f ? NAN : o[n][i];
       __builtin_amdgcn_sched_barrier(0);
     }
   }
 
   __device__ __forceinline__ void finish() {
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      l[t] += __shfl_xor(l[t], 16);
-      l[t] += __shfl_xor(l[t], 32);
-    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
   }
 };
 
@@ -421,7 +397,7 @@ template <bool ONCE> __device__ __forceinline__ u32x4_t load16(const uint8_t* p)
 // 4 KV heads of 128 dims: 57.4 us, 5.7 TB/s.
 template <typename A, int HD>
 __global__ void __launch_bounds__(256, 2) k_attention_kv8_few(Kv8Args a) {
-  using T = Tiles<A, HD, 1>;
+  using T = Tile<A, HD>;
   constexpr int NP = T::NP;
   __shared__ float s_o[kWaves][16][HD + 4], s_m[kWaves][16], s_l[kWaves][16];
   const int s = blockIdx.x / a.G, g = blockIdx.x % a.G, split = blockIdx.y;
@@ -460,13 +436,13 @@ __global__ void __launch_bounds__(256, 2) k_attention_kv8_few(Kv8Args a) {
     after = entry(p + 2 * kWaves);
 #pragma unroll
     for (int n = 0; n < NP; ++n) vr[n] = load16<true>(page + (size_t)(a.G + g) * kPage * HD + n * 1024 + lane * 16);
-    f32x4_t st[1][4];
+    f32x4_t st[4];
     w.scores([&](int n) { return kr[n]; }, st);
     const float2 scale = {same(sc.x), same(sc.y)};
     if (p + kWaves < p1) load_keys(next);
     if (id >= 0) {  // a bad page's slots are seen by nobody
       const float vscale = w.value_scale(scale.y);
-      f16x8_t ph[1][2], pl[1][2];
+      f16x8_t ph[2], pl[2];
       if constexpr (kEdge) {
         w.mask(a, q, p, st);
         // 0 times NaN is NaN: NaN codes are taken out, and the rows that see one get it back
@@ -479,7 +455,7 @@ __global__ void __launch_bounds__(256, 2) k_attention_kv8_few(Kv8Args a) {
           for (int n = 0; n < NP; ++n) vr[n] = without_nans(vr[n]);
         }
       }
-      w.weights(0, st, scale.x, ph[0], pl[0]);
+      w.weights(st, scale.x, ph, pl);
       w.outputs([&](int n) { return vr[n]; }, vscale, ph, pl);
     }
     id = next;
@@ -495,10 +471,10 @@ __global__ void __launch_bounds__(256, 2) k_attention_kv8_few(Kv8Args a) {
 #pragma unroll
   for (int n = 0; n < NP; ++n)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s_o[wave][ql][16 * n + 4 * kg + i] = w.o[0][n][i] * __uint_as_float(w.unit);
+    for (int i = 0; i < 4; ++i) s_o[wave][ql][16 * n + 4 * kg + i] = w.o[n][i] * __uint_as_float(w.unit);
   if (kg == 0) {
-    s_m[wave][ql] = w.m[0];
-    s_l[wave][ql] = w.l[0];
+    s_m[wave][ql] = w.m;
+    s_l[wave][ql] = w.l;
   }
   __syncthreads();
   // wave w merges pieces w, w + 4, ...; its lanes keep their query
@@ -510,30 +486,31 @@ __global__ void __launch_bounds__(256, 2) k_attention_kv8_few(Kv8Args a) {
     f[i] = s_m[i][ql] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[i][ql] - m);
     l += s_l[i][ql] * f[i];
   }
-  if (w.valid[0])
+  if (w.valid)
     for (int n = wave; n < NP; n += kWaves) {
       float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < kWaves; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] += f[i] * s_o[i][ql][16 * n + 4 * kg + e];
-      put_outputs<A>(a, q.r0 + w.qi[0], w.qhd[0], split, 16 * n + 4 * kg, m, l, v);
+      put_outputs<A>(a, q.r0 + w.qi, w.qhd, split, 16 * n + 4 * kg, m, l, v);
     }
 }
 
-// More tiles: QT of its own for each of W waves.  Workgroup: KV head, W QT
-// tiles, key split.  A page's codes go from memory to one of two LDS buffers without
-// passing registers, while the page before is worked on; the waves read them
-// as operands and turn them to fp16 (as fp16 in LDS the writes alone, 32 KB a
-// page at the 31 bytes a cycle that they reach, took a quarter of the time).
-// 512 rows after up to 8000 keys, heads as above: 135 us, 122 GFLOP issued at
-// 0.90 PFLOP/s.  Bound by issue: a wave's 128 matrix instructions a page take
-// 2050 cycles, its 350 vector instructions 1800, and the two waves of a SIMD
-// overlap these only in part.  (Half pages in a pipeline, one half's
-// exponentials beside the other's matrix work, ran out of registers: 143 us.)
-template <typename A, int HD, int QT, int W>
+// More tiles: one of its own for each of W waves.  Workgroup: KV head, W
+// tiles, key split.  A page's codes go from memory to one of two LDS buffers
+// without passing registers, while the page before is worked on; the waves
+// read them as operands and turn them to fp16 (as fp16 in LDS the writes
+// alone, 32 KB a page at the 31 bytes a cycle that they reach, took a quarter
+// of the time).  512 rows after up to 8000 keys, heads as above: 133 us, 122
+// GFLOP issued at 0.92 PFLOP/s.  Bound by issue: a page's 64 matrix
+// instructions of a wave take 1020 cycles, its 230 vector instructions 1150,
+// and the three waves of a SIMD overlap these in part.  Two tiles a wave share
+// the conversions, but leave registers for two waves a SIMD: 135 us, and 49.1
+// against 35.0 for 512 rows after 1000 keys, 17.0 against 11.0 for 16 rows.
+template <typename A, int HD, int W>
 __global__ void __launch_bounds__(64 * W, 2) k_attention_kv8_many(Kv8Args a) {
-  using T = Tiles<A, HD, QT>;
+  using T = Tile<A, HD>;
   constexpr int NP = T::NP;
   constexpr int kItems = 2 * NP / W;      // 1 KB pieces of a page that each wave brings
   __shared__ u32x4_t s_kv[2][2 * NP][64];      // pieces: keys, then values
@@ -548,15 +525,15 @@ __global__ void __launch_bounds__(64 * W, 2) k_attention_kv8_many(Kv8Args a) {
   if (!batch_seq(a.b, s, q)) return;
   const int nq = grp * q.n;
   const int lane = threadIdx.x & 63, wave = same((int)threadIdx.x >> 6), kg = lane >> 4;
-  if (group * W * QT * 16 >= nq) return;
+  if (group * W * 16 >= nq) return;
   const int pages = (q.C + q.n + kPage - 1) / kPage;
   const int p0 = split * a.chunk;
   int p1 = min(p0 + a.chunk, pages);
   if (p0 >= pages) return;
-  const int tile0 = (group * W + wave) * QT;
+  const int tile0 = group * W + wave;
   int mine = tile0 * 16 < nq ? p1 : p0;        // the wave's tiles need pages [p0, mine)
   if (!a.vis) {                                // causal: no slot past the last row
-    const int last_wave = min((tile0 + QT) * 16, nq) - 1, last = min((group + 1) * W * QT * 16, nq) - 1;
+    const int last_wave = min((tile0 + 1) * 16, nq) - 1, last = min((group + 1) * W * 16, nq) - 1;
     mine = min(mine, (q.C + last_wave / grp) / kPage + 1);
     p1 = min(p1, (q.C + last / grp) / kPage + 1);
   }
@@ -600,12 +577,11 @@ __global__ void __launch_bounds__(64 * W, 2) k_attention_kv8_many(Kv8Args a) {
     if (work) {
       auto key = [&](int n) { return s_kv[buf][n][lane]; };
       auto value = [&](int n) { return s_kv[buf][NP + n][lane]; };
-      f32x4_t st[QT][4];
+      f32x4_t st[4];
       w.scores_fed(key, st);
       if constexpr (kEdge) w.mask(a, q, p, st);
-      f16x8_t ph[QT][2], pl[QT][2];
-#pragma unroll
-      for (int t = 0; t < QT; ++t) w.weights(t, st, key_scale, ph[t], pl[t]);
+      f16x8_t ph[2], pl[2];
+      w.weights(st, key_scale, ph, pl);
       if constexpr (kEdge) {
         // 0 times NaN is NaN: NaN codes are taken out, and the rows that see one get it back
         bool any = false;
@@ -630,14 +606,12 @@ __global__ void __launch_bounds__(64 * W, 2) k_attention_kv8_many(Kv8Args a) {
 #pragma unroll 1
   for (; p < p1; ++p) step(std::true_type{}, p);
   w.finish();
-#pragma unroll
-  for (int t = 0; t < QT; ++t)
-    if (w.valid[t])
+    if (w.valid)
 #pragma unroll
       for (int n = 0; n < NP; ++n) {
         const float unit = __uint_as_float(w.unit);
-        float v[4] = {w.o[t][n][0] * unit, w.o[t][n][1] * unit, w.o[t][n][2] * unit, w.o[t][n][3] * unit};
-        put_outputs<A>(a, q.r0 + w.qi[t], w.qhd[t], split, 16 * n + 4 * kg, w.m[t], w.l[t], v);
+        float v[4] = {w.o[n][0] * unit, w.o[n][1] * unit, w.o[n][2] * unit, w.o[n][3] * unit};
+        put_outputs<A>(a, q.r0 + w.qi, w.qhd, split, 16 * n + 4 * kg, w.m, w.l, v);
       }
 }
 
@@ -713,29 +687,24 @@ __global__ void __launch_bounds__(256) k_attention_kv8_merge(Kv8Args a, int bloc
 // row after 1024 keys 9.7 us, split five ways 6.0 and 3.2 for the merge);
 // beyond, 512 workgroups of 4 to 24 pages (64 ragged sequences of up to 8192:
 // 24 pages 57.6 us, 64 pages 61.7).
-// More tiles: as many splits as fill the chip's places, of 8 pages or more
-// (192 rows after 2048 keys: 8 pages 29.2 us and 6.4 for the merge, 4 pages
-// 30.5 and 13), or of 4 where these leave most of the chip free (16 rows after
-// 1024 keys: 17.2 against 23.9 us).  A compute unit has places for two
-// workgroups of four waves with two tiles a wave, and for three with one tile,
-// whose registers allow it (64 sequences of 6 rows after up to 4000 keys 54.1
-// us, 62.9 with two).  Two tiles have workgroups of two waves, four a compute
-// unit, as two more waves would only load (the same with 4 rows 41.8 us, 57.6
-// with four waves); three and four tiles as two waves of two tiles would take
-// 64.7 and 67.0 us, as four of one 62.1 and 63.9.
+// More tiles: as many splits as fill the chip's places, three workgroups of
+// four waves a compute unit (64 sequences of 6 rows after up to 4000 keys 54.1
+// us, 62.0 with two), of 8 pages or more (192 rows after 2048 keys: 8 pages
+// 25.8 us and 6.4 for the merge, 4 pages 24.1 and 12.9), or of 4 where these
+// leave most of the chip free (16 rows after 1024 keys: 10.5 against 14.7 us).
+// Two tiles have workgroups of two waves, four a compute unit, as two more
+// waves would only load (64 sequences of 4 rows 41.9 us, 57.6 with four waves).
 void kv8_plan(Kv8Args& a) {
   const int tiles = (int)(((int64_t)a.H / a.G * a.b.max_rows + 15) / 16);
-  a.qt = tiles == 1 ? 0 : tiles <= kWaves ? 1 : 2;
-  a.waves = tiles == 2 ? 2 : kWaves;
-  a.groups = a.qt == 0 ? 1 : (tiles + a.waves * a.qt - 1) / (a.waves * a.qt);
+  a.waves = tiles <= 2 ? tiles : kWaves;
+  a.groups = (tiles + a.waves - 1) / a.waves;
   const int pages = (a.b.max_ctx + kPage - 1) / kPage;
   const int64_t base = (int64_t)a.b.n_seqs * a.G * a.groups;
-  if (a.qt == 0) {
+  if (tiles == 1) {
     const int64_t c = (base * pages / 512 + 2) / 4 * 4;
     a.chunk = pages <= 20 ? pages : (int)std::min<int64_t>(std::max<int64_t>(c, 4), 24);
   } else {
-    const int places = a.waves == 2 ? 1024 : a.qt == 1 ? 768 : 512;
-    const int64_t want = std::max<int64_t>(places / base, 1);
+    const int64_t want = std::max<int64_t>((a.waves == 2 ? 1024 : 768) / base, 1);
     a.chunk = std::max<int>((int)((pages + want - 1) / want), base * pages <= 1024 ? 4 : 8);
   }
   a.chunk = std::max(a.chunk, (pages + kMaxSplits - 1) / kMaxSplits);
@@ -746,10 +715,9 @@ template <typename A, int HD>
 static void attention_qt(const Kv8Args& a, hipStream_t st) {
   const dim3 few((unsigned)(a.b.n_seqs * a.G), (unsigned)a.splits);
   const unsigned many = (unsigned)((a.b.n_seqs * a.G * a.groups * a.splits + kXcds - 1) / kXcds * kXcds);
-  if (a.qt == 0) k_attention_kv8_few<A, HD><<<few, 256, 0, st>>>(a);
-  else if (a.waves == 2) k_attention_kv8_many<A, HD, 1, 2><<<many, 128, 0, st>>>(a);
-  else if (a.qt == 1) k_attention_kv8_many<A, HD, 1, 4><<<many, 256, 0, st>>>(a);
-  else k_attention_kv8_many<A, HD, 2, 4><<<many, 256, 0, st>>>(a);
+  if (a.waves == 1) k_attention_kv8_few<A, HD><<<few, 256, 0, st>>>(a);
+  else if (a.waves == 2) k_attention_kv8_many<A, HD, 2><<<many, 128, 0, st>>>(a);
+  else k_attention_kv8_many<A, HD, 4><<<many, 256, 0, st>>>(a);
 }
 template <typename A> static hipError_t attention_act(const Kv8Args& a, hipStream_t st) {
   if (a.hd == 32) attention_qt<A, 32>(a, st);

@@ -325,8 +325,7 @@ struct Kv8Args {
   float* o_part;             // [splits][n_rows * H][hd]
   float* ml_part;            // [splits][n_rows * H][2]
   // the plan (kv8_plan)
-  int qt;                    // query tiles of a wave (0: one tile, whose keys the waves share)
-  int waves;                 // waves of a workgroup
+  int waves;                 // waves with a query tile of their own in a workgroup (1: one tile, whose keys four waves share)
   int groups;                // workgroups along the query tiles
   int chunk;                 // pages of a key split
   int splits;
