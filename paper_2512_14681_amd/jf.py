@@ -365,7 +365,8 @@ class Batch:
         if not ctx.get_device() == row_start.get_device() == page_table.get_device():
             raise ValueError("row_start, ctx and page_table are on one device")
         self.device, self.n_rows, self.n_pages = ctx.get_device(), int(n_rows), int(n_pages)
-        self.c = JfBatch(n, self.n_rows, int(max_rows), int(max_ctx), int(n_pages), int(page_table.shape[1]),
+        # a looser bound on the rows than the slots allow is no other bound
+        self.c = JfBatch(n, self.n_rows, min(int(max_rows), int(max_ctx)), int(max_ctx), int(n_pages), int(page_table.shape[1]),
                          row_start.data_ptr(), ctx.data_ptr(), page_table.data_ptr())
         self.ref = ctypes.byref(self.c)
         self.ws = {}    # {(n_heads, n_kv_heads, head_dim): bytes of attention_kv8's workspace}

@@ -227,3 +227,12 @@ def test_binding_refuses_short_tensors(monkeypatch):
     x = torch.zeros(3, 5000)
     with pytest.raises(ValueError, match="expected"):
         jf.token_logprobs(x, torch.zeros(jf.token_logprobs_ws_bytes(3, 5000, 4) - 1, dtype=torch.uint8), k=4)
+
+
+def test_batch_takes_a_loose_bound_on_the_rows():
+    """More rows a sequence than the slots allow: the call itself refuses it, the binding takes the slots' bound."""
+    import torch
+    i32 = dict(dtype=torch.int32)
+    b = jf.Batch(torch.zeros(3, **i32), torch.zeros(2, **i32), torch.zeros(2, 1, **i32), 4, 70, 33, 3)
+    assert (b.c.max_rows, b.c.max_ctx) == (33, 33)
+    assert jf.attention_kv8_ws_bytes(b, 4, 2, 64) > 0
