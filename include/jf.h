@@ -453,7 +453,8 @@ jf_status jf_kv_append(const jf_batch *batch, int32_t n_heads, int32_t n_kv_head
 
 /* Reads slots d_ctx[s] .. d_ctx[s] + rows - 1 back as the values they hold:
  * d_k, d_v rows [n_rows][n_kv_heads * head_dim] of x_dtype, ld_* elements
- * apart (JF_BF16 holds an e4m3 value exactly). */
+ * apart (JF_BF16 holds an e4m3 value exactly).  d_kv must start on a 16-byte
+ * boundary.  Rows whose page is bad stay as they were. */
 jf_status jf_kv_read(const jf_batch *batch, int32_t n_kv_heads, int32_t head_dim, int32_t kv_dtype, int32_t x_dtype,
                      const void *d_kv, void *d_k, int64_t ld_k, void *d_v, int64_t ld_v, int32_t *d_flags,
                      jf_stream stream);
