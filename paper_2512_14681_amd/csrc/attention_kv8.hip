@@ -569,8 +569,9 @@ __global__ void __launch_bounds__(64 * W, 2) k_attention_kv8_many(Kv8Args a) {
     // every wave's pieces of page p have arrived, and its work on the page before is done
     wait_vm<0>();
     __syncthreads();
-    const float key_scale = same(sc.x), vscale = w.value_scale(sc.y);
-    const bool work = id >= 0 && p < mine;   // a bad page's slots are seen by nobody
+    // a bad page's slots are seen by nobody, and what stands in for it sets no scale
+    const float key_scale = same(sc.x), vscale = w.value_scale(id >= 0 ? sc.y : 0.f);
+    const bool work = id >= 0 && p < mine;
     const int next = batch_page_id(a.b, same(after));
     if (p + 1 < p1) load(buf ^ 1, next);
     after = entry(p + 2);
@@ -606,13 +607,13 @@ __global__ void __launch_bounds__(64 * W, 2) k_attention_kv8_many(Kv8Args a) {
 #pragma unroll 1
   for (; p < p1; ++p) step(std::true_type{}, p);
   w.finish();
-    if (w.valid)
+  if (w.valid)
 #pragma unroll
-      for (int n = 0; n < NP; ++n) {
-        const float unit = __uint_as_float(w.unit);
-        float v[4] = {w.o[n][0] * unit, w.o[n][1] * unit, w.o[n][2] * unit, w.o[n][3] * unit};
-        put_outputs<A>(a, q.r0 + w.qi, w.qhd, split, 16 * n + 4 * kg, w.m, w.l, v);
-      }
+    for (int n = 0; n < NP; ++n) {
+      const float unit = __uint_as_float(w.unit);
+      float v[4] = {w.o[n][0] * unit, w.o[n][1] * unit, w.o[n][2] * unit, w.o[n][3] * unit};
+      put_outputs<A>(a, q.r0 + w.qi, w.qhd, split, 16 * n + 4 * kg, w.m, w.l, v);
+    }
 }
 
 // Merges a row's key splits, four dims of one row and head a thread.  SG

@@ -402,6 +402,37 @@ def test_attention_rows_that_see_nothing(tj):
     assert (got[S.start[0]] == 0).all() and (got[S.start[1] + 5] == 0).all()
 
 
+@pytest.mark.parametrize("rows", [1, 6, 30])
+def test_attention_skips_a_bad_pages_slots(tj, rows):
+    """A table entry beyond the pool, while page 0 holds NaN scales: what attention over the other pages gives."""
+    torch, jf = tj
+    G, grp, hd, C = 2, 4, 64, 200
+    rng = np.random.default_rng(rows)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    table = np.array([[3, 5, 1, 4]], np.int32)
+    pool = ob.Pool8(np.zeros((6, ob.page_bytes(G, hd)), np.uint8), G, hd)
+    kv = rng.normal(size=(2, C + rows, G, hd))
+    ob.append(pool, [0, C + rows], [0], table, kv[0], kv[1])
+    k, v = (ob.gather(pool, table[0], C + rows, G, kind) for kind in (0, 1))
+    n = 2 * G * 64 * hd
+    pool.raw[0, :n] = 0x7F
+    pool.raw[0, n:n + 8 * G] = np.full(2 * G, np.nan, np.float32).view(np.uint8)
+    q = torch.tensor(rng.normal(size=(1, rows, G * grp, hd)), dtype=torch.float32).cuda()
+    bad = table.copy()
+    bad[0, 1] = 6
+    flags = torch.zeros(1, **i32)
+    b = jf.Batch(torch.tensor([0, rows], **i32), torch.tensor([C], **i32), torch.tensor(bad).cuda(), rows, rows, 256, 6)
+    out = torch.zeros(1, (rows + 15) // 16 * 16 * G * grp * hd, device="cuda")
+    ws = torch.empty(jf.attention_kv8_ws_bytes(b, G * grp, G, hd), dtype=torch.uint8, device="cuda")
+    jf.attention_kv8(b, G * grp, G, hd, jf.JF_F32, q, torch.tensor(pool.raw).cuda(), out, ws, d_flags=flags)
+    assert int(flags) == jf.JF_FLAG_BAD_PAGE
+    got = jf.act_unlayout(out[0].cpu().numpy(), rows, G * grp * hd).reshape(rows, G * grp, hd)
+    rest = np.r_[0:64, 128:C + rows]
+    want = ob.attention(q[0].double().cpu().numpy(), k[rest], v[rest], C - 64, np.tril(np.ones((rows, rows), bool)))
+    # scores below 16 in all: 2 (16 (2^-20 + 64 2^-24 + 2^-23)) of the largest value, and the sums
+    assert np.abs(got - want).max() <= (2 * 16 * (2.0 ** -20 + 2.0 ** -18 + 2.0 ** -23) + 80 * 2.0 ** -24) * np.abs(v).max()
+
+
 @pytest.mark.parametrize("rows", [6, 100])
 def test_attention_nan_reaches_only_the_rows_that_see_it(tj, rows):
     """NaN in a key (every output of the rows that see it) and in one dim of a value (that dim of them)."""
