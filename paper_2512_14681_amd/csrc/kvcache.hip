@@ -22,26 +22,28 @@
 namespace jf {
 
 // Sine and cosine of x turns: Taylor polynomials on an eighth of a turn to
-// either side of the nearest quarter, 1.2e-10 off at most, so that both are
-// the fp32 values next to the true ones.  About 25 instructions at the rate of
-// 32 bits.  In 32 bits from the fraction on, more rotated keys fell on the
-// other side of a rounding to e4m3 (a prefill's read-back keys 1.2e-4 off in
-// the root of the mean square, now 6.5e-5; the time is the same).
-__device__ __forceinline__ void sincos_turns(double x, float& sn, float& cs) {
+// either side of the nearest quarter, 1.2e-10 off at most, about 25
+// instructions at the rate of 32 bits.  The queries take them rounded to fp32.
+// The keys are turned in 64 bits and rounded once, as every error before the
+// rounding to e4m3 sends some of them to its other side (with 32-bit angles a
+// prefill's read-back keys were up to twice as far off as a plain rotation's;
+// the time is the same).
+template <typename R> __device__ __forceinline__ void sincos_turns(double x, R& sn, R& cs) {
   const double y = 4.0 * (x - rint(x)), n = rint(y), r = (y - n) * 1.5707963267948966, z = r * r;
   const double ps = 1.0 / 362880 - z * (1.0 / 39916800), pc = 1.0 / 40320 - z * (1.0 / 3628800);
-  const float s = (float)(r + r * z * (-1.0 / 6 + z * (1.0 / 120 + z * (-1.0 / 5040 + z * ps))));
-  const float c = (float)(1.0 + z * (-0.5 + z * (1.0 / 24 + z * (-1.0 / 720 + z * pc))));
+  const R s = (R)(r + r * z * (-1.0 / 6 + z * (1.0 / 120 + z * (-1.0 / 5040 + z * ps))));
+  const R c = (R)(1.0 + z * (-0.5 + z * (1.0 / 24 + z * (-1.0 / 720 + z * pc))));
   const int k = (int)n;  // -2 .. 2
-  const float u = k & 1 ? c : s, v = k & 1 ? s : c;
+  const R u = k & 1 ? c : s, v = k & 1 ? s : c;
   sn = k & 2 ? -u : u;
   cs = (k + 1) & 2 ? -v : v;
 }
 
 // Sine and cosine of four consecutive pairs at a position.
-__device__ __forceinline__ void angles4(const double* freq, int i, int pos, float (&cs)[4], float (&sn)[4]) {
+template <typename R>
+__device__ __forceinline__ void angles4(const double* freq, int i, int pos, R (&cs)[4], R (&sn)[4]) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) sincos_turns((double)pos * freq[i + e], sn[e], cs[e]);
+  for (int e = 0; e < 4; ++e) sincos_turns<R>((double)pos * freq[i + e], sn[e], cs[e]);
 }
 
 template <typename T> __device__ __forceinline__ void store4(T* p, const float (&v)[4]);
@@ -144,13 +146,13 @@ __global__ void __launch_bounds__(256) k_kv_append(AppendArgs a) {
       const int item = n * 256 + tid, c = item % (HD / 8), t = item / (HD / 8);
       if (t < t0 || t >= t1) continue;
       const int row = row0 + t;
-      float cs[4], sn[4];
+      double cs[4], sn[4];
       angles4(a.freq, 4 * c, a.pos ? a.pos[row] : q.C + row - q.r0, cs, sn);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float u = x[n][0][e], w = x[n][0][4 + e];
-        x[n][0][e] = u * cs[e] - w * sn[e];
-        x[n][0][4 + e] = w * cs[e] + u * sn[e];
+        x[n][0][e] = (float)((double)u * cs[e] - (double)w * sn[e]);
+        x[n][0][4 + e] = (float)((double)w * cs[e] + (double)u * sn[e]);
       }
     }
   }
