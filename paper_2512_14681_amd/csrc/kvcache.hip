@@ -24,10 +24,9 @@ namespace jf {
 // Sine and cosine of x turns: Taylor polynomials on an eighth of a turn to
 // either side of the nearest quarter, 1.2e-10 off at most, about 25
 // instructions at the rate of 32 bits.  The queries take them rounded to fp32.
-// The keys are turned in 64 bits and rounded once, as every error before the
-// rounding to e4m3 sends some of them to its other side (with 32-bit angles a
-// prefill's read-back keys were up to twice as far off as a plain rotation's;
-// the time is the same).
+// The keys are turned in 64 bits, as every error before the rounding to e4m3
+// sends some of them to its other side (a prefill's read-back keys are 4e-7
+// off, in 32 bits 7e-5, for half a microsecond of 64).
 template <typename R> __device__ __forceinline__ void sincos_turns(double x, R& sn, R& cs) {
   const double y = 4.0 * (x - rint(x)), n = rint(y), r = (y - n) * 1.5707963267948966, z = r * r;
   const double ps = 1.0 / 362880 - z * (1.0 / 39916800), pc = 1.0 / 40320 - z * (1.0 / 3628800);
@@ -99,6 +98,20 @@ template <int HD> struct AppendShared<HD, uint8_t> {
   float amax[2][4];
 };
 
+// A turned key in 32 bits: the nearest value, but for codes the neighbour with
+// an odd last bit where bits were lost, so that the second rounding, to e4m3,
+// is that of the 64-bit value (a tie in 32 bits is one in 64).
+template <typename KV> __device__ __forceinline__ float round_key(double y) {
+  const float t = (float)y;
+  if constexpr (sizeof(KV) == 1) {
+    const double left = y - (double)t;
+    const uint32_t b = __float_as_uint(t);
+    if (left != 0.0 && !(b & 1) && t != 0.f && fabsf(t) < INFINITY)
+      return __uint_as_float((left > 0.0) == (t > 0.f) ? b + 1 : b - 1);
+  }
+  return t;
+}
+
 // KV: float, bf16_t (pages of jf_model_load) or uint8_t (e4m3 pages).
 template <typename X, typename A, typename KV, int HD>
 __global__ void __launch_bounds__(256) k_kv_append(AppendArgs a) {
@@ -151,8 +164,8 @@ __global__ void __launch_bounds__(256) k_kv_append(AppendArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float u = x[n][0][e], w = x[n][0][4 + e];
-        x[n][0][e] = (float)((double)u * cs[e] - (double)w * sn[e]);
-        x[n][0][4 + e] = (float)((double)w * cs[e] + (double)u * sn[e]);
+        x[n][0][e] = round_key<KV>((double)u * cs[e] - (double)w * sn[e]);
+        x[n][0][4 + e] = round_key<KV>((double)w * cs[e] + (double)u * sn[e]);
       }
     }
   }
