@@ -465,7 +465,8 @@ jf_status jf_kv_read(const jf_batch *batch, int32_t n_kv_heads, int32_t head_dim
  * that sees nothing gets zeros; what a slot holds does not reach a row that
  * does not see it, NaN included.  d_q [n_rows][n_heads][head_dim] and d_out
  * are activation planes of act_dtype, d_out in the GEMM-input layout of
- * [n_rows][n_heads * head_dim] (a multiple of 128 columns); max_rows <=
+ * [n_rows][n_heads * head_dim] (a multiple of 128 columns), Rp * n_heads *
+ * head_dim elements per plane with Rp = n_rows rounded up to 16; max_rows <=
  * JF_MAX_ROWS.  d_q, d_kv, d_out and d_ws must start on 16-byte boundaries;
  * d_ws holds jf_attention_kv8_ws_bytes(...) bytes, needs no clearing and may
  * be shared by calls that do not overlap. */

@@ -438,10 +438,11 @@ def attention_kv8_ws_bytes(batch, n_heads, n_kv_heads, head_dim):
 def attention_kv8(batch, n_heads, n_kv_heads, head_dim, act_dtype, d_q, d_kv, d_out, d_ws, d_vis=None, d_flags=None,
                   stream=None):
     dev, n = _current_device(), batch.n_rows
-    rows = 4 * n * n_heads * head_dim   # bytes: fp32, or two bf16 planes
-    status = lib().jf_attention_kv8(batch.on(dev), n_heads, n_kv_heads, head_dim, act_dtype, _buf(dev, d_q, rows),
+    row = 4 * n_heads * head_dim        # bytes: fp32, or two bf16 planes
+    status = lib().jf_attention_kv8(batch.on(dev), n_heads, n_kv_heads, head_dim, act_dtype, _buf(dev, d_q, n * row),
                                     _buf(dev, d_kv, _pool_bytes(batch, n_kv_heads, head_dim, JF_E4M3)),
-                                    _buf(dev, d_vis, n * 8 * JF_VIS_WORDS), _buf(dev, d_out, rows),
+                                    _buf(dev, d_vis, n * 8 * JF_VIS_WORDS),
+                                    _buf(dev, d_out, (n + 15) // 16 * 16 * row),  # the layout's tiles have 16 rows
                                     _buf(dev, d_ws, _kv8_ws_bytes(batch, (n_heads, n_kv_heads, head_dim))),
                                     _vec(dev, d_flags, _I32, 1), _on(dev, stream))
     if status:

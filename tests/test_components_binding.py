@@ -1,0 +1,62 @@
+"""What the binding of the component calls lets through to the library, on host tensors and with the library's entry
+points replaced by ones that write down their arguments."""
+import types
+
+import pytest
+
+from paper_2512_14681_amd import jf
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The names of the library calls that were reached; host tensors pass for the GPU's."""
+    jf._types()
+    seen = []
+    real = jf.lib()
+
+    class Lib:
+        def __getattr__(self, name):
+            if name.endswith("_bytes"):
+                return getattr(real, name)
+            return lambda *a: seen.append(name) or jf.JF_OK
+    monkeypatch.setattr(jf, "lib", lambda: Lib())
+    monkeypatch.setattr(jf, "_current_device", lambda: -1)   # what host tensors answer
+    return seen
+
+
+STREAM = types.SimpleNamespace(cuda_stream=0)
+
+
+def batch(n_rows, max_rows=None, max_ctx=640):
+    import torch
+    i32 = dict(dtype=torch.int32)
+    return jf.Batch(torch.tensor([0, n_rows], **i32), torch.zeros(1, **i32), torch.zeros(1, 10, **i32), n_rows,
+                    max_rows or n_rows, max_ctx, 3)
+
+
+def layout_offset(row, col, K):
+    """The GEMM-input layout of include/jf.h: 16-row tiles of 128-column blocks."""
+    c = col % 128
+    return ((row // 16) * (K // 128) + col // 128) * 2048 + (c % 32) // 8 * 512 + (row % 16 + 16 * (c // 32)) * 8 + c % 8
+
+
+@pytest.mark.parametrize("n", [1, 4, 15, 16, 17, 100])
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+def test_attention_output_holds_whole_tiles(calls, n, act):
+    """d_out is written in tiles of 16 rows, its second plane behind whole tiles: a tensor of the rows alone is refused."""
+    import torch
+    H, G, hd = 4, 2, 32
+    K, Rp = H * hd, (n + 15) // 16 * 16
+    code, dt, planes = (jf.JF_F32, torch.float32, 1) if act == "f32" else (jf.JF_BF16, torch.bfloat16, 2)
+    last = (planes - 1) * Rp * K + max(layout_offset(n - 1, c, K) for c in range(K))
+    assert last < planes * Rp * K and (last >= planes * n * K or n % 16 == 0)
+    b = batch(n)
+    args = dict(d_q=torch.zeros(planes, n, H, hd, dtype=dt),
+                d_kv=torch.zeros(3 * jf.kv_page_bytes(G, hd, jf.JF_E4M3), dtype=torch.uint8),
+                d_ws=torch.zeros(jf.attention_kv8_ws_bytes(b, H, G, hd), dtype=torch.uint8), stream=STREAM)
+    for short in [planes * Rp * K - 1] + [planes * n * K] * (n % 16 != 0):
+        with pytest.raises(ValueError, match="expected"):
+            jf.attention_kv8(b, H, G, hd, code, d_out=torch.zeros(short, dtype=dt), **args)
+    assert calls == []
+    jf.attention_kv8(b, H, G, hd, code, d_out=torch.zeros(planes, Rp * K, dtype=dt), **args)
+    assert calls == ["jf_attention_kv8"]
