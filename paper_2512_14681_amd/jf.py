@@ -293,8 +293,8 @@ def _types():
     if not _DTYPES:
         import torch
         _DTYPES.update({torch.float32: JF_F32, torch.bfloat16: JF_BF16})
-        global _I32, _F32, _current_device, _raw_stream
-        _I32, _F32 = torch.int32, torch.float32
+        global _I32, _F32, _U8, _current_device, _raw_stream
+        _I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
         # the stream's address without a Stream object around it (2.7 us a call)
         _current_device, _raw_stream = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
     return _DTYPES
@@ -325,6 +325,13 @@ def _buf(dev, t, n):
     if t.nbytes < n or not t.is_contiguous():
         raise ValueError(f"expected a contiguous tensor of {n} bytes, got {tuple(t.shape)} of {t.dtype}")
     return _at(dev, t)
+
+
+def _act(dev, t, act_dtype, n):
+    """Address of activation planes of act_dtype in a contiguous tensor of that type (or raw bytes), n bytes or more."""
+    if t is not None and t.dtype is not _U8 and _DTYPES.get(t.dtype) != act_dtype and act_dtype in (JF_F32, JF_BF16):
+        raise TypeError(f"expected activation planes of jf_dtype {act_dtype}, got {t.dtype}")
+    return _buf(dev, t, n)
 
 
 def _rows(t, least=0, width=1):
@@ -401,7 +408,7 @@ def kv_append(batch, n_heads, n_kv_heads, head_dim, kv_dtype, d_kv, d_k, d_v, d_
     status = lib().jf_kv_append(batch.on(dev), n_heads, n_kv_heads, head_dim, kv_dtype, x, act_dtype, _at(dev, d_q),
                                 ld_q, _at(dev, d_k), ld_k, _at(dev, d_v), ld_v, _vec(dev, d_pos, _I32, n), rope_base,
                                 _buf(dev, d_kv, _pool_bytes(batch, n_kv_heads, head_dim, kv_dtype)),
-                                _buf(dev, d_q_out, 4 * n * n_heads * head_dim),  # fp32, or two bf16 planes
+                                _act(dev, d_q_out, act_dtype, 4 * n * n_heads * head_dim),  # fp32, or two bf16 planes
                                 _vec(dev, d_flags, _I32, 1), _on(dev, stream))
     if status:
         check(status)
@@ -439,10 +446,11 @@ def attention_kv8(batch, n_heads, n_kv_heads, head_dim, act_dtype, d_q, d_kv, d_
                   stream=None):
     dev, n = _current_device(), batch.n_rows
     row = 4 * n_heads * head_dim        # bytes: fp32, or two bf16 planes
-    status = lib().jf_attention_kv8(batch.on(dev), n_heads, n_kv_heads, head_dim, act_dtype, _buf(dev, d_q, n * row),
+    status = lib().jf_attention_kv8(batch.on(dev), n_heads, n_kv_heads, head_dim, act_dtype,
+                                    _act(dev, d_q, act_dtype, n * row),
                                     _buf(dev, d_kv, _pool_bytes(batch, n_kv_heads, head_dim, JF_E4M3)),
                                     _buf(dev, d_vis, n * 8 * JF_VIS_WORDS),
-                                    _buf(dev, d_out, (n + 15) // 16 * 16 * row),  # the layout's tiles have 16 rows
+                                    _act(dev, d_out, act_dtype, (n + 15) // 16 * 16 * row),  # 16 rows a tile
                                     _buf(dev, d_ws, _kv8_ws_bytes(batch, (n_heads, n_kv_heads, head_dim))),
                                     _vec(dev, d_flags, _I32, 1), _on(dev, stream))
     if status:

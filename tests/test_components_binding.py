@@ -60,3 +60,35 @@ def test_attention_output_holds_whole_tiles(calls, n, act):
     assert calls == []
     jf.attention_kv8(b, H, G, hd, code, d_out=torch.zeros(planes, Rp * K, dtype=dt), **args)
     assert calls == ["jf_attention_kv8"]
+
+
+@pytest.mark.parametrize("act,other", [("f32", "bf16"), ("bf16", "f32"), ("f32", "f16"), ("bf16", "i32")])
+def test_activation_planes_are_of_the_named_type(calls, act, other):
+    """act_dtype says what the queries and outputs hold; a tensor of another type is refused, bytes are taken."""
+    import torch
+    H, G, hd, n = 4, 2, 32, 16
+    dts = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16, "i32": torch.int32}
+    code = {"f32": jf.JF_F32, "bf16": jf.JF_BF16}[act]
+    b, size = batch(n), 4 * n * H * hd
+
+    def planes(dt):
+        return torch.zeros(size, dtype=torch.uint8).view(dt)
+    pool = torch.zeros(3 * jf.kv_page_bytes(G, hd, jf.JF_E4M3), dtype=torch.uint8)
+    rows = torch.zeros(n, G * hd)
+    ws = torch.zeros(jf.attention_kv8_ws_bytes(b, H, G, hd), dtype=torch.uint8)
+
+    def append(q_out):
+        jf.kv_append(b, H, G, hd, jf.JF_E4M3, pool, rows, rows, d_q=torch.zeros(n, H * hd), d_q_out=q_out, act_dtype=code,
+                     stream=STREAM)
+
+    def attend(q, out):
+        jf.attention_kv8(b, H, G, hd, code, q, pool, out, ws, stream=STREAM)
+    right, wrong = planes(dts[act]), planes(dts[other])
+    for call in (lambda: append(wrong), lambda: attend(wrong, right), lambda: attend(right, wrong)):
+        with pytest.raises(TypeError, match="expected"):
+            call()
+    assert calls == []
+    for t in (right, planes(torch.uint8)):
+        append(t)
+        attend(t, t.clone())
+    assert calls == ["jf_kv_append", "jf_attention_kv8"] * 2
