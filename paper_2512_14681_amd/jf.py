@@ -292,11 +292,12 @@ def _types():
     """{torch dtype: jf_dtype} of rows, and int32; torch is imported at the first use."""
     if not _DTYPES:
         import torch
-        _DTYPES.update({torch.float32: JF_F32, torch.bfloat16: JF_BF16})
         global _I32, _F32, _U8, _current_device, _raw_stream
         _I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
         # the stream's address without a Stream object around it (2.7 us a call)
         _current_device, _raw_stream = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
+        # last: who finds a type here (in another thread) finds the names above too
+        _DTYPES.update({torch.float32: JF_F32, torch.bfloat16: JF_BF16})
     return _DTYPES
 
 

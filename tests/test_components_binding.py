@@ -92,3 +92,18 @@ def test_activation_planes_are_of_the_named_type(calls, act, other):
         append(t)
         attend(t, t.clone())
     assert calls == ["jf_kv_append", "jf_attention_kv8"] * 2
+
+
+def test_the_types_appear_after_what_calls_need(monkeypatch):
+    """Another thread that finds the table of types filled finds the device and stream functions too."""
+    names = ("_I32", "_F32", "_U8", "_current_device", "_raw_stream")
+    jf._types()
+    for name in names:
+        monkeypatch.delattr(jf, name)
+
+    class Table(dict):
+        def update(self, *a):
+            assert all(hasattr(jf, name) for name in names)
+            super().update(*a)
+    monkeypatch.setattr(jf, "_DTYPES", Table())
+    assert len(jf._types()) == 2
