@@ -353,6 +353,13 @@ def _rows(t, least=0, width=1):
     return code, ld
 
 
+def _count(*counts):
+    """Refuses what a 32-bit argument would take for another number."""
+    for n in counts:
+        if not -1 << 31 <= n < 1 << 31:
+            raise JfError(JF_E_CAPACITY, f"{n} does not fit 32 bits")
+
+
 def _on(dev, stream):
     return _raw_stream(dev) if stream is None else stream.cuda_stream
 
@@ -372,6 +379,7 @@ class Batch:
             raise ValueError(f"{n} sequences need {n + 1} row starts and {n} rows of the page table")
         if not ctx.get_device() == row_start.get_device() == page_table.get_device():
             raise ValueError("row_start, ctx and page_table are on one device")
+        _count(n, int(n_rows), min(int(max_rows), int(max_ctx)), int(max_ctx), int(n_pages), page_table.shape[1])
         self.device, self.n_rows, self.n_pages = ctx.get_device(), int(n_rows), int(n_pages)
         # a looser bound on the rows than the slots allow is no other bound
         self.c = JfBatch(n, self.n_rows, min(int(max_rows), int(max_ctx)), int(max_ctx), int(n_pages), int(page_table.shape[1]),
@@ -460,6 +468,7 @@ def attention_kv8(batch, n_heads, n_kv_heads, head_dim, act_dtype, d_q, d_kv, d_
 
 @functools.lru_cache(4096)
 def token_logprobs_ws_bytes(R, V, k=0):
+    _count(R, V, k)
     return lib().jf_token_logprobs_ws_bytes(int(R), int(V), int(k))
 
 
@@ -484,6 +493,7 @@ def token_logprobs_grad(d_logits, d_norm, d_grad, d_tokens=None, d_entropy=None,
     if x != xg or d_grad.shape != d_logits.shape:
         raise TypeError("the gradient has the logits' shape and type")
     R, V = d_logits.shape
+    _count(R, V)
     dev = _current_device()
     status = lib().jf_token_logprobs_grad(R, V, x, _at(dev, d_logits), ld, _vec(dev, d_tokens, _I32, R),
                                           _vec(dev, d_norm, _F32, 2 * R), _vec(dev, d_entropy, _F32, R),

@@ -107,3 +107,25 @@ def test_the_types_appear_after_what_calls_need(monkeypatch):
             super().update(*a)
     monkeypatch.setattr(jf, "_DTYPES", Table())
     assert len(jf._types()) == 2
+
+
+def test_counts_beyond_32_bits_are_refused(calls):
+    """2^32 + 8 logits are not 8: the library's arguments have 32 bits (meta tensors, nothing is allocated)."""
+    import torch
+    V = 2 ** 32 + 8
+    x, g = (torch.empty(1, V, dtype=torch.bfloat16, device="meta") for _ in range(2))
+    norm, one = torch.zeros(1, 2), torch.zeros(1)
+    for call in (lambda: jf.token_logprobs(x, None, k=1),
+                 lambda: jf.token_logprobs_ws_bytes(3, V, 0), lambda: jf.token_logprobs_ws_bytes(2 ** 32 + 3, 8, 0),
+                 lambda: jf.token_logprobs_ws_bytes(3, 8, 2 ** 32 + 1),
+                 lambda: jf.token_logprobs_grad(x, norm, g, d_g_logprob=one, d_tokens=torch.zeros(1, dtype=torch.int32))):
+        with pytest.raises(jf.JfError) as e:
+            call()
+        assert e.value.status == jf.JF_E_CAPACITY
+    i32 = dict(dtype=torch.int32)
+    three = torch.zeros(2, **i32), torch.zeros(1, **i32), torch.zeros(1, 10, **i32)
+    for bounds in ((2 ** 32 + 4, 4, 640, 3), (4, 4, 2 ** 32 + 640, 3), (4, 4 - 2 ** 32, 640, 3), (4, 4, 640, 2 ** 31)):
+        with pytest.raises(jf.JfError) as e:
+            jf.Batch(*three, *bounds)
+        assert e.value.status == jf.JF_E_CAPACITY
+    assert calls == []
