@@ -20,6 +20,7 @@ paper's procedures:
 """
 from __future__ import annotations
 
+import functools
 import math
 
 import numpy as np
@@ -37,6 +38,28 @@ def pad_token(seed: int, pos: int, vocab: int) -> int:
     z = ((z ^ (z >> 30)) * 0xBF58476D1CE4E5B9) & _MASK
     z = ((z ^ (z >> 27)) * 0x94D049BB133111EB) & _MASK
     return (z ^ (z >> 31)) % vocab
+
+
+def _on_the_models_stream(loop):
+    """A loop that runs on the stream of a model that has one of its own: after what the current stream holds, which
+    then waits for it.  Fills, uploads and reads are in order with the model's calls that way."""
+    @functools.wraps(loop)
+    def run(self, *args, **kwargs):
+        own, cuda = self.m.stream, self.t.cuda
+        if own is None:
+            return loop(self, *args, **kwargs)
+        callers = cuda.current_stream()
+        own.wait_stream(callers)
+        try:
+            with cuda.stream(own):
+                out = loop(self, *args, **kwargs)
+        finally:
+            callers.wait_stream(own)
+        for x in out if isinstance(out, tuple) else ():
+            if self.t.is_tensor(x):     # allocated on the model's stream, used on the caller's
+                x.record_stream(callers)
+        return out
+    return run
 
 
 class Decoder:
@@ -75,6 +98,7 @@ class Decoder:
         self.m.jf_kv_truncate(0)
         self.trace = []
 
+    @_on_the_models_stream
     def prefill(self, prompt) -> int:
         toks = self.t.as_tensor(np.asarray(prompt, dtype=np.int32), device="cuda")
         self.m.jf_prefill(toks, self.d_pending)
@@ -86,6 +110,7 @@ class Decoder:
         buf[:k].copy_(self.h_stage[:k], non_blocking=True)
 
     # ---- Eq. 1 -----------------------------------------------------------------
+    @_on_the_models_stream
     def generate_ar(self, prompt, max_new: int):
         p = self.prefill(prompt)
         out = [p]
@@ -98,6 +123,7 @@ class Decoder:
         return out
 
     # ---- Eq. 3 / Eq. 4 / running window ------------------------------------------
+    @_on_the_models_stream
     def generate_jacobi(self, prompt, n: int, max_new: int, mode: str = "window",
                         pad_seed: int = 2, logits=None):
         """Returns (tokens, accept counts).  ``logits`` (optional list) gets,
@@ -134,6 +160,7 @@ class Decoder:
         return out[:max_new], accepts
 
     # ---- Sec. 2.1 trajectories ----------------------------------------------------
+    @_on_the_models_stream
     def collect_trajectories(self, prompt, n: int, n_blocks: int, pad_seed: int = 2):
         """Block-mode Jacobi decoding (Eq. 4) of n_blocks blocks of n tokens
         after the prompt, recording every iterate on the device
@@ -170,6 +197,7 @@ class Decoder:
         return d_traj, lengths
 
     # ---- teacher forcing ------------------------------------------------------------
+    @_on_the_models_stream
     def score(self, prompt, tokens, k: int = 0):
         """Log probabilities of given tokens after a prompt of two tokens or
         more: returns (logprob [T], entropy [T], top_ids [T][k],
@@ -204,6 +232,7 @@ class Decoder:
         return lp.cpu().numpy(), ent.cpu().numpy(), ids.cpu().numpy(), top.cpu().numpy()
 
     # ---- App. A Alg. 1 ------------------------------------------------------------
+    @_on_the_models_stream
     def generate_multiblock(self, prompt, n: int, K: int, r: float, max_new: int,
                             n_cand: int = 8, cand_len: int = 16, pool_cap: int = 64,
                             pad_seed: int = 2, logits=None):
