@@ -205,12 +205,16 @@ class Decoder:
         tokens[i] given prompt + tokens[:i].  The prompt without its last
         token is prefilled; steps of up to max_rows rows feed the rest and
         commit every row, and jf_token_logprobs reads their logits on the
-        device.  The cache then holds prompt + tokens[:-1]."""
+        device.  The cache then holds prompt + tokens[:-1].  ValueError for
+        an id outside the vocabulary, RuntimeError if a step raised a flag."""
         t, m, V = self.t, self.m, self.V
-        prompt = np.asarray(prompt, dtype=np.int32)
-        tokens = np.asarray(tokens, dtype=np.int32)
+        prompt, tokens = np.asarray(prompt), np.asarray(tokens)
         if len(prompt) < 2 or len(tokens) < 1:
             raise ValueError("score needs a prompt of two tokens or more and one token or more")
+        for ids in (prompt, tokens):
+            if ids.min() < 0 or ids.max() >= V:
+                raise ValueError(f"score needs token ids in [0, {V})")
+        prompt, tokens = prompt.astype(np.int32), tokens.astype(np.int32)
         T, R = len(tokens), m.cfg.max_rows
         self.prefill(prompt[:-1])
         feed = t.as_tensor(np.concatenate([prompt[-1:], tokens[:-1]]), device="cuda")
@@ -220,15 +224,20 @@ class Decoder:
         ids = t.empty((T, k), dtype=t.int32, device="cuda")
         logits = t.empty((min(R, T), V), **f32)
         ws = t.empty(jf.token_logprobs_ws_bytes(min(R, T), V, k), dtype=t.uint8, device="cuda")
+        flags = t.zeros(1, dtype=t.int32, device="cuda")
         for at in range(0, T, R):
             n = min(R, T - at)
             m.jf_jacobi_step(feed[at:at + n], n, 0, 0, self.d_argmax, self.d_result, self.d_next, logits)
+            flags.bitwise_or_(self.d_result[3:4])    # every step writes its own
             # every fed row is committed, accepted or not (argument of the commit: a result of n rows)
             self.d_result[0].fill_(n)
             m.jf_commit_kv(None, self.d_result)
             jf.token_logprobs(logits[:n], ws, d_tokens=d_tok[at:at + n], k=k, d_logprob=lp[at:at + n],
                               d_entropy=ent[at:at + n], d_top_ids=ids[at:at + n], d_top_logprob=top[at:at + n],
                               stream=m.stream)
+        raised = int(flags.cpu()[0])
+        if raised:
+            raise RuntimeError(f"score: a step raised the JF_FLAG_* bits {raised}")
         return lp.cpu().numpy(), ent.cpu().numpy(), ids.cpu().numpy(), top.cpu().numpy()
 
     # ---- App. A Alg. 1 ------------------------------------------------------------

@@ -121,3 +121,22 @@ def test_callers_wait_for_a_loop_that_fails(monkeypatch):
     with pytest.raises(ValueError):
         d.score([1], [2])
     assert log[-1] == ("wait", "callers", "models") and d.t.cuda.at.name == "callers"
+
+
+@pytest.mark.parametrize("flags", [[0, jf.JF_FLAG_CAPACITY], [jf.JF_FLAG_SYNC, 0], [jf.JF_FLAG_BAD_TOKEN]])
+def test_score_raises_what_any_step_flagged(monkeypatch, flags):
+    """Every step writes its own flags: those of an earlier one are not lost."""
+    d, _ = decoder(monkeypatch, own=False, flags=flags)
+    with pytest.raises(RuntimeError, match=f"bits {max(flags)}"):
+        d.score([1, 2, 3], [4, 5, 6, 7, 8])
+    d.score([1, 2, 3], [4, 5, 6, 7, 8])
+
+
+@pytest.mark.parametrize("prompt,tokens", [([1, V], [2]), ([1, -1], [2]), ([1, 2], [3, V, 4]), ([1, 2], [-1]),
+                                           ([1, 2], [2 ** 32 + 3]), (range(2 ** 40, 2 ** 40 + 3), [1])])
+def test_score_refuses_ids_that_are_no_tokens(monkeypatch, prompt, tokens):
+    """A step would read them as id 0 and go on from there."""
+    d, log = decoder(monkeypatch, own=False)
+    with pytest.raises(ValueError, match="token ids"):
+        d.score(prompt, tokens)
+    assert log == []
