@@ -89,6 +89,9 @@ __device__ __forceinline__ uint64_t from_lane_below(uint64_t v) {
   return (uint64_t)hi << 32 | lo;
 }
 
+// A logit's key: rising with the value, then with a falling column.  -0 and +0
+// are one value: the sum makes both +0.
+__device__ __forceinline__ uint64_t logit_key(float v, uint32_t col) { return argmax_key(v + 0.f, col); }
 // The value of a key.
 __device__ __forceinline__ float key_value(uint64_t k) {
   const uint32_t o = (uint32_t)(k >> 32);
@@ -132,7 +135,7 @@ template <typename T> struct TopList {
     for (int h = 0; h < kCand / 64; ++h) {
       const int i = 64 * h + lane;
       const uint64_t c = cand[i];
-      mine[h] = i >= n ? 0 : (i < sorted ? c : argmax_key(__uint_as_float((uint32_t)(c >> 32)), (uint32_t)c));
+      mine[h] = i >= n ? 0 : (i < sorted ? c : logit_key(__uint_as_float((uint32_t)(c >> 32)), (uint32_t)c));
       cand[i] = mine[h];
     }
     fence();
@@ -209,7 +212,7 @@ template <typename T> struct TopList {
     uint64_t key = lane < n ? cand[lane] : 0, kth = from_lane(key, k - 1);
 #pragma unroll
     for (int j = 0; j < kTileElems; ++j) {
-      const uint64_t c = x[j] >= low ? argmax_key(x[j], (uint32_t)tile_col<T>(base, tid, j)) : 0;
+      const uint64_t c = x[j] >= low ? logit_key(x[j], (uint32_t)tile_col<T>(base, tid, j)) : 0;
       uint64_t left = __ballot(c > kth);
       while (left) {
         const uint64_t y = from_lane(c, __builtin_ctzll(left));
