@@ -11,8 +11,9 @@
 // Precision: e4m3 codes are exact in fp16.  A row of Q, scaled by a power of
 // two to a largest element in [1, 2), and the weights, which are at most 2^15,
 // enter the matrix cores as two fp16 terms each, which hold 22 bits.  The
-// values' scales are applied relative to the largest one met so far; a page's
-// codes lose bits by that only 2^11 and more below it.
+// values' scales are applied to the codes, relative to a unit that follows the
+// scales where fp16 would not hold the codes exactly: no page's scale costs
+// another page's codes bits, whoever sees what set it.
 #include <algorithm>
 #include <type_traits>
 
@@ -102,8 +103,8 @@ __device__ __forceinline__ int same(int v) { return __builtin_amdgcn_readfirstla
 __device__ __forceinline__ float same(float v) {
   return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
 }
-// The bits of a power of two over those of one no smaller, as their ratio (0
-// below the normal range).
+// The bits of a power of two over those of another, as their ratio (0 below
+// the normal range).
 __device__ __forceinline__ float power_ratio(int a, int b) {
   const int d = a - b + 0x3F800000;
   return __uint_as_float(d > 0 ? d : 0);
@@ -124,6 +125,10 @@ __device__ __forceinline__ float query_max(float v) {
 // are.
 constexpr float kWeightBits = 10.f, kMostWeight = 32768.f;
 constexpr int kWaves = 4, kXcds = 8;
+// In the bits of a float: codes times 2^-11 .. 2^7 are exact in fp16 (448 2^7
+// is below its largest value, 2^-9 2^-11 above its smallest), outputs may
+// reach 2^124, and 2^-126 is the least normal number.
+constexpr int kScaleAbove = 7 << 23, kScaleBelow = 11 << 23, kMostOutput = (127 + 124) << 23, kLeastScale = 1 << 23;
 
 // A wave's tile: 16 queries of one KV head.  Query j of the head group is row
 // j / grp, head j % grp of the group, so that a tile's queries have
@@ -138,12 +143,12 @@ template <typename A, int HD> struct Tile {
   bool valid;
   float m, l;
   f32x4_t o[NP];    // in units of the value scale `unit`
-  int unit;         // the bits of a power of two (0 before the first page)
+  int unit;         // the bits of a power of two (the least one before the first page)
   float minus_one;
 
   __device__ __forceinline__ void init(const Kv8Args& a, const Seq& q, int g, int tile0) {
     const int grp = a.H / a.G, nq = grp * q.n, lane = threadIdx.x & 63, ql = lane & 15, kg = lane >> 4;
-    unit = 0;
+    unit = kLeastScale;
     minus_one = -1.f;
     asm("" : "+s"(minus_one));
     const int j = tile0 * 16 + ql;
@@ -242,18 +247,31 @@ template <typename A, int HD> struct Tile {
     split16(x + 8, minus_one, ph[1], pl[1]);
   }
 
-  // A page's value scale relative to the outputs' unit, which becomes the
-  // larger of the two (both in scalar registers; powers of two divide by
-  // their exponents).
+  // A page's value scale relative to the outputs' unit (both in scalar
+  // registers; powers of two divide by their exponents).
   __device__ __forceinline__ float value_scale(float scale) {
-    const int s = same((int)__float_as_uint(scale));
-    if (s > unit) {
-      const float f = power_ratio(unit, s);
-#pragma unroll
-      for (int d = 0; d < NP; ++d) o[d] *= f;
-      unit = s;
-    }
+    const int s = max(same((int)__float_as_uint(scale)), kLeastScale);
+    if (__builtin_expect(s > unit + kScaleAbove || s < unit - kScaleBelow, 0)) follow(s);
     return power_ratio(s, unit);
+  }
+  // The unit becomes s, or goes down as far as the outputs' range allows.
+  __device__ __forceinline__ void follow(int s) {
+    int to = s;
+    if (s < unit) {
+      float mine = 0.f;
+#pragma unroll
+      for (int d = 0; d < NP; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mine = fmaxf(mine, fabsf(o[d][i]));
+      int top = 0;  // over the lanes, one by one: exchanges would hold registers throughout the loop
+#pragma unroll 1
+      for (int i = 0; i < 64; ++i) top = max(top, __builtin_amdgcn_readlane((int)__float_as_uint(mine), i));
+      to = max(s, unit - min((kMostOutput - top) >> 23 << 23, 127 << 23));
+    }
+    const float f = power_ratio(unit, to);
+#pragma unroll
+    for (int d = 0; d < NP; ++d) o[d] *= f;
+    unit = to;
   }
 
   // Weighted values; piece(n): the lane's 16 value bytes of piece n.
@@ -569,20 +587,20 @@ __global__ void __launch_bounds__(64 * W, 2) k_attention_kv8_many(Kv8Args a) {
     // every wave's pieces of page p have arrived, and its work on the page before is done
     wait_vm<0>();
     __syncthreads();
-    // a bad page's slots are seen by nobody, and what stands in for it sets no scale
-    const float key_scale = same(sc.x), vscale = w.value_scale(id >= 0 ? sc.y : 0.f);
-    const bool work = id >= 0 && p < mine;
+    const float2 scale = {same(sc.x), same(sc.y)};
+    const bool work = id >= 0 && p < mine;  // a bad page's slots are seen by nobody
     const int next = batch_page_id(a.b, same(after));
     if (p + 1 < p1) load(buf ^ 1, next);
     after = entry(p + 2);
     if (work) {
       auto key = [&](int n) { return s_kv[buf][n][lane]; };
       auto value = [&](int n) { return s_kv[buf][NP + n][lane]; };
+      const float vscale = w.value_scale(scale.y);
       f32x4_t st[4];
       w.scores_fed(key, st);
       if constexpr (kEdge) w.mask(a, q, p, st);
       f16x8_t ph[2], pl[2];
-      w.weights(st, key_scale, ph, pl);
+      w.weights(st, scale.x, ph, pl);
       if constexpr (kEdge) {
         // 0 times NaN is NaN: NaN codes are taken out, and the rows that see one get it back
         bool any = false;
