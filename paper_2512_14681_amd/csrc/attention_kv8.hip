@@ -219,7 +219,7 @@ template <typename A, int HD> struct Tile {
   // Weights of a page with that key scale.
   __device__ __forceinline__ void weights(const f32x4_t (&st)[4], float key_scale, f16x8_t (&ph)[2],
                                           f16x8_t (&pl)[2]) {
-    const float f = cq * key_scale;
+    const float f = fmaxf(cq * key_scale, 1.17549435e-38f);  // 0 times the -inf of an unseen slot would be NaN
     float x[16], sum;
     auto compute = [&](float off) {
       sum = 0.f;

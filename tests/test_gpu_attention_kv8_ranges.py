@@ -87,3 +87,15 @@ def test_scales_apart_in_pages_that_all_rows_see(n, big):
     v[128:192] *= big
     v[600:640] *= big
     check(G, grp, hd, C, np.tril(np.ones((n, n), bool)), rng.normal(size=(C + n, G, hd)), v, rng.normal(size=(n, G * grp, hd)))
+
+
+@pytest.mark.parametrize("qs,ks", [(1e-30, 1e-15), (1e-25, 1e-25), (0.0, 1e-30), (1e-38, 1e-30)])
+@pytest.mark.parametrize("hd,grp,C,n", [(64, 4, 70, 3), (128, 7, 0, 2), (32, 2, 100, 40), (128, 2, 64, 150)])
+def test_scores_below_the_smallest_number(hd, grp, C, n, qs, ks):
+    """Queries and keys so small that every score is 0: the mean of the values that a row sees, no more of the others."""
+    rng = np.random.default_rng([hd, n])
+    G = 2
+    vis = np.tril(rng.random((n, n)) < 0.6)
+    vis[0] = False
+    check(G, grp, hd, C, vis, rng.normal(size=(C + n, G, hd)) * ks, rng.normal(size=(C + n, G, hd)),
+          rng.normal(size=(n, G * grp, hd)) * qs)
