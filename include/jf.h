@@ -438,10 +438,10 @@ size_t jf_kv_page_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t kv_dtype);
  * call that appends into a page takes the smallest power of two that brings
  * the finite new values there to 448 or less (1 if they are all 0) or, where
  * the page keeps earlier tokens (slots below d_ctx), the scale it has if that
- * is larger; if the scale grows, the kept tokens' codes are rounded anew on
- * it.  Codes round to nearest, ties to even; infinities saturate at 448 times
- * the scale and NaN stays NaN.  A scale never shrinks until the page is
- * appended to from its first token on.
+ * is larger (not a scale of 1 over kept tokens that are all 0); if the scale
+ * grows, the kept tokens' codes are rounded anew on it.  Codes round to
+ * nearest, ties to even; infinities saturate at 448 times the scale and NaN
+ * stays NaN.
  * Rows dropped by a verification need no call: the next append at the shorter
  * d_ctx overwrites them.  Slots that no row names keep what they hold.
  * d_kv and d_q_out must start on 16-byte boundaries.  No two sequences of a

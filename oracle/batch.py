@@ -96,11 +96,13 @@ class Pool8:
         return E4M3[self.raw[page, self.at[kind][g]]] * self.scale(page, g, kind)
 
     def append(self, page, g, kind, t0, new):
-        """new [m][hd] at tokens t0 .. t0 + m - 1; tokens below t0 are kept."""
+        """new [m][hd] at tokens t0 .. t0 + m - 1; tokens below t0 are kept.  Kept zeros on scale 1 (which zeros get)
+        do not hold the new ones to it."""
         need = block_scale(new)
-        scale = max(need, self.scale(page, g, kind)) if t0 else need
         at = self.at[kind][g]
-        if t0 and scale > self.scale(page, g, kind):
+        keeps = t0 and (self.scale(page, g, kind) != 1 or (self.raw[page, at[:t0]] & 127).any())
+        scale = max(need, self.scale(page, g, kind)) if keeps else need
+        if keeps and scale > self.scale(page, g, kind):
             kept = E4M3[self.raw[page, at[:t0]]] * self.scale(page, g, kind)
             self.raw[page, at[:t0]] = round_e4m3(kept / scale)
         self.raw[page, at[t0:t0 + len(new)]] = round_e4m3(new / scale)

@@ -112,6 +112,24 @@ template <typename KV> __device__ __forceinline__ float round_key(double y) {
   return t;
 }
 
+// The tokens of a head's code word i of an e4m3 page: a key word is four dims
+// of one token, a value word four tokens (this one and the next three) of a dim.
+template <int HD> __device__ __forceinline__ int key_token(int i) {
+  return ((i >> 8) * 16 + (i & 3) * 4) / (HD / 4) * 16 + ((i >> 2) & 15);
+}
+__device__ __forceinline__ int value_token(int i) { return (i & 3) * 16 + (i >> 6 & 3) * 4; }
+
+// Whether a head's keys (w = 0) or values are 0 in every token below t0: such
+// tokens got scale 1 for want of a value, and must not hold later ones to it.
+template <int HD> __device__ __forceinline__ bool kept_zeros(const uint32_t* codes, int w, int t0) {
+  uint32_t any = 0;
+  for (int i = threadIdx.x; i < 16 * HD; i += 256) {
+    const int n = w ? min(t0 - value_token(i), 4) : (key_token<HD>(i) < t0 ? 4 : 0);  // bytes of tokens below t0
+    if (n > 0) any |= codes[i] & (0x7F7F7F7Fu >> (32 - 8 * n));
+  }
+  return !__syncthreads_or((int)any);
+}
+
 // KV: float, bf16_t (pages of jf_model_load) or uint8_t (e4m3 pages).
 template <typename X, typename A, typename KV, int HD>
 __global__ void __launch_bounds__(256) k_kv_append(AppendArgs a) {
@@ -225,7 +243,8 @@ __global__ void __launch_bounds__(256) k_kv_append(AppendArgs a) {
     for (int w = 0; w < 2; ++w) {
       const float amax = fmaxf(fmaxf(sh.amax[w][0], sh.amax[w][1]), fmaxf(sh.amax[w][2], sh.amax[w][3]));
       const float need = f8_block_scale(amax);
-      const float old = t0 > 0 ? held[w] : need;
+      const bool keeps = t0 > 0 && !(held[w] == 1.f && need < 1.f && kept_zeros<HD>(codes[w], w, t0));
+      const float old = keeps ? held[w] : need;
       const float sc = fmaxf(old, need);
       inv[w] = 1.f / sc;  // a power of two: exact
       from[w] = t0;
@@ -279,10 +298,8 @@ __global__ void __launch_bounds__(256) k_kv_append(AppendArgs a) {
     // Words of four dims of one token (keys), of four tokens of one dim
     // (values); only the tokens written change.
     for (int i = tid; i < 16 * HD; i += 256) {
-      const int lane = (i >> 2) & 63, b = (i >> 8) * 16 + (i & 3) * 4;
-      const int tk = (b / (HD / 4)) * 16 + (lane & 15);
+      const int tk = key_token<HD>(i), tv = value_token(i);
       if (tk >= from[0] && tk < t1) codes[0][i] = sh.code[0][i];
-      const int tv = (i & 3) * 16 + (lane >> 4) * 4;
       if (tv >= from[1] && tv + 4 <= t1) {
         codes[1][i] = sh.code[1][i];
       } else {

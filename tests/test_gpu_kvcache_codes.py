@@ -145,3 +145,38 @@ def test_keys_of_an_fp32_cache_are_rounded_once(hd, base):
     want = ob.rotate(k, np.arange(n), base)
     mag = np.abs(k.reshape(n, G, 2, hd // 2)).sum(2)
     assert (np.abs(got - want) <= 2.0 ** -24 * np.abs(want) + EPS * np.concatenate([mag, mag], -1)).all()
+
+
+@pytest.mark.parametrize("hd,G", [(32, 3), (64, 2), (128, 2)])
+@pytest.mark.parametrize("t0", [1, 3, 17, 63])
+def test_zeros_hold_nobody_to_their_scale(hd, G, t0):
+    """Tokens of 0 (either sign) get scale 1; small ones appended after them get their own, whatever stands in the slots
+    behind.  Kept NaN and saturated infinities, which have scale 1 for want of finite values, keep it."""
+    import torch
+    from paper_2512_14681_amd import jf
+    rng = np.random.default_rng([hd, t0])
+    n = 70 - t0
+    i32 = dict(dtype=torch.int32, device="cuda")
+    table = torch.tensor([[1, 0]], **i32)
+    for kept in (0.0, -0.0, np.nan, np.inf, "one"):
+        raw = rng.integers(0, 127, (2, ob.page_bytes(G, hd))).astype(np.uint8)      # what an earlier sequence left
+        d, want = torch.tensor(raw).cuda(), ob.Pool8(raw, G, hd)
+        first = np.zeros((t0, G, hd))
+        first[:, 0] = 300.0 if kept == "one" else kept      # head 0 alone; a value that has scale 1 by itself
+        rest = rng.normal(size=(n, G, hd)) * 2.0 ** -12
+        for at, rows in ((0, first), (t0, np.float32(rest).astype(np.float64))):
+            b = jf.Batch(torch.tensor([0, len(rows)], **i32), torch.tensor([at], **i32), table, len(rows), len(rows), 128, 2)
+            x = torch.tensor(rows.reshape(len(rows), -1), dtype=torch.float32).cuda()
+            jf.kv_append(b, G, G, hd, jf.JF_E4M3, d, x, -x)
+            ob.append(want, [0, len(rows)], [at], [[1, 0]], rows, -rows)
+        got = ob.Pool8(d.cpu().numpy(), G, hd)
+        for g in range(G):
+            for kind in (0, 1):
+                small = g > 0 or kept == 0
+                assert (got.scale(1, g, kind) == 1) == (not small) and got.scale(1, g, kind) <= 1
+                a, b = (np.concatenate([w.values(1, g, kind), w.values(0, g, kind)])[:70] for w in (got, want))
+                assert np.array_equal(a, b, equal_nan=True)
+                if small:       # half a step of the values that are not subnormal on their scale
+                    x = rest[:, g] * (-1 if kind else 1)
+                    assert (np.abs(a[t0:64] - x[:64 - t0]) <= 2.0 ** -4 * np.abs(x[:64 - t0]) + 2.0 ** -10 * got.scale(1, g, kind)).all()
+        assert np.array_equal(got.raw[0, :2 * G * 64 * hd], want.raw[0, :2 * G * 64 * hd])
