@@ -401,8 +401,9 @@ jf_status jf_trajectory_select(const int32_t *d_traj, const int32_t *d_len,
  * JF_FLAG_CAPACITY is raised; a page table entry outside [0, n_pages) raises
  * JF_FLAG_BAD_PAGE and its tokens are skipped.  d_flags (optional, one int32)
  * gets these bits ORed in; the caller clears it.  n_seqs, n_rows or max_rows
- * = 0 does nothing; n_pages = 0 otherwise is JF_E_CAPACITY.  n_seqs times the workgroups that max_rows and max_ctx
- * call for must stay within 2^22 (JF_E_CAPACITY). */
+ * = 0 does nothing; n_pages = 0 otherwise is JF_E_CAPACITY.  n_seqs times the
+ * workgroups that max_rows and max_ctx call for must stay within 2^22
+ * (JF_E_CAPACITY). */
 typedef struct {
   int32_t n_seqs, n_rows, max_rows, max_ctx, n_pages, table_stride;
   const int32_t *d_row_start;  /* [n_seqs + 1] */
@@ -443,7 +444,11 @@ size_t jf_kv_page_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t kv_dtype);
  * nearest, ties to even; infinities saturate at 448 times the scale and NaN
  * stays NaN.
  * Rows dropped by a verification need no call: the next append at the shorter
- * d_ctx overwrites them.  Slots that no row names keep what they hold.
+ * d_ctx overwrites them.  Their scale stays: but for kept zeros, a scale does
+ * not shrink until the page is appended to from its first token on, so a draft
+ * row with a large element leaves the tokens of its page on coarser codes.
+ * Slots that no row names keep what they hold; in a JF_E4M3 page those past the
+ * rows keep their codes, which stand for other values on another scale.
  * d_kv and d_q_out must start on 16-byte boundaries.  No two sequences of a
  * call may write into the same page. */
 jf_status jf_kv_append(const jf_batch *batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t kv_dtype,
@@ -489,7 +494,8 @@ jf_status jf_attention_kv8(const jf_batch *batch, int32_t n_heads, int32_t n_kv_
  *     logits' ids and log probabilities in order (ties: lowest id first).
  * A logit of -inf has p = 0 and is no alternative; places beyond the finite
  * logits get id -1 and -inf.  A row that is no distribution (all -inf, +inf or
- * NaN among its logits) gets NaN everywhere and ids -1.  d_ws, 16-byte
+ * NaN among its logits) gets ids -1 and NaN everywhere else, but for the 0 of a
+ * row without a token.  d_ws, 16-byte
  * aligned, holds jf_token_logprobs_ws_bytes(R, V, k) bytes, which are enough
  * for fewer rows too, and needs no clearing.
  * R = 0 does nothing.  V <= 2^30, R <= 2^22. */
