@@ -123,7 +123,9 @@ __device__ __forceinline__ float query_max(float v) {
 // lane's 16 weights of a page sum to more than kMostWeight, which fp16 still
 // holds: most pages look for no maximum and leave sums and outputs as they
 // are.
-constexpr float kWeightBits = 10.f, kMostWeight = 32768.f;
+// A maximum beyond kFarScore is too coarse to hold kWeightBits beside it: the
+// weights are held to what fp16 holds one by one.
+constexpr float kWeightBits = 10.f, kMostWeight = 32768.f, kFarScore = 1 << 20;
 constexpr int kWaves = 4, kXcds = 8;
 // In the bits of a float: codes times 2^-11 .. 2^7 are exact in fp16 (448 2^7
 // is below its largest value, 2^-9 2^-11 above its smallest), outputs may
@@ -234,13 +236,27 @@ template <typename A, int HD> struct Tile {
       float mx = st[0][0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) mx = fmaxf(mx, st[e >> 2][e & 3]);
-      const float m_new = fmaxf(m, query_max(mx) * f), m_use = m_new == -INFINITY ? 0.f : m_new;
+      mx = query_max(mx);
+      float top = mx * f;
+      // beyond 2^24 the rounded product may lie far above the score itself, which would lose all weight
+      if (__builtin_fmaf(mx, f, -top) < -1.f) top -= fabsf(top) * 0x1p-23f;
+      const float m_new = fmaxf(m, top), m_use = m_new == -INFINITY ? 0.f : m_new;
       const float alpha = __builtin_amdgcn_exp2f(m - m_use);
       l *= alpha;
       m = m_new;
 #pragma unroll
       for (int d = 0; d < NP; ++d) o[d] *= alpha;
-      compute(kWeightBits - m_use);
+      if (__any(fabsf(m_use) > kFarScore)) {
+        sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float d = __builtin_fmaf(st[e >> 2][e & 3], f, -m_use);
+          x[e] = __builtin_amdgcn_exp2f((d > 4.f ? 4.f : d) + kWeightBits);  // NaN stays
+          sum += x[e];
+        }
+      } else {
+        compute(kWeightBits - m_use);
+      }
     }
     l += sum;
     split16(x, minus_one, ph[0], pl[0]);

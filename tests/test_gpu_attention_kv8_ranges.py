@@ -99,3 +99,15 @@ def test_scores_below_the_smallest_number(hd, grp, C, n, qs, ks):
     vis[0] = False
     check(G, grp, hd, C, vis, rng.normal(size=(C + n, G, hd)) * ks, rng.normal(size=(C + n, G, hd)),
           rng.normal(size=(n, G * grp, hd)) * qs)
+
+
+@pytest.mark.parametrize("qs,ks", [(1e5, 1.0), (1e8, 1.0), (1e9, 3.0), (1e10, 1e3), (1e15, 1e15)])
+@pytest.mark.parametrize("hd,grp,C,n", [(64, 4, 700, 3), (128, 7, 300, 2), (32, 2, 100, 40), (128, 2, 640, 150)])
+def test_scores_of_any_size(hd, grp, C, n, qs, ks):
+    """Scores far beyond what fp32 tells apart: nothing overflows, and the outputs are means of the values that a row sees."""
+    rng = np.random.default_rng([hd, n])
+    G = 2
+    vis = np.tril(rng.random((n, n)) < 0.6)
+    vis[0] = False
+    check(G, grp, hd, C, vis, rng.normal(size=(C + n, G, hd)) * ks, rng.normal(size=(C + n, G, hd)),
+          rng.normal(size=(n, G * grp, hd)) * qs)
