@@ -380,10 +380,15 @@ template <typename A, int HD> struct Tile {
     }
   }
 
+  // Sums and outputs (times factor()) as they are merged and divided: 2^-24 of
+  // what was summed, as values next to the largest number times weights of
+  // 2^kWeightBits would not fit.
   __device__ __forceinline__ void finish() {
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
+    l *= 0x1p-24f;
   }
+  __device__ __forceinline__ float factor() const { return __uint_as_float(unit) * 0x1p-24f; }
 };
 
 // A value page's NaN codes as codes of 1, and the codes without them.
@@ -505,7 +510,7 @@ __global__ void __launch_bounds__(256, 2) k_attention_kv8_few(Kv8Args a) {
 #pragma unroll
   for (int n = 0; n < NP; ++n)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s_o[wave][ql][16 * n + 4 * kg + i] = w.o[n][i] * __uint_as_float(w.unit);
+    for (int i = 0; i < 4; ++i) s_o[wave][ql][16 * n + 4 * kg + i] = w.o[n][i] * w.factor();
   if (kg == 0) {
     s_m[wave][ql] = w.m;
     s_l[wave][ql] = w.l;
@@ -644,7 +649,7 @@ __global__ void __launch_bounds__(64 * W, 2) k_attention_kv8_many(Kv8Args a) {
   if (w.valid)
 #pragma unroll
     for (int n = 0; n < NP; ++n) {
-      const float unit = __uint_as_float(w.unit);
+      const float unit = w.factor();
       float v[4] = {w.o[n][0] * unit, w.o[n][1] * unit, w.o[n][2] * unit, w.o[n][3] * unit};
       put_outputs<A>(a, q.r0 + w.qi, w.qhd, split, 16 * n + 4 * kg, w.m, w.l, v);
     }

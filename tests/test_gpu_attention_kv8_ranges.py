@@ -111,3 +111,13 @@ def test_scores_of_any_size(hd, grp, C, n, qs, ks):
     vis[0] = False
     check(G, grp, hd, C, vis, rng.normal(size=(C + n, G, hd)) * ks, rng.normal(size=(C + n, G, hd)),
           rng.normal(size=(n, G * grp, hd)) * qs)
+
+
+@pytest.mark.parametrize("hd,grp,C,n", [(64, 4, 700, 3), (128, 7, 300, 2), (32, 2, 100, 40), (128, 2, 640, 150)])
+@pytest.mark.parametrize("vs", [1e30, 1e35, 2e37, 1e-30])
+def test_values_of_any_size(hd, grp, C, n, vs):
+    """Values close to fp32's largest: their mean is a number, whatever the sum of the weights."""
+    rng = np.random.default_rng([hd, n])
+    G = 2
+    check(G, grp, hd, C, np.tril(np.ones((n, n), bool)), rng.normal(size=(C + n, G, hd)),
+          np.clip(rng.normal(size=(C + n, G, hd)), -4, 4) * vs, rng.normal(size=(n, G * grp, hd)))
