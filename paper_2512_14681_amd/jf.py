@@ -292,8 +292,9 @@ def _types():
     """{torch dtype: jf_dtype} of rows, and int32; torch is imported at the first use."""
     if not _DTYPES:
         import torch
-        global _I32, _F32, _U8, _current_device, _raw_stream
+        global _I32, _F32, _U8, _ACT, _current_device, _raw_stream
         _I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
+        _ACT = {JF_F32: torch.float32, JF_BF16: torch.bfloat16}
         # the stream's address without a Stream object around it (2.7 us a call)
         _current_device, _raw_stream = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
         # last: who finds a type here (in another thread) finds the names above too
@@ -330,9 +331,13 @@ def _buf(dev, t, n):
 
 def _act(dev, t, act_dtype, n):
     """Address of activation planes of act_dtype in a contiguous tensor of that type (or raw bytes), n bytes or more."""
-    if t is not None and t.dtype is not _U8 and _DTYPES.get(t.dtype) != act_dtype and act_dtype in (JF_F32, JF_BF16):
+    if t is None:
+        return None
+    if t.dtype is not _ACT.get(act_dtype, t.dtype) and t.dtype is not _U8:
         raise TypeError(f"expected activation planes of jf_dtype {act_dtype}, got {t.dtype}")
-    return _buf(dev, t, n)
+    if t.nbytes < n or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous tensor of {n} bytes, got {tuple(t.shape)} of {t.dtype}")
+    return _at(dev, t)
 
 
 def _rows(t, least=0, width=1):
