@@ -146,11 +146,14 @@ template <typename A, int HD> struct Tile {
   float m, l;
   f32x4_t o[NP];    // in units of the value scale `unit`
   int unit;         // the bits of a power of two (the least one before the first page)
+  int last;         // the page before's value scale, and that scale in units
+  float ratio;
   float minus_one;
 
   __device__ __forceinline__ void init(const Kv8Args& a, const Seq& q, int g, int tile0) {
     const int grp = a.H / a.G, nq = grp * q.n, lane = threadIdx.x & 63, ql = lane & 15, kg = lane >> 4;
-    unit = kLeastScale;
+    unit = last = kLeastScale;
+    ratio = 1.f;
     minus_one = -1.f;
     asm("" : "+s"(minus_one));
     const int j = tile0 * 16 + ql;
@@ -267,8 +270,12 @@ template <typename A, int HD> struct Tile {
   // registers; powers of two divide by their exponents).
   __device__ __forceinline__ float value_scale(float scale) {
     const int s = max(same((int)__float_as_uint(scale)), kLeastScale);
-    if (__builtin_expect(s > unit + kScaleAbove || s < unit - kScaleBelow, 0)) follow(s);
-    return power_ratio(s, unit);
+    if (__builtin_expect(s != last, 0)) {
+      last = s;
+      if (s > unit + kScaleAbove || s < unit - kScaleBelow) follow(s);
+      ratio = power_ratio(s, unit);
+    }
+    return ratio;
   }
   // The unit becomes s, or goes down as far as the outputs' range allows.
   __device__ __forceinline__ void follow(int s) {
