@@ -437,20 +437,20 @@ size_t jf_kv_page_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t kv_dtype);
  * act_dtype, as the attention calls take them.
  * JF_E4M3: the keys and the values of one head in one page share a scale.  A
  * call that appends into a page takes the smallest power of two that brings
- * the finite new values there to 448 or less (1 if they are all 0) or, where
- * the page keeps earlier tokens (slots below d_ctx), the scale it has if that
- * is larger (not a scale of 1 over kept tokens that are all 0); if the scale
- * grows, the kept tokens' codes are rounded anew on it.  Codes round to
- * nearest, ties to even; infinities saturate at 448 times the scale and NaN
- * stays NaN.
+ * the finite new values there to 448 or less (1 if they are all 0, 2^-100 at
+ * least) or, where the page keeps earlier tokens (slots below d_ctx), the scale
+ * it has if that is larger (not a scale of 1 over kept tokens that are all 0);
+ * if the scale grows, the kept tokens' codes are rounded anew on it.  Codes
+ * round to nearest, ties to even; infinities saturate at 448 times the scale
+ * and NaN stays NaN.
  * Rows dropped by a verification need no call: the next append at the shorter
  * d_ctx overwrites them.  Their scale stays: but for kept zeros, a scale does
  * not shrink until the page is appended to from its first token on, so a draft
  * row with a large element leaves the tokens of its page on coarser codes.
  * Slots that no row names keep what they hold; in a JF_E4M3 page those past the
  * rows keep their codes, which stand for other values on another scale.
- * d_kv and d_q_out must start on 16-byte boundaries.  No two sequences of a
- * call may write into the same page. */
+ * d_kv and d_q_out must start on 16-byte boundaries.  No page may be written
+ * twice by one call (by two sequences, or at two places of one's table). */
 jf_status jf_kv_append(const jf_batch *batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t kv_dtype,
                        int32_t x_dtype, int32_t act_dtype, const void *d_q, int64_t ld_q, const void *d_k,
                        int64_t ld_k, const void *d_v, int64_t ld_v, const int32_t *d_pos, double rope_base,

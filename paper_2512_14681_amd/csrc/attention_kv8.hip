@@ -440,7 +440,7 @@ template <bool ONCE> __device__ __forceinline__ u32x4_t load16(const uint8_t* p)
 // key split; the waves take every fourth page straight into registers, as
 // nobody shares it, the next page's keys in flight from when this one's scores
 // are done, and merge in LDS.  64 sequences of up to 8192 tokens, 28 query and
-// 4 KV heads of 128 dims: 57.4 us, 5.7 TB/s.
+// 4 KV heads of 128 dims: 58.0 us, 5.7 TB/s.
 template <typename A, int HD>
 __global__ void __launch_bounds__(256, 2) k_attention_kv8_few(Kv8Args a) {
   using T = Tile<A, HD>;
@@ -548,11 +548,11 @@ __global__ void __launch_bounds__(256, 2) k_attention_kv8_few(Kv8Args a) {
 // without passing registers, while the page before is worked on; the waves
 // read them as operands and turn them to fp16 (as fp16 in LDS the writes
 // alone, 32 KB a page at the 31 bytes a cycle that they reach, took a quarter
-// of the time).  512 rows after up to 8000 keys, heads as above: 133 us, 122
-// GFLOP issued at 0.92 PFLOP/s.  Bound by issue: a page's 64 matrix
+// of the time).  512 rows after up to 8000 keys, heads as above: 128 us, 122
+// GFLOP issued at 0.95 PFLOP/s.  Bound by issue: a page's 64 matrix
 // instructions of a wave take 1020 cycles, its 230 vector instructions 1150,
 // and the three waves of a SIMD overlap these in part.  Two tiles a wave share
-// the conversions, but leave registers for two waves a SIMD: 135 us, and 49.1
+// the conversions, but leave registers for two waves a SIMD: 2% more, and 49.1
 // against 35.0 for 512 rows after 1000 keys, 17.0 against 11.0 for 16 rows.
 template <typename A, int HD, int W>
 __global__ void __launch_bounds__(64 * W, 2) k_attention_kv8_many(Kv8Args a) {

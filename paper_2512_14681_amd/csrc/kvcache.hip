@@ -12,9 +12,9 @@
 //
 // Both are bound by memory for many rows and by three dependent loads (the
 // sequence, its page table entry, the page) for few.  Append: 14458 rows of 16
-// + 2 x 4 heads of 128 dims in fp32 to an e4m3 cache 63 us, 310 MB at 4.9
-// TB/s; one row 4.8 us, 64 sequences of one row 9.7 us.  Read: the 14458 rows
-// to bf16 14.5 us, 44 MB at 3.1 TB/s; the last pages of 64 sequences 6.8 us.
+// + 2 x 4 heads of 128 dims in fp32 to an e4m3 cache 67 us, 310 MB at 4.7
+// TB/s; one row 4.7 us, 64 sequences of one row 10.1 us.  Read: the 14458 rows
+// to bf16 14.6 us, 44 MB at 3.0 TB/s; the last pages of 64 sequences 6.5 us.
 #include <algorithm>
 
 #include "jf_batch.h"
@@ -25,8 +25,7 @@ namespace jf {
 // either side of the nearest quarter, 1.2e-10 off at most, about 25
 // instructions at the rate of 32 bits.  The queries take them rounded to fp32.
 // The keys are turned in 64 bits, as every error before the rounding to e4m3
-// sends some of them to its other side (a prefill's read-back keys are 4e-7
-// off, in 32 bits 7e-5, for half a microsecond of 64).
+// sends some of them to its other side, for half a microsecond of 64.
 template <typename R> __device__ __forceinline__ void sincos_turns(double x, R& sn, R& cs) {
   const double y = 4.0 * (x - rint(x)), n = rint(y), r = (y - n) * 1.5707963267948966, z = r * r;
   const double ps = 1.0 / 362880 - z * (1.0 / 39916800), pc = 1.0 / 40320 - z * (1.0 / 3628800);
@@ -342,7 +341,7 @@ __device__ __forceinline__ void put8(bf16_t* p, bool vec, const float (&v)[8]) {
 // of one token (head_dim 32: 8 dims of two) and go straight to its row; those
 // of the values are 16 tokens of one dim and pass through LDS, where the low
 // bits of a slot are turned by the piece so that the dims of a token lie in
-// different banks (14458 rows to bf16 14.5 us; byte by byte, in the page's own order, 20.8).
+// different banks (14458 rows to bf16 14.6 us; byte by byte, in the page's own order, 20.8).
 template <typename X, int HD>
 __device__ __forceinline__ void read_codes(const ReadArgs& a, const char* base, int g, int row0, int t0, int t1,
                                            uint4* sh) {

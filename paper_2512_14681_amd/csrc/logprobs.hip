@@ -5,10 +5,10 @@
 // u = sum e^(x - m) (x - m), all in fp32 and relative to the running maximum:
 //   log p_t = (x_t - m) - log s,   entropy = log s - u / s.
 // The alternatives are the k largest 64-bit keys (value, then lowest index).
-// Bound by memory without alternatives (512 rows of 152064 fp32 logits 56 us,
+// Bound by memory without alternatives (512 rows of 152064 fp32 logits 55 us,
 // 5.6 TB/s, kept in the caches for the gradient; 50 us if loaded as read once,
 // which calls with alternatives do), by the vector unit with them where the
-// rows are few (64 rows in bf16: k = 0 8 us, k = 8 13 us; 400 rows in fp32 and
+// rows are few (64 rows in bf16: k = 0 8 us, k = 8 12.4 us; 400 rows in fp32 and
 // k = 8 46 us, 5.2 TB/s).  A row is split until there are about four
 // workgroups a compute unit; a second launch joins (4 us).
 #include <algorithm>
