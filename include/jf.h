@@ -518,6 +518,127 @@ jf_status jf_token_logprobs_grad(int32_t R, int32_t V, int32_t dtype, const void
                                  const float *d_g_logprob, const float *d_g_entropy, void *d_grad, int64_t ld_grad,
                                  jf_stream stream);
 
+/* ---- causal attention over packed sequences, with its gradient ---------------
+ * Sequences lie one after the other in the row tensors: rows d_row_start[s] ..
+ * d_row_start[s + 1] - 1 (device, [n_seqs + 1], not decreasing) belong to
+ * sequence s, and each sees the rows of its own sequence up to itself.  Rows
+ * before d_row_start[0] and from d_row_start[n_seqs] on (padding) are neither
+ * read nor written.  A captured call takes new starts at every replay.  A
+ * sequence whose start or end lies outside [0, n_rows], or whose end lies
+ * before its start, is left as it was and JF_FLAG_CAPACITY is raised in
+ * d_flags (optional, one int32, ORed; the caller clears it).
+ * d_q, d_out [n_rows][n_heads * head_dim], d_k, d_v [n_rows][n_kv_heads *
+ * head_dim] are rows of dtype (JF_F32 or JF_BF16), ld_* elements apart (views
+ * into one fused projection, for instance); query head j reads KV head j /
+ * (n_heads / n_kv_heads); scores are q k / sqrt(head_dim), head_dim in {32,
+ * 64, 128}.  Rows that start on 16-byte boundaries are read faster.
+ * d_lse (optional) [n_heads][n_rows] gets the logarithm of each row's sum of
+ * e^score, which the gradient takes.  What a row does not see does not reach
+ * it, NaN included; an infinity among the values that it sees gives an
+ * infinity, or NaN beside another or where its weight is too small for fp32.
+ * A row all of whose scores are -inf gets zeros and -inf.  d_out must not
+ * overlap the inputs.  n_seqs or n_rows = 0 does nothing. */
+jf_status jf_attention_causal(int32_t n_seqs, int32_t n_rows, const int32_t *d_row_start, int32_t n_heads,
+                              int32_t n_kv_heads, int32_t head_dim, int32_t dtype, const void *d_q, int64_t ld_q,
+                              const void *d_k, int64_t ld_k, const void *d_v, int64_t ld_v, void *d_out,
+                              int64_t ld_out, float *d_lse, int32_t *d_flags, jf_stream stream);
+
+/* Gradient of sum(d_g_out * out) to the queries, keys and values, from what
+ * jf_attention_causal was given and gave (d_out, d_lse).  The gradients of
+ * keys and values are sums over the query heads that share them.  All row
+ * tensors are of dtype; the gradients must overlap no input (but may be
+ * columns of one tensor).  Nothing depends on the order in which workgroups
+ * run.  An infinity or NaN among a sequence's inputs may reach every gradient
+ * of that sequence, and none of another's.  d_ws, on a 16-byte boundary,
+ * holds jf_attention_causal_grad_ws_bytes(...) bytes, needs no clearing and
+ * may be shared by calls that do not overlap. */
+size_t jf_attention_causal_grad_ws_bytes(int32_t n_seqs, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads,
+                                         int32_t head_dim);
+jf_status jf_attention_causal_grad(int32_t n_seqs, int32_t n_rows, const int32_t *d_row_start, int32_t n_heads,
+                                   int32_t n_kv_heads, int32_t head_dim, int32_t dtype, const void *d_q, int64_t ld_q,
+                                   const void *d_k, int64_t ld_k, const void *d_v, int64_t ld_v, const void *d_out,
+                                   int64_t ld_out, const float *d_lse, const void *d_g_out, int64_t ld_g_out,
+                                   void *d_g_q, int64_t ld_g_q, void *d_g_k, int64_t ld_g_k, void *d_g_v,
+                                   int64_t ld_g_v, void *d_ws, int32_t *d_flags, jf_stream stream);
+
+/* ---- attention of a batch that shares prefixes --------------------------------
+ * Groups of sequences that follow each other share their first pages: samples
+ * of one prompt, requests behind one system prompt.  Sequences d_seq_start[g]
+ * .. d_seq_start[g + 1] - 1 (device, [n_groups + 1], not decreasing) form
+ * group g, and the first d_pages[g] entries of their rows of the page table
+ * name the same pages (those of the group's first sequence are read).  Only
+ * whole pages of committed tokens are shared: 64 d_pages[g] <= d_ctx of each.
+ * Sequences of no group share nothing.  The host gives bounds: at most
+ * max_rows rows of one group and max_pages (<= table_stride) shared pages.
+ * What the device holds beyond these, or a sequence with fewer committed
+ * tokens than it is said to share, raises JF_FLAG_CAPACITY, and the rows of
+ * such a group or sequence are left as they were. */
+typedef struct {
+  int32_t n_groups, max_rows, max_pages;
+  const int32_t *d_seq_start; /* [n_groups + 1] */
+  const int32_t *d_pages;     /* [n_groups] */
+} jf_prefix;
+
+/* Attention over a cache of dtype JF_F32 or JF_BF16 (the pages of jf_kv_append)
+ * that already holds the rows' keys and values: row i of sequence s sees
+ * slots [0, d_ctx[s]) and in-step slot d_ctx[s] + j iff bit j of
+ * d_vis[row][JF_VIS_WORDS] is set (d_vis NULL: j <= i), as if nothing were
+ * shared; the shared pages are read once for all rows of a group.  A row that
+ * sees nothing gets zeros; what a slot holds does not reach a row that does
+ * not see it, NaN included (an infinity that it sees gives an output that is
+ * not finite).  A page outside the pool raises JF_FLAG_BAD_PAGE and its
+ * slots are seen by nobody.  d_q [n_rows][n_heads][head_dim] and d_out are
+ * activation planes of dtype, d_out in the GEMM-input layout of [n_rows]
+ * [n_heads * head_dim] (a multiple of 128 columns); the batch's max_rows <=
+ * JF_MAX_ROWS.  d_q, d_kv, d_out and d_ws must start on 16-byte boundaries;
+ * d_ws holds jf_attention_shared_ws_bytes(...) bytes (0: the call would be
+ * refused), needs no clearing and may be shared by calls that do not overlap.
+ * prefix NULL: nothing is shared. */
+size_t jf_attention_shared_ws_bytes(const jf_batch *batch, const jf_prefix *prefix, int32_t n_heads,
+                                    int32_t n_kv_heads, int32_t head_dim);
+jf_status jf_attention_shared(const jf_batch *batch, const jf_prefix *prefix, int32_t n_heads, int32_t n_kv_heads,
+                              int32_t head_dim, int32_t dtype, const void *d_q, const void *d_kv,
+                              const uint64_t *d_vis, void *d_out, void *d_ws, int32_t *d_flags, jf_stream stream);
+
+/* ---- policy loss ----------------------------------------------------------------
+ * Clipped policy loss with a KL term over the tokens of sampled sequences, and
+ * its gradient to the log probabilities and entropies of jf_token_logprobs,
+ * as jf_token_logprobs_grad takes it (d_g_logprob, d_g_entropy).
+ * Rows d_row_start[s] .. d_row_start[s + 1] - 1 (device, [n_seqs + 1], not
+ * decreasing) belong to sequence s; a row with d_tokens[row] = -1 (d_tokens
+ * NULL: none) has no token: its gradients are 0 and it counts nowhere.  Rows
+ * outside all sequences are neither read nor written.  For a row with
+ * advantage A (d_advantage[row], or [sequence] for adv_rows 0):
+ *   r = e^(logprob - old), policy = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A), 0 for A = 0
+ *   k = ref - logprob, kl = e^k - k - 1 (d_ref_logprob NULL: 0)
+ *   loss = scale * sum w (policy + kl_weight kl - entropy_weight entropy)   (d_entropy NULL: without it)
+ * with w = 1 / tokens (JF_MEAN_TOKENS), 1 / (sequences with tokens * tokens of
+ * the row's) (JF_MEAN_SEQS) or 1 (JF_SUM).  Clipped rows (A > 0 and r > 1 +
+ * clip_high, or A < 0 and r < 1 - clip_low) have no gradient of the policy
+ * term.  Differences and exponentials are computed in 64 bits; the order of
+ * the sums is fixed.
+ *   d_stats[JF_POLICY_STATS]: the loss, then sum w of policy, kl, entropy and
+ *     clipped rows, then the number of tokens (no tokens: all 0);
+ *   d_g_logprob, d_g_entropy [n_rows] (either may be NULL): the gradient.
+ * Row starts that decrease or lie outside [0, n_rows] raise JF_FLAG_CAPACITY
+ * in d_flags (optional): the statistics are NaN and no gradient is written.
+ * n_seqs or n_rows = 0: statistics 0, no gradient.  n_rows, n_seqs <= 2^22.
+ * d_ws, on a 16-byte boundary, holds jf_policy_loss_ws_bytes(...) bytes, needs
+ * no clearing and may be shared by calls that do not overlap. */
+enum { JF_MEAN_TOKENS = 0, JF_MEAN_SEQS = 1, JF_SUM = 2 };
+#define JF_POLICY_STATS 6
+typedef struct {
+  double clip_low, clip_high;  /* 0 <= clip_low <= 1, clip_high >= 0 (may be infinite) */
+  double kl_weight, entropy_weight, scale;
+  int32_t mean;                /* JF_MEAN_TOKENS, JF_MEAN_SEQS or JF_SUM */
+  int32_t adv_rows;            /* 0: one advantage a sequence, 1: one a row */
+} jf_policy;
+size_t jf_policy_loss_ws_bytes(int32_t n_seqs, int32_t n_rows);
+jf_status jf_policy_loss(const jf_policy *policy, int32_t n_seqs, int32_t n_rows, const int32_t *d_row_start,
+                         const int32_t *d_tokens, const float *d_logprob, const float *d_old_logprob,
+                         const float *d_ref_logprob, const float *d_entropy, const float *d_advantage, float *d_stats,
+                         float *d_g_logprob, float *d_g_entropy, void *d_ws, int32_t *d_flags, jf_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -13,7 +13,8 @@ BUILD = os.path.join(os.path.dirname(HERE), "_build")
 LIB = os.path.join(HERE, "libjf.so")
 SOURCES = ["jf_api.hip", "gemm.hip", "gemm_mr.hip", "gemm_mr_any.hip",
            *(f"gemm_mr_rt{n}.hip" for n in (2, 4, 6, 8, 10, 12, 16)), "attention.hip", "layer.hip", "step.hip",
-           "trajectory.hip", "kvcache.hip", "attention_kv8.hip", "logprobs.hip"]
+           "trajectory.hip", "kvcache.hip", "attention_kv8.hip", "logprobs.hip", "attention_causal.hip", "attention_shared.hip",
+           "policy.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-Wall",

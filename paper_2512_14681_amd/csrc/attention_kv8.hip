@@ -60,25 +60,6 @@ __device__ __forceinline__ void split16(const float* x, float minus_one, f16x8_t
   lo = l.v;
 }
 
-// Low n bits, n clamped to [0, 64].
-__device__ __forceinline__ uint64_t low_bits(int n) { return n >= 64 ? ~0ull : (n <= 0 ? 0ull : (1ull << n) - 1); }
-
-// Bits j0 .. j0 + 63 of what a row sees (j0 > -64): slots before the in-step
-// ones, then those of its mask (causal for vis null), none past the
-// sequence's n rows.
-__device__ __forceinline__ uint64_t seen_bits(const uint64_t* vis, int i, int n, int j0) {
-  uint64_t w;
-  if (vis) {
-    const int k = j0 >> 6, sh = j0 & 63;  // floor: k = -1 for a window that starts before the in-step slots
-    const uint64_t a = k >= 0 && k < kVisWords ? vis[k] : 0, b = k + 1 < kVisWords ? vis[k + 1] : 0;
-    w = sh ? (a >> sh) | (b << (64 - sh)) : a;
-    w &= low_bits(n - j0);
-  } else {
-    w = low_bits(min(i + 1, n) - j0);
-  }
-  return w | low_bits(-j0);
-}
-
 // NaN codes of four bytes, as 0x80 in each.
 __device__ __forceinline__ uint32_t f8_nans(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 

@@ -1,0 +1,457 @@
+// Grouped-query attention of a batch of sequences over a paged fp32 or bf16
+// cache in which groups of sequences share their first pages
+// (jf_attention_shared).
+//
+// The rows of all sequences of a group go over the shared pages together, as
+// one product, and the rows of each sequence over the pages of its own; what
+// the parts give (maximum, sum, weighted values) is merged.  Both kinds of
+// work are in one launch.
+//
+// A wave works on 32 queries (row, head) of one KV head.  Scores come out of
+// the matrix cores transposed (keys x queries), with a page's keys in an
+// order that gives a lane 8 consecutive keys of its query: these weights and
+// 8 consecutive keys of V^T, as the page holds it, are operands of O^T += V^T P^T.
+//
+// Precision: bf16 queries come as two terms (hi and lo) and the weights enter
+// the second product as two, which keeps 16 bits of either; keys and values
+// are exact.  Sums and maxima are fp32.
+#include <algorithm>
+#include <type_traits>
+
+#include "jf_batch.h"
+#include "jf_tile32.h"
+
+namespace jf {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.f;  // weights are 2^(s - m), m the row's maximum or up to this below it
+constexpr int kChunk = 4;      // pages of a part at least
+
+// Queries as operands: bf16 in two terms.
+template <typename T> struct Query;
+template <> struct Query<bf16_t> { Frag<bf16_t> hi, lo; };
+template <> struct Query<float> { Frag<float> v; };
+__device__ __forceinline__ void load_query(const bf16_t* p, size_t plane, Query<bf16_t>& q) {
+  q.hi = frag_load<bf16_t>(p);
+  q.lo = frag_load<bf16_t>(p + plane);
+}
+__device__ __forceinline__ void load_query(const float* p, size_t, Query<float>& q) { q.v = frag_load<float>(p); }
+__device__ __forceinline__ void split_query(const float* x, Query<bf16_t>& q) {
+  split2(x[0], x[1], q.hi.v.x, q.lo.v.x);
+  split2(x[2], x[3], q.hi.v.y, q.lo.v.y);
+  split2(x[4], x[5], q.hi.v.z, q.lo.v.z);
+  split2(x[6], x[7], q.hi.v.w, q.lo.v.w);
+}
+__device__ __forceinline__ void split_query(const float* x, Query<float>& q) { frag_of(x, q.v); }
+__device__ __forceinline__ void mul(f32x16_t& acc, const Frag<bf16_t>& a, const Query<bf16_t>& b) {
+  mfma32(acc, a, b.hi);
+  mfma32(acc, a, b.lo);
+}
+__device__ __forceinline__ void mul(f32x16_t& acc, const Frag<float>& a, const Query<float>& b) { mfma32(acc, a, b.v); }
+
+// What a sequence shares: the first `pages` pages, if its group is what the
+// host announced (else false, with JF_FLAG_CAPACITY raised).
+__device__ __forceinline__ bool group_ok(const SharedArgs& a, int s0, int s1, int pages) {
+  if (s0 < 0 || s1 < s0 || s1 > a.b.n_seqs || pages < 0 || pages > a.max_pages) return false;
+  const int r0 = a.b.row_start[s0], r1 = a.b.row_start[s1];
+  return r0 >= 0 && r1 >= r0 && r1 <= a.b.n_rows && r1 - r0 <= a.max_group_rows;
+}
+__device__ __forceinline__ bool shared_pages(const SharedArgs& a, int s, const Seq& q, int& pages) {
+  const int lane = threadIdx.x & 63;
+  pages = 0;
+  bool ok = true;
+  for (int g0 = 0; g0 < a.n_groups; g0 += 64) {
+    const int g = g0 + lane;
+    const int s0 = g < a.n_groups ? a.seq_start[g] : 0, s1 = g < a.n_groups ? a.seq_start[g + 1] : 0;
+    const uint64_t hit = __ballot(s0 <= s && s < s1);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      pages = a.pages[g0 + l];
+      ok = group_ok(a, __builtin_amdgcn_readlane(s0, l), __builtin_amdgcn_readlane(s1, l), pages) && pages <= q.C / kPage;
+      break;
+    }
+  }
+  if (!ok && a.b.flags && threadIdx.x == 0) atomicOr(a.b.flags, kFlagCapacity);
+  return ok;
+}
+// Pages of a part, when `splits` parts at most share n pages.
+__device__ __forceinline__ int part_pages(int n, int splits) {
+  return max((n + splits - 1) / max(splits, 1), kChunk);
+}
+
+}  // namespace
+
+// A wave's 32 queries of KV head g: query j is row j / grp, head j % grp of
+// the group's.  Lane l holds query l % 32.
+template <typename T, int HD> struct SharedTile {
+  static constexpr int NS = HD / 16, ND = HD / 32;
+  Query<T> q[NS];
+  int qi, qhd;    // the lane's query: row among the job's, head
+  bool valid;
+  float m, l;
+  f32x16_t o[ND];
+
+  __device__ __forceinline__ void init(const SharedArgs& a, int r0, int n, int g, int tile) {
+    const int grp = a.H / a.G, nq = grp * n, lane = threadIdx.x & 63;
+    const int j0 = tile * 32 + (lane & 31), j = min(j0, nq - 1);
+    valid = j0 < nq;
+    qi = j / grp;
+    qhd = g * grp + j - qi * grp;
+    const T* p = reinterpret_cast<const T*>(a.q) + ((size_t)(r0 + qi) * a.H + qhd) * HD + 8 * (lane >> 5);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) load_query(p + 16 * s, a.q_plane, q[s]);
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) o[d] = zero16();
+  }
+
+  // 32 KT keys in LDS (their rows in the order of key_row) and V^T beside
+  // them.  kEdge: seen holds a bit for each that the lane's query sees.
+  template <int KT, bool kEdge>
+  __device__ __forceinline__ void step(const char* keys, const char* values, uint64_t seen) {
+    using Keys = RowTile<T, HD>;
+    using Values = RowTile<T, 32 * KT>;
+    const float c = kLog2e / sqrtf((float)HD);
+    f32x16_t st[KT];
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+      st[kt] = zero16();
+#pragma unroll
+      for (int s = 0; s < NS; ++s) mul(st[kt], Keys::rows(keys, 32 * kt, s), q[s]);
+    }
+    seen >>= 8 * ((threadIdx.x & 63) >> 5);
+    const uint32_t bits[2] = {(uint32_t)seen, (uint32_t)(seen >> 32)};
+    if constexpr (kEdge) {
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[kt][i] = (bits[kt] >> (16 * (i / 8) + i % 8)) & 1 ? st[kt][i] : -INFINITY;
+    }
+    float mx = st[0][0];
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[kt][i]);
+    mx = pair_max(mx) * c;
+    if (__any(mx > m + kSlack)) {
+      const float m_new = fmaxf(m, mx);
+      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] *= alpha;
+    }
+    const float off = m == -INFINITY ? 0.f : -m;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        st[kt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][i], c, off));
+        l += st[kt][i];
+      }
+    bool finite = true;
+    if constexpr (kEdge) {  // 0 times a value that is not finite would reach rows that do not see it
+      uint32_t top = 0;
+#pragma unroll
+      for (int j = 0; j < 2 * KT; ++j)
+#pragma unroll
+        for (int d = 0; d < ND; ++d) magnitude(Values::rows(values, 32 * d, j), top);
+      finite = !__any(!all_finite<T>(top));
+    }
+#pragma unroll
+    for (int j = 0; j < 2 * KT; ++j) {
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = st[j / 2][8 * (j % 2) + e];
+      Query<T> pf;
+      split_query(p, pf);
+      if (!kEdge || finite) {
+#pragma unroll
+        for (int d = 0; d < ND; ++d) mul(o[d], Values::rows(values, 32 * d, j), pf);
+      } else {
+        Frag<T> clean, up, down, sees;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = (bits[j / 2] >> (16 * (j % 2) + e)) & 1 ? 1.f : 0.f;
+        frag_of(p, sees);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          part_finite(Values::rows(values, 32 * d, j), clean, up, down);
+          mul(o[d], clean, pf);
+          add_infinite<T>(o[d], up, down, sees);
+        }
+      }
+    }
+  }
+};
+
+// Brings 32 KT keys of a page from token t0 on, and their V^T, into LDS, by W
+// waves of which this is number `wave`.  LDS row r of the keys holds the key
+// with bits 2 and 3 of r exchanged: a result's elements 8 j .. + 7 of lane l
+// then are keys 16 j + 8 (l / 32) .. + 7.
+template <typename T, int HD, int KT, int W> struct PageLoader {
+  static __device__ __forceinline__ void load(const T* keys, const T* values, int t0, int wave, char* tile) {
+    constexpr int kKeyRow = HD * (int)sizeof(T), kValueRow = 32 * KT * (int)sizeof(T);
+    constexpr int kPieces = 32 * KT * kKeyRow / 1024 / W;
+    const int lane = threadIdx.x & 63;
+    const uint32_t at = lds_address(tile);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int o = (i * W + wave) * 1024 + lane * 16, r = o / kKeyRow;
+      const int c = (o % kKeyRow / 16) ^ turn<kKeyRow>(r), key = (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1);
+      dma_1k<false>(reinterpret_cast<const char*>(keys + (size_t)t0 * HD), key * kKeyRow + c * 16, at + (i * W + wave) * 1024);
+    }
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int o = (i * W + wave) * 1024 + lane * 16, r = o / kValueRow;
+      const int c = (o % kValueRow / 16) ^ turn<kValueRow>(r);
+      dma_1k<false>(reinterpret_cast<const char*>(values + t0), r * kPage * (int)sizeof(T) + c * 16,
+                    at + 32 * KT * kKeyRow + (i * W + wave) * 1024);
+    }
+  }
+};
+
+// Four outputs of a query: the result, or a part of it.
+template <typename T>
+__device__ __forceinline__ void put_outputs(const SharedArgs& a, int row, int head, int part, int dim, float m, float l,
+                                            float (&v)[4]) {
+  if (part < 0) {
+    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = inv == 0.f ? 0.f : v[i] * inv;
+    act_store4(reinterpret_cast<T*>(a.out) + act_offset(row, head * a.hd + dim, a.H * a.hd), a.out_plane, v);
+  } else {
+    const size_t at = ((size_t)part * a.b.n_rows + row) * a.H + head;
+    *reinterpret_cast<float4*>(a.o_part + at * a.hd + dim) = make_float4(v[0], v[1], v[2], v[3]);
+    if (dim == 0) *reinterpret_cast<float2*>(a.ml_part + at * 2) = make_float2(m, l);
+  }
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_shared(SharedArgs a) {
+  using Tile = SharedTile<T, HD>;
+  constexpr int KT = sizeof(T) == 2 ? 2 : 1, ND = HD / 32;
+  constexpr int kOne = 2 * 32 * HD * (int)sizeof(T);   // 32 keys and their values
+  constexpr int kBytes = std::max({4 * kOne, 2 * KT * kOne, 4 * 32 * HD * 4});
+  __shared__ __align__(1024) char s_kv[kBytes];
+  __shared__ float s_ml[4][2][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
+  // The jobs: shared pages first.
+  const bool shared = (int)blockIdx.x < a.shared_jobs;
+  int job = shared ? blockIdx.x : blockIdx.x - a.shared_jobs;
+  const int splits = shared ? a.shared_splits : a.own_splits, groups = shared ? a.shared_groups : a.own_groups;
+  const int g = job % a.G, split = job / a.G % splits, group = job / (a.G * splits) % groups;
+  const int unit = job / (a.G * splits * groups);
+  int r0, n, p0, p1, part;
+  const int32_t* table;
+  Seq q{};
+  if (shared) {
+    const int s0 = a.seq_start[unit], s1 = a.seq_start[unit + 1], pages = a.pages[unit];
+    if (!group_ok(a, s0, s1, pages)) {
+      if (a.b.flags && threadIdx.x == 0) atomicOr(a.b.flags, kFlagCapacity);
+      return;
+    }
+    if (s0 == s1) return;
+    r0 = a.b.row_start[s0];
+    n = a.b.row_start[s1] - r0;
+    table = a.b.table + (size_t)s0 * a.b.stride;
+    const int chunk = part_pages(pages, splits);
+    p0 = split * chunk;
+    p1 = min(p0 + chunk, pages);
+    part = split;
+  } else {
+    int pages;
+    if (!batch_seq(a.b, unit, q) || !shared_pages(a, unit, q, pages)) return;
+    r0 = q.r0;
+    n = q.n;
+    table = q.table;
+    const int end = (q.C + q.n + kPage - 1) / kPage, chunk = part_pages(end - pages, splits);
+    p0 = pages + split * chunk;
+    p1 = min(p0 + chunk, end);
+    part = a.parts == 1 ? -1 : a.shared_splits + split;
+  }
+  const int nq = a.H / a.G * n;
+  const bool few = shared ? a.shared_few : a.own_few;
+  if (p0 >= p1 || group * (few ? 32 : 128) >= nq) return;
+  const int whole = shared ? p1 : max(min(q.C / kPage, p1), p0);   // pages below are seen by all
+  const T* pool = reinterpret_cast<const T*>(a.kv);
+  const size_t page_elems = (size_t)2 * a.G * kPage * HD;
+  // slots of page p that the lane's query sees
+  auto seen = [&](const Tile& w, int p) {
+    return seen_bits(a.vis ? a.vis + (size_t)(r0 + w.qi) * kVisWords : nullptr, w.qi, n, p * kPage - q.C);
+  };
+  Tile w;
+  if (few) {
+    // One tile: the waves take every fourth page, each in LDS of its own.
+    w.init(a, r0, n, g, group);
+    char* mine = s_kv + wave * kOne;
+    auto page = [&](auto edge, int p) {
+      const int id = batch_page_id(a.b, table[p]);
+      if (id < 0) return;
+      const T* keys = pool + (size_t)id * page_elems + (size_t)g * kPage * HD;
+      uint64_t bits = 0;
+      if constexpr (decltype(edge)::value) bits = seen(w, p);
+#pragma unroll 1
+      for (int t0 = 0; t0 < kPage; t0 += 32) {
+        PageLoader<T, HD, 1, 1>::load(keys, keys + (size_t)a.G * kPage * HD, t0, 0, mine);
+        wait_vm<0>();
+        w.template step<1, decltype(edge)::value>(mine, mine + kOne / 2, bits >> t0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the next load takes the place of what was read
+      }
+    };
+    int p = p0 + wave;
+#pragma unroll 1
+    for (; p < whole; p += 4) page(std::false_type{}, p);
+#pragma unroll 1
+    for (; p < p1; p += 4) page(std::true_type{}, p);
+    // The waves' parts, dims by queries; each wave merges a quarter of the dims.
+    w.l = pair_sum(w.l);
+    __syncthreads();
+    float* s_o = reinterpret_cast<float*>(s_kv);
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s_o[(wave * HD + 32 * d + acc_row(i) + 4 * h) * 32 + (lane & 31)] = w.o[d][i];
+    if (h == 0) {
+      s_ml[wave][0][lane] = w.m;
+      s_ml[wave][1][lane] = w.l;
+    }
+    __syncthreads();
+    if (!w.valid) return;
+    float m = -INFINITY, l = 0.f, f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = fmaxf(m, s_ml[i][0][lane & 31]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[i] = s_ml[i][0][lane & 31] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_ml[i][0][lane & 31] - m);
+      l += s_ml[i][1][lane & 31] * f[i];
+    }
+#pragma unroll
+    for (int k = 0; k < HD / 32; ++k) {
+      const int dim = wave * (HD / 4) + 8 * k + 4 * h;
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += f[i] * s_o[(i * HD + dim + e) * 32 + (lane & 31)];
+      put_outputs<T>(a, r0 + w.qi, w.qhd, part, dim, m, l, v);
+    }
+    return;
+  }
+  // Four tiles, one a wave, over pages that all share.
+  constexpr int kStep = 32 * KT, kTile = KT * kOne, kPerPage = kPage / kStep;
+  w.init(a, r0, n, g, group * 4 + wave);
+  const bool work = (group * 4 + wave) * 32 < nq;
+  auto entry = [&](int p) { return batch_page_id(a.b, __builtin_amdgcn_readfirstlane(table[p])); };
+  auto load = [&](int id, int t0, int buf) {
+    const T* keys = pool + (size_t)max(id, 0) * page_elems + (size_t)g * kPage * HD;
+    PageLoader<T, HD, KT, 4>::load(keys, keys + (size_t)a.G * kPage * HD, t0, wave, s_kv + buf * kTile);
+  };
+  int id = entry(p0), buf = 0;
+  load(id, 0, 0);
+  auto page = [&](auto edge, int p) {
+    const int next = p + 1 < p1 ? entry(p + 1) : -1;
+    uint64_t bits = 0;
+    if constexpr (decltype(edge)::value) bits = seen(w, p);
+#pragma unroll
+    for (int t = 0; t < kPerPage; ++t) {
+      wait_vm<0>();
+      __syncthreads();
+      if (t + 1 < kPerPage) load(id, (t + 1) * kStep, buf ^ 1);
+      else if (p + 1 < p1) load(next, 0, buf ^ 1);
+      if (work && id >= 0)
+        w.template step<KT, decltype(edge)::value>(s_kv + buf * kTile, s_kv + buf * kTile + kTile / 2, bits >> (t * kStep));
+      buf ^= 1;
+    }
+    id = next;
+  };
+  int p = p0;
+#pragma unroll 1
+  for (; p < whole; ++p) page(std::false_type{}, p);
+#pragma unroll 1
+  for (; p < p1; ++p) page(std::true_type{}, p);
+  if (!w.valid) return;
+  w.l = pair_sum(w.l);
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      float v[4] = {w.o[d][i], w.o[d][i + 1], w.o[d][i + 2], w.o[d][i + 3]};
+      put_outputs<T>(a, r0 + w.qi, w.qhd, part, 32 * d + acc_row(i) + 4 * h, w.m, w.l, v);
+    }
+}
+
+// Merges a row's parts in order, four dims of one row and head a thread.
+template <typename T>
+__global__ void __launch_bounds__(256) k_attention_shared_merge(SharedArgs a, int blocks) {
+  const int s = blockIdx.x / blocks;
+  Seq q;
+  int pages;
+  if (!batch_seq(a.b, s, q) || !shared_pages(a, s, q, pages)) return;
+  const int chunks = a.hd / 4, item = (blockIdx.x % blocks * 256 + threadIdx.x) / chunks, dim = threadIdx.x % chunks * 4;
+  if (item >= q.n * a.H) return;
+  const int head = item % a.H, row = q.r0 + item / a.H;
+  const int own = (q.C + q.n + kPage - 1) / kPage - pages;
+  const int c0 = part_pages(pages, a.shared_splits), c1 = part_pages(own, a.own_splits);
+  const int n0 = (pages + c0 - 1) / c0, n1 = (own + c1 - 1) / c1;
+  const size_t stride = (size_t)a.b.n_rows * a.H, at = (size_t)row * a.H + head;
+  float m = -INFINITY;
+  for (int i = 0; i < n0 + n1; ++i) m = fmaxf(m, a.ml_part[((i < n0 ? i : a.shared_splits + i - n0) * stride + at) * 2]);
+  float l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < n0 + n1; ++i) {
+    const size_t k = (i < n0 ? i : a.shared_splits + i - n0) * stride + at;
+    const float2 ml = *reinterpret_cast<const float2*>(a.ml_part + k * 2);
+    const float4 o = *reinterpret_cast<const float4*>(a.o_part + k * a.hd + dim);
+    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+    l += ml.y * f;
+    v[0] += o.x * f; v[1] += o.y * f; v[2] += o.z * f; v[3] += o.w * f;
+  }
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = inv == 0.f ? 0.f : v[e] * inv;
+  act_store4(reinterpret_cast<T*>(a.out) + act_offset(row, head * a.hd + dim, a.H * a.hd), a.out_plane, v);
+}
+
+// ---- launch --------------------------------------------------------------------------
+// Workgroups of two a compute unit, in parts of kChunk pages or more; how
+// many pages there are to split is known on the device.
+void shared_plan(SharedArgs& a) {
+  const int grp = a.H / a.G;
+  auto tiles = [&](int64_t rows) { return (int)((rows * grp + 31) / 32); };
+  const bool prefix = a.n_groups > 0 && a.max_pages > 0 && a.max_group_rows > 0;
+  const int ts = prefix ? tiles(a.max_group_rows) : 0, to = tiles(a.b.max_rows);
+  a.shared_few = ts <= 1;
+  a.own_few = to <= 1;
+  a.shared_groups = a.shared_few ? 1 : (ts + 3) / 4;
+  a.own_groups = a.own_few ? 1 : (to + 3) / 4;
+  auto splits = [&](int64_t base, int pages) {
+    const int64_t want = (512 + base - 1) / base, most = (pages + kChunk - 1) / kChunk;
+    return (int)std::max<int64_t>(std::min<int64_t>({want, most, 64}), 1);
+  };
+  a.shared_splits = prefix ? splits((int64_t)a.n_groups * a.G * a.shared_groups, a.max_pages) : 0;
+  a.own_splits = splits((int64_t)a.b.n_seqs * a.G * a.own_groups, (a.b.max_ctx + kPage - 1) / kPage);
+  a.parts = a.shared_splits + a.own_splits;
+  a.shared_jobs64 = prefix ? (int64_t)a.n_groups * a.G * a.shared_groups * a.shared_splits : 0;
+  a.own_jobs64 = (int64_t)a.b.n_seqs * a.G * a.own_groups * a.own_splits;
+  if (!prefix) a.shared_splits = 0;
+}
+
+template <typename T> static hipError_t shared_type(const SharedArgs& a, hipStream_t st) {
+  const unsigned jobs = (unsigned)(a.shared_jobs64 + a.own_jobs64);
+  if (a.hd == 32) k_attention_shared<T, 32><<<jobs, 256, 0, st>>>(a);
+  else if (a.hd == 64) k_attention_shared<T, 64><<<jobs, 256, 0, st>>>(a);
+  else k_attention_shared<T, 128><<<jobs, 256, 0, st>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.parts == 1) return e;
+  const int per = 256 / (a.hd / 4), blocks = (a.b.max_rows * a.H + per - 1) / per;
+  k_attention_shared_merge<T><<<(unsigned)(a.b.n_seqs * blocks), 256, 0, st>>>(a, blocks);
+  return hipGetLastError();
+}
+hipError_t launch_attention_shared(int dtype, SharedArgs& a, hipStream_t st) {
+  a.shared_jobs = (int)a.shared_jobs64;
+  return dtype == 0 ? shared_type<float>(a, st) : shared_type<bf16_t>(a, st);
+}
+
+}  // namespace jf

@@ -1173,3 +1173,213 @@ extern "C" jf_status jf_token_logprobs_grad(int32_t R, int32_t V, int32_t dtype,
   HIP_TRY(launch_logprobs_grad(dtype, a, (hipStream_t)stream));
   return JF_OK;
 }
+
+// ---- causal attention over packed sequences ----------------------------------------------
+// Whether the rows (and so every eight elements from a multiple of eight) start on 16-byte boundaries.
+static bool rows16(const void* p, int64_t ld, size_t esz) { return aligned16(p) && ld * (int64_t)esz % 16 == 0; }
+
+static jf_status check_causal(int n_seqs, int n_rows, const int32_t* d_row_start, int n_heads, int n_kv_heads,
+                              int head_dim, int dtype, bool* none) {
+  if (dtype != JF_F32 && dtype != JF_BF16) return fail(JF_E_DTYPE, "dtype %d unsupported", dtype);
+  if (n_seqs < 0 || n_rows < 0) return fail(JF_E_INVAL, "negative count");
+  if (n_heads < 1 || n_kv_heads < 1 || n_heads > 65536 || n_heads % n_kv_heads)
+    return fail(JF_E_SHAPE, "bad head counts %d, %d", n_heads, n_kv_heads);
+  if (!head_dim_ok(head_dim)) return fail(JF_E_SHAPE, "head_dim must be 32, 64 or 128");
+  if (n_rows > (1 << 30)) return fail(JF_E_CAPACITY, "n_rows goes up to 2^30");
+  *none = n_seqs == 0 || n_rows == 0;
+  if (*none) return JF_OK;
+  if (!d_row_start) return fail(JF_E_INVAL, "null pointer argument");
+  if (((int64_t)causal_blocks(n_rows, n_seqs) + 8) * n_heads > kMaxBlocks ||
+      ((int64_t)n_rows * n_heads * (head_dim / 8) + 255) / 256 > 4 * kMaxBlocks)
+    return fail(JF_E_CAPACITY, "%d rows of %d heads exceed one launch", n_rows, n_heads);
+  return JF_OK;
+}
+static void causal_args(CausalArgs* a, int n_seqs, int n_rows, const int32_t* d_row_start, int n_heads, int n_kv_heads,
+                        int head_dim, size_t esz, const void* d_q, int64_t ld_q, const void* d_k, int64_t ld_k,
+                        const void* d_v, int64_t ld_v, void* d_out, int64_t ld_out, float* d_lse, int32_t* d_flags) {
+  a->n_seqs = n_seqs; a->n_rows = n_rows; a->H = n_heads; a->G = n_kv_heads; a->hd = head_dim;
+  a->row_start = d_row_start;
+  a->flags = d_flags;
+  a->q = d_q; a->k = d_k; a->v = d_v;
+  a->ld_q = (size_t)ld_q; a->ld_k = (size_t)ld_k; a->ld_v = (size_t)ld_v;
+  constexpr int64_t kMostStride = 1 << 22;  // 64 rows stay within 32-bit offsets
+  a->vec = rows16(d_q, ld_q, esz) && rows16(d_k, ld_k, esz) && rows16(d_v, ld_v, esz) && ld_q <= kMostStride &&
+           ld_k <= kMostStride && ld_v <= kMostStride;
+  a->out = d_out; a->ld_out = (size_t)ld_out;
+  a->vec_out = vector4(d_out, ld_out, esz);
+  a->lse = d_lse;
+  a->blocks = causal_blocks(n_rows, n_seqs);
+}
+
+extern "C" jf_status jf_attention_causal(int32_t n_seqs, int32_t n_rows, const int32_t* d_row_start, int32_t n_heads,
+                                         int32_t n_kv_heads, int32_t head_dim, int32_t dtype, const void* d_q,
+                                         int64_t ld_q, const void* d_k, int64_t ld_k, const void* d_v, int64_t ld_v,
+                                         void* d_out, int64_t ld_out, float* d_lse, int32_t* d_flags,
+                                         jf_stream stream) {
+  bool none = false;
+  const jf_status s = check_causal(n_seqs, n_rows, d_row_start, n_heads, n_kv_heads, head_dim, dtype, &none);
+  if (s != JF_OK || none) return s;
+  if (!d_q || !d_k || !d_v || !d_out) return fail(JF_E_INVAL, "null pointer argument");
+  const int64_t wq = (int64_t)n_heads * head_dim, wk = (int64_t)n_kv_heads * head_dim;
+  if (ld_q < wq || ld_out < wq || ld_k < wk || ld_v < wk) return fail(JF_E_SHAPE, "row strides are shorter than the rows");
+  CausalArgs a{};
+  causal_args(&a, n_seqs, n_rows, d_row_start, n_heads, n_kv_heads, head_dim, dtype == JF_BF16 ? 2 : 4, d_q, ld_q, d_k,
+              ld_k, d_v, ld_v, d_out, ld_out, d_lse, d_flags);
+  HIP_TRY(launch_causal(dtype, a, (hipStream_t)stream));
+  return JF_OK;
+}
+
+// The rows' statistics, then the parts of the keys' and values' gradients.
+static size_t causal_dots_bytes(int n_rows, int n_heads) { return ((size_t)n_rows * n_heads * 8 + 15) / 16 * 16; }
+
+extern "C" size_t jf_attention_causal_grad_ws_bytes(int32_t n_seqs, int32_t n_rows, int32_t n_heads,
+                                                    int32_t n_kv_heads, int32_t head_dim) {
+  bool none = false;
+  static const int32_t some = 0;
+  if (check_causal(n_seqs, n_rows, &some, n_heads, n_kv_heads, head_dim, JF_F32, &none) != JF_OK) return 0;
+  if (none) return 256;
+  const int parts = causal_parts(n_rows, n_seqs, n_heads, n_kv_heads);
+  const size_t part = parts > 1 ? (size_t)2 * parts * n_rows * n_kv_heads * head_dim * 4 : 0;
+  return causal_dots_bytes(n_rows, n_heads) + part + 256;
+}
+
+extern "C" jf_status jf_attention_causal_grad(int32_t n_seqs, int32_t n_rows, const int32_t* d_row_start,
+                                              int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                              const void* d_q, int64_t ld_q, const void* d_k, int64_t ld_k,
+                                              const void* d_v, int64_t ld_v, const void* d_out, int64_t ld_out,
+                                              const float* d_lse, const void* d_g_out, int64_t ld_g_out, void* d_g_q,
+                                              int64_t ld_g_q, void* d_g_k, int64_t ld_g_k, void* d_g_v, int64_t ld_g_v,
+                                              void* d_ws, int32_t* d_flags, jf_stream stream) {
+  bool none = false;
+  const jf_status s = check_causal(n_seqs, n_rows, d_row_start, n_heads, n_kv_heads, head_dim, dtype, &none);
+  if (s != JF_OK || none) return s;
+  if (!d_q || !d_k || !d_v || !d_out || !d_lse || !d_g_out || !d_g_q || !d_g_k || !d_g_v || !d_ws)
+    return fail(JF_E_INVAL, "null pointer argument");
+  if (!aligned16(d_ws)) return fail(JF_E_INVAL, "d_ws must start on a 16-byte boundary");
+  const int64_t wq = (int64_t)n_heads * head_dim, wk = (int64_t)n_kv_heads * head_dim;
+  if (ld_q < wq || ld_out < wq || ld_g_out < wq || ld_g_q < wq || ld_k < wk || ld_v < wk || ld_g_k < wk || ld_g_v < wk)
+    return fail(JF_E_SHAPE, "row strides are shorter than the rows");
+  const size_t esz = dtype == JF_BF16 ? 2 : 4;
+  CausalGradArgs a{};
+  causal_args(&a.f, n_seqs, n_rows, d_row_start, n_heads, n_kv_heads, head_dim, esz, d_q, ld_q, d_k, ld_k, d_v, ld_v,
+              const_cast<void*>(d_out), ld_out, const_cast<float*>(d_lse), d_flags);
+  a.f.vec = a.f.vec && rows16(d_g_out, ld_g_out, esz) && ld_g_out <= (1 << 22);
+  a.vec_dot = rows16(d_out, ld_out, esz) && rows16(d_g_out, ld_g_out, esz);
+  a.g_out = d_g_out; a.ld_g_out = (size_t)ld_g_out;
+  a.g_q = d_g_q; a.g_k = d_g_k; a.g_v = d_g_v;
+  a.ld_g_q = (size_t)ld_g_q; a.ld_g_k = (size_t)ld_g_k; a.ld_g_v = (size_t)ld_g_v;
+  a.vec_q = vector4(d_g_q, ld_g_q, esz);
+  a.vec_kv = vector4(d_g_k, ld_g_k, esz) && vector4(d_g_v, ld_g_v, esz);
+  a.dots = (float2*)d_ws;
+  a.kv_part = (float*)((char*)d_ws + causal_dots_bytes(n_rows, n_heads));
+  a.parts = causal_parts(n_rows, n_seqs, n_heads, n_kv_heads);
+  HIP_TRY(launch_causal_grad(dtype, a, (hipStream_t)stream));
+  return JF_OK;
+}
+
+// ---- attention of a batch that shares prefixes -------------------------------------------
+static jf_status shared_args(const jf_batch* batch, const jf_prefix* prefix, int n_heads, int n_kv_heads, int head_dim,
+                             int32_t* d_flags, SharedArgs* a, bool* none) {
+  jf_status s = check_batch(batch, n_heads, n_kv_heads, head_dim, d_flags, &a->b, none);
+  if (s != JF_OK) return s;
+  if ((int64_t)n_heads * head_dim % 128) return fail(JF_E_SHAPE, "n_heads * head_dim must be a multiple of 128");
+  if (batch->max_rows > kMaxRows) return fail(JF_E_CAPACITY, "max_rows must be at most %d", kMaxRows);
+  if (prefix) {
+    if (prefix->n_groups < 0 || prefix->max_rows < 0 || prefix->max_pages < 0)
+      return fail(JF_E_INVAL, "negative count in the prefix");
+    if (prefix->max_pages > batch->table_stride)
+      return fail(JF_E_CAPACITY, "max_pages %d exceeds table_stride %d", prefix->max_pages, batch->table_stride);
+    if (!*none && prefix->n_groups > 0 && (!prefix->d_seq_start || !prefix->d_pages))
+      return fail(JF_E_INVAL, "null array in the prefix");
+    a->n_groups = prefix->n_groups;
+    a->max_group_rows = std::min(prefix->max_rows, batch->n_rows);
+    a->max_pages = prefix->max_pages;
+    a->seq_start = prefix->d_seq_start;
+    a->pages = prefix->d_pages;
+  }
+  if (*none) return JF_OK;
+  a->H = n_heads; a->G = n_kv_heads; a->hd = head_dim;
+  shared_plan(*a);
+  if (a->shared_jobs64 > kMaxBlocks || a->shared_jobs64 + a->own_jobs64 > kMaxBlocks)
+    return fail(JF_E_CAPACITY, "the batch's workgroups exceed the %lld of a launch", (long long)kMaxBlocks);
+  return check_blocks(((int64_t)batch->max_rows * n_heads * (head_dim / 4) + 255) / 256, batch->n_seqs);
+}
+
+// Parts' outputs, then (max, sum).
+static size_t shared_part_rows(const SharedArgs& a) { return (size_t)a.parts * a.b.n_rows * a.H; }
+
+extern "C" size_t jf_attention_shared_ws_bytes(const jf_batch* batch, const jf_prefix* prefix, int32_t n_heads,
+                                               int32_t n_kv_heads, int32_t head_dim) {
+  SharedArgs a{};
+  bool none = false;
+  if (shared_args(batch, prefix, n_heads, n_kv_heads, head_dim, nullptr, &a, &none) != JF_OK) return 0;
+  if (none || a.parts == 1) return 256;
+  return shared_part_rows(a) * (head_dim + 2) * 4 + 256;
+}
+
+extern "C" jf_status jf_attention_shared(const jf_batch* batch, const jf_prefix* prefix, int32_t n_heads,
+                                         int32_t n_kv_heads, int32_t head_dim, int32_t dtype, const void* d_q,
+                                         const void* d_kv, const uint64_t* d_vis, void* d_out, void* d_ws,
+                                         int32_t* d_flags, jf_stream stream) {
+  if (dtype != JF_F32 && dtype != JF_BF16) return fail(JF_E_DTYPE, "dtype %d unsupported", dtype);
+  SharedArgs a{};
+  bool none = false;
+  const jf_status s = shared_args(batch, prefix, n_heads, n_kv_heads, head_dim, d_flags, &a, &none);
+  if (s != JF_OK || none) return s;
+  if (!d_q || !d_kv || !d_out || !d_ws) return fail(JF_E_INVAL, "null pointer argument");
+  if (!aligned16(d_q) || !aligned16(d_kv) || !aligned16(d_out) || !aligned16(d_ws))
+    return fail(JF_E_INVAL, "d_q, d_kv, d_out and d_ws must start on 16-byte boundaries");
+  a.q = d_q;
+  a.q_plane = (size_t)batch->n_rows * n_heads * head_dim;
+  a.kv = d_kv;
+  a.vis = d_vis;
+  a.out = d_out;
+  a.out_plane = (size_t)(batch->n_rows + 15) / 16 * 16 * n_heads * head_dim;
+  a.o_part = (float*)d_ws;
+  a.ml_part = a.o_part + shared_part_rows(a) * head_dim;
+  HIP_TRY(launch_attention_shared(dtype, a, (hipStream_t)stream));
+  return JF_OK;
+}
+
+// ---- policy loss -------------------------------------------------------------------------
+static jf_status check_policy(int n_seqs, int n_rows) {
+  if (n_seqs < 0 || n_rows < 0) return fail(JF_E_INVAL, "negative count");
+  if (n_seqs > (1 << 22) || n_rows > (1 << 22)) return fail(JF_E_CAPACITY, "n_seqs and n_rows go up to 2^22");
+  return JF_OK;
+}
+extern "C" size_t jf_policy_loss_ws_bytes(int32_t n_seqs, int32_t n_rows) {
+  return check_policy(n_seqs, n_rows) == JF_OK ? policy_ws_bytes(n_seqs, n_rows) + 256 : 0;
+}
+
+extern "C" jf_status jf_policy_loss(const jf_policy* policy, int32_t n_seqs, int32_t n_rows,
+                                    const int32_t* d_row_start, const int32_t* d_tokens, const float* d_logprob,
+                                    const float* d_old_logprob, const float* d_ref_logprob, const float* d_entropy,
+                                    const float* d_advantage, float* d_stats, float* d_g_logprob, float* d_g_entropy,
+                                    void* d_ws, int32_t* d_flags, jf_stream stream) {
+  if (!policy) return fail(JF_E_INVAL, "policy is null");
+  const jf_status s = check_policy(n_seqs, n_rows);
+  if (s != JF_OK) return s;
+  if (!(policy->clip_low >= 0.0 && policy->clip_low <= 1.0 && policy->clip_high >= 0.0))
+    return fail(JF_E_INVAL, "need 0 <= clip_low <= 1 and clip_high >= 0");
+  if (!std::isfinite(policy->kl_weight) || !std::isfinite(policy->entropy_weight) || !std::isfinite(policy->scale))
+    return fail(JF_E_INVAL, "weights and scale must be finite");
+  if (policy->mean != JF_MEAN_TOKENS && policy->mean != JF_MEAN_SEQS && policy->mean != JF_SUM)
+    return fail(JF_E_INVAL, "unknown mean %d", policy->mean);
+  if (policy->adv_rows != 0 && policy->adv_rows != 1) return fail(JF_E_INVAL, "adv_rows is 0 or 1");
+  if (!d_stats || !d_ws) return fail(JF_E_INVAL, "null pointer argument");
+  if (!aligned16(d_ws)) return fail(JF_E_INVAL, "d_ws must start on a 16-byte boundary");
+  const bool none = n_seqs == 0 || n_rows == 0;
+  if (!none && (!d_row_start || !d_logprob || !d_old_logprob || !d_advantage || (d_g_entropy && !d_entropy)))
+    return fail(JF_E_INVAL, "null pointer argument");
+  PolicyArgs a{};
+  a.n_seqs = none ? 0 : n_seqs; a.n_rows = none ? 0 : n_rows; a.mean = policy->mean; a.adv_rows = policy->adv_rows;
+  a.row_start = d_row_start; a.tokens = d_tokens;
+  a.lp = d_logprob; a.old = d_old_logprob; a.ref = d_ref_logprob; a.entropy = d_entropy; a.adv = d_advantage;
+  a.low = policy->clip_low; a.high = policy->clip_high;
+  a.kl_weight = policy->kl_weight; a.entropy_weight = policy->entropy_weight; a.scale = policy->scale;
+  a.stats = d_stats; a.g_lp = d_g_logprob; a.g_entropy = d_g_entropy;
+  a.ws = d_ws;
+  a.flags = d_flags;
+  HIP_TRY(launch_policy(a, (hipStream_t)stream));
+  return JF_OK;
+}

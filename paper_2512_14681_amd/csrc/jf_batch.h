@@ -35,6 +35,26 @@ __device__ __forceinline__ int batch_page_id(const BatchArgs& b, int id) {
 }
 __device__ __forceinline__ int batch_page(const BatchArgs& b, const Seq& q, int p) { return batch_page_id(b, q.table[p]); }
 
+// ---- what a row sees ---------------------------------------------------------------
+// Low n bits, n clamped to [0, 64].
+__device__ __forceinline__ uint64_t low_bits(int n) { return n >= 64 ? ~0ull : (n <= 0 ? 0ull : (1ull << n) - 1); }
+
+// Bits j0 .. j0 + 63 of what a row sees (j0 > -64): slots before the in-step
+// ones, then those of its mask (causal for vis null), none past the
+// sequence's n rows.
+__device__ __forceinline__ uint64_t seen_bits(const uint64_t* vis, int i, int n, int j0) {
+  uint64_t w;
+  if (vis) {
+    const int k = j0 >> 6, sh = j0 & 63;  // floor: k = -1 for a window that starts before the in-step slots
+    const uint64_t a = k >= 0 && k < kVisWords ? vis[k] : 0, b = k + 1 < kVisWords ? vis[k + 1] : 0;
+    w = sh ? (a >> sh) | (b << (64 - sh)) : a;
+    w &= low_bits(n - j0);
+  } else {
+    w = low_bits(min(i + 1, n) - j0);
+  }
+  return w | low_bits(-j0);
+}
+
 // ---- 8-bit pages ------------------------------------------------------------------
 // Codes of the keys [G][64 hd], of the values [G][64 hd], then the scales
 // [G][2] (key, value; powers of two), padded to 128 bytes.  A head's 64 hd

@@ -359,6 +359,77 @@ struct LogprobGradArgs {
 };
 hipError_t launch_logprobs_grad(int dtype, const LogprobGradArgs& a, hipStream_t stream);
 
+// attention_causal.hip
+struct CausalArgs {
+  int n_seqs, n_rows, H, G, hd;
+  const int32_t* row_start;  // [n_seqs + 1]
+  int32_t* flags;            // or null
+  const void *q, *k, *v;     // rows [n_rows][ld]
+  size_t ld_q, ld_k, ld_v;
+  int vec;                   // all rows read start on 16-byte boundaries, their strides fit 32-bit offsets
+  void* out;
+  size_t ld_out;
+  int vec_out;               // every four elements from a multiple of 4 are aligned
+  float* lse;                // [H][n_rows]; may be null in the forward pass
+  int blocks;                // bound on the blocks of rows of all sequences (causal_blocks)
+};
+int causal_blocks(int n_rows, int n_seqs);
+hipError_t launch_causal(int dtype, const CausalArgs& a, hipStream_t stream);
+struct CausalGradArgs {
+  CausalArgs f;              // out: read
+  const void* g_out;
+  size_t ld_g_out;
+  int vec_dot;               // rows of out and g_out start on 16-byte boundaries
+  void *g_q, *g_k, *g_v;
+  size_t ld_g_q, ld_g_k, ld_g_v;
+  int vec_q, vec_kv;         // every four elements from a multiple of 4 are aligned
+  float2* dots;              // [H][n_rows]
+  float* kv_part;            // [2][parts][n_rows][G * hd], with more than one part
+  int parts;                 // shares of a group's heads (causal_parts)
+};
+int causal_parts(int n_rows, int n_seqs, int H, int G);
+hipError_t launch_causal_grad(int dtype, const CausalGradArgs& a, hipStream_t stream);
+
+// attention_shared.hip
+struct SharedArgs {
+  BatchArgs b;
+  int n_groups, max_group_rows, max_pages;
+  const int32_t* seq_start;  // [n_groups + 1]
+  const int32_t* pages;      // [n_groups]
+  int H, G, hd;
+  const void* q;             // activation planes [n_rows][H][hd]
+  size_t q_plane;
+  const void* kv;
+  const uint64_t* vis;       // [n_rows][kVisWords], or null (causal)
+  void* out;                 // activation planes, GEMM-input layout of [n_rows][H * hd]
+  size_t out_plane;
+  float* o_part;             // [parts][n_rows * H][hd]
+  float* ml_part;            // [parts][n_rows * H][2]
+  // the plan (shared_plan)
+  int shared_few, own_few;   // one tile of queries: the waves of a workgroup split its pages
+  int shared_groups, own_groups;   // workgroups along the queries
+  int shared_splits, own_splits;   // parts of the pages at most
+  int parts;                 // their sum; 1: nothing to merge
+  int64_t shared_jobs64, own_jobs64;
+  int shared_jobs;
+};
+void shared_plan(SharedArgs& a);
+hipError_t launch_attention_shared(int dtype, SharedArgs& a, hipStream_t stream);
+
+// policy.hip
+struct PolicyArgs {
+  int n_seqs, n_rows, mean, adv_rows;
+  const int32_t *row_start, *tokens;
+  const float *lp, *old, *ref, *entropy, *adv;   // ref and entropy may be null
+  double low, high, kl_weight, entropy_weight, scale;
+  float *stats, *g_lp, *g_entropy;               // the gradients may be null
+  void* ws;
+  int32_t* flags;
+  int blocks;
+};
+size_t policy_ws_bytes(int n_seqs, int n_rows);
+hipError_t launch_policy(PolicyArgs& a, hipStream_t stream);
+
 // trajectory.hip
 hipError_t launch_traj_record(const int32_t* prev, const int32_t* g, int n, int rows, int32_t* out,
                               hipStream_t stream);

@@ -1,0 +1,259 @@
+// 32 x 32 matrix-core tiles whose operands come from row-major tiles in LDS:
+// the attention over packed rows and over shared prefixes.
+//
+// A tile's contraction runs in steps of 16: lane l gives row (or column)
+// l % 32 and elements 8 (l / 32) .. + 7 of the step.  In the result lane l
+// holds column l % 32 of rows 8 (i / 4) + 4 (l / 32) + i % 4, i < 16.
+#pragma once
+
+#include "jf_device.h"
+
+namespace jf {
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+// fp32: eight instructions of two elements each (element e of both halves).
+__device__ __forceinline__ void mfma32(f32x16_t& acc, const Frag<bf16_t>& a, const Frag<bf16_t>& b) {
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a.v), __builtin_bit_cast(bf16x8_t, b.v),
+                                                acc, 0, 0, 0);
+}
+__device__ __forceinline__ void mfma32(f32x16_t& acc, const Frag<float>& a, const Frag<float>& b) {
+  const float x[8] = {a.lo.x, a.lo.y, a.lo.z, a.lo.w, a.hi.x, a.hi.y, a.hi.z, a.hi.w};
+  const float y[8] = {b.lo.x, b.lo.y, b.lo.z, b.lo.w, b.hi.x, b.hi.y, b.hi.z, b.hi.w};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16_t zero16() {
+  f32x16_t z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.f;
+  return z;
+}
+// Row of element i in a result, without the 4 (l / 32) of the lane.
+__device__ __forceinline__ constexpr int acc_row(int i) { return 8 * (i / 4) + i % 4; }
+
+// Eight values as an operand.
+__device__ __forceinline__ void frag_of(const float* x, Frag<bf16_t>& f) {
+  f.v = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+}
+__device__ __forceinline__ void frag_of(const float* x, Frag<float>& f) {
+  f.lo = make_float4(x[0], x[1], x[2], x[3]);
+  f.hi = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+// Maximum over, and sum over, the two lanes that hold one column.
+__device__ __forceinline__ float pair_max(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float pair_sum(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+// A tile of rows in LDS, kRowBytes each, in 16-byte chunks: chunk c of row r
+// lies at place c ^ turn(r) of its row.  Eight rows' chunks of one column, and
+// four rows' pairs of chunks, then lie in different banks.
+template <int kRowBytes> __device__ __forceinline__ constexpr int turn(int r) {
+  return kRowBytes >= 256 ? ((r & 3) << 1) | ((r >> 2) & 1) : kRowBytes == 128 ? ((r >> 1) & 3) << 1 : ((r >> 2) & 1) << 1;
+}
+
+typedef __attribute__((address_space(3))) char lds_char_t;
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(lds_char_t*)reinterpret_cast<char*>(const_cast<void*>(p));
+}
+
+// Operand reads from a row-major tile [rows][HD] of T.
+template <typename T, int HD> struct RowTile {
+  static constexpr int kRowBytes = HD * (int)sizeof(T);
+  static constexpr int kChunks = kRowBytes / 16;
+  static_assert(kChunks >= 4, "a row holds four chunks or more");
+
+  // Rows r0 + l % 32 (r0 a multiple of 8), dims 16 s + 8 (l / 32) .. + 7.
+  static __device__ __forceinline__ Frag<T> rows(const char* tile, int r0, int s) {
+    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+    const char* p = tile + (r0 + r) * kRowBytes;
+    if constexpr (sizeof(T) == 2) {
+      Frag<T> f;
+      f.v = *reinterpret_cast<const uint4*>(p + (((2 * s + h) ^ turn<kRowBytes>(r)) << 4));
+      return f;
+    } else {
+      Frag<T> f;
+      f.lo = *reinterpret_cast<const float4*>(p + (((4 * s + 2 * h) ^ turn<kRowBytes>(r)) << 4));
+      f.hi = *reinterpret_cast<const float4*>(p + (((4 * s + 2 * h + 1) ^ turn<kRowBytes>(r)) << 4));
+      return f;
+    }
+  }
+  // The transposed tile: dims 32 t + l % 32, of the 16 tile rows from r0 (a
+  // multiple of 8) those that a result's elements 0 .. 7 stand for:
+  // r0 + 8 (e / 4) + 4 (l / 32) + e % 4.
+  static __device__ __forceinline__ Frag<T> columns(const char* tile, int r0, int t) {
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    if constexpr (sizeof(T) == 2) {
+      // a group of 16 lanes reads 4 rows of 16 dims, and each lane gets its dim of the 4 rows
+      const int i = lane & 15, g = (lane >> 4) & 1, r = 4 * h + (i >> 2);
+      const char* p = tile + (r0 + r) * kRowBytes + (((4 * t + 2 * g + ((i & 3) >> 1)) ^ turn<kRowBytes>(r)) << 4) + (i & 1) * 8;
+      typedef short s16x4_t __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+      const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(lds_char_t*)const_cast<char*>(p)));
+      const uint2 b = __builtin_bit_cast(
+          uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(lds_char_t*)const_cast<char*>(p + 8 * kRowBytes)));
+      Frag<T> f;
+      f.v = make_uint4(a.x, a.y, b.x, b.y);
+      return f;
+    } else {
+      const int d = lane & 31;
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int r = 8 * (e / 4) + 4 * h + e % 4;
+        x[e] = *reinterpret_cast<const float*>(tile + (r0 + r) * kRowBytes + (((8 * t + (d >> 2)) ^ turn<kRowBytes>(r)) << 4) +
+                                               (d & 3) * 4);
+      }
+      Frag<T> f;
+      f.lo = make_float4(x[0], x[1], x[2], x[3]);
+      f.hi = make_float4(x[4], x[5], x[6], x[7]);
+      return f;
+    }
+  }
+};
+
+// Largest magnitude bits of an operand's elements, kept over several
+// operands (pairs of bf16, or one fp32), and whether they were all finite.
+__device__ __forceinline__ void magnitude(const Frag<bf16_t>& f, uint32_t& top) {
+  const uint32_t w[4] = {f.v.x, f.v.y, f.v.z, f.v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+    top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, top),
+                                                                 __builtin_bit_cast(u16x2_t, w[i] & 0x7FFF7FFFu)));
+  }
+}
+__device__ __forceinline__ void magnitude(const Frag<float>& f, uint32_t& top) {
+  const float x[8] = {f.lo.x, f.lo.y, f.lo.z, f.lo.w, f.hi.x, f.hi.y, f.hi.z, f.hi.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+}
+template <typename T> __device__ __forceinline__ bool all_finite(uint32_t top);
+template <> __device__ __forceinline__ bool all_finite<bf16_t>(uint32_t top) {
+  return (top & 0xFFFFu) < 0x7F80u && (top >> 16) < 0x7F80u;
+}
+template <> __device__ __forceinline__ bool all_finite<float>(uint32_t top) { return top < 0x7F800000u; }
+
+// An operand with its infinities and NaN as 0; where they were, 1 in `up` (+inf
+// and NaN) and in `down` (-inf and NaN), which have 0 elsewhere.
+__device__ __forceinline__ void part_finite(const Frag<bf16_t>& f, Frag<bf16_t>& clean, Frag<bf16_t>& up, Frag<bf16_t>& down) {
+  const uint32_t w[4] = {f.v.x, f.v.y, f.v.z, f.v.w};
+  uint32_t c[4], u[4], d[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    c[i] = u[i] = d[i] = 0;
+#pragma unroll
+    for (int s = 0; s < 32; s += 16) {
+      const uint32_t x = (w[i] >> s) & 0xFFFFu, one = 0x3F80u << s;
+      const bool bad = (x & 0x7F80u) == 0x7F80u;
+      c[i] |= bad ? 0u : x << s;
+      u[i] |= bad && x != 0xFF80u ? one : 0u;
+      d[i] |= bad && x != 0x7F80u ? one : 0u;
+    }
+  }
+  clean.v = make_uint4(c[0], c[1], c[2], c[3]);
+  up.v = make_uint4(u[0], u[1], u[2], u[3]);
+  down.v = make_uint4(d[0], d[1], d[2], d[3]);
+}
+__device__ __forceinline__ void part_finite(const Frag<float>& f, Frag<float>& clean, Frag<float>& up, Frag<float>& down) {
+  float x[8] = {f.lo.x, f.lo.y, f.lo.z, f.lo.w, f.hi.x, f.hi.y, f.hi.z, f.hi.w}, u[8], d[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const bool bad = (__float_as_uint(x[i]) & 0x7F800000u) == 0x7F800000u;
+    u[i] = bad && x[i] != -INFINITY ? 1.f : 0.f;
+    d[i] = bad && x[i] != INFINITY ? 1.f : 0.f;
+    x[i] = bad ? 0.f : x[i];
+  }
+  frag_of(x, clean);
+  frag_of(u, up);
+  frag_of(d, down);
+}
+// Adds to a column's outputs what it sees (1 in `seen`) of such values: an
+// infinity, or NaN.
+template <typename T>
+__device__ __forceinline__ void add_infinite(f32x16_t& o, const Frag<T>& up, const Frag<T>& down, const Frag<T>& seen) {
+  f32x16_t ups = zero16(), downs = zero16();
+  mfma32(ups, up, seen);
+  mfma32(downs, down, seen);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    if (ups[i] > 0.f) o[i] += INFINITY;
+    if (downs[i] > 0.f) o[i] -= INFINITY;
+  }
+}
+
+// Eight consecutive elements of a row in memory; vec: on a boundary of all eight.
+template <typename T> __device__ __forceinline__ Frag<T> row_frag(const T* p, bool vec);
+template <> __device__ __forceinline__ Frag<bf16_t> row_frag<bf16_t>(const bf16_t* p, bool vec) {
+  if (vec) return frag_load<bf16_t>(p);
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = p[2 * i] | ((uint32_t)p[2 * i + 1] << 16);
+  Frag<bf16_t> f;
+  f.v = make_uint4(w[0], w[1], w[2], w[3]);
+  return f;
+}
+template <> __device__ __forceinline__ Frag<float> row_frag<float>(const float* p, bool vec) {
+  if (vec) return frag_load<float>(p);
+  Frag<float> f;
+  f.lo = make_float4(p[0], p[1], p[2], p[3]);
+  f.hi = make_float4(p[4], p[5], p[6], p[7]);
+  return f;
+}
+
+// Brings rows of a matrix (HD of its columns, ld elements a row) into an LDS
+// tile of ROWS rows, by W waves; rows past `last` repeat row `last`.  kVec:
+// rows on 16-byte boundaries go to LDS without passing registers, and the
+// reader waits for them (wait_vm).
+template <typename T, int HD, int ROWS, int W, bool kVec> struct RowLoader {
+  static constexpr int kRowBytes = HD * (int)sizeof(T);
+  static constexpr int kPieces = ROWS * kRowBytes / 1024 / W;  // 1 KB pieces a wave
+  static_assert(ROWS * kRowBytes % (1024 * W) == 0, "whole pieces");
+
+  static __device__ __forceinline__ void load(const T* base, size_t ld, int last, char* tile) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int o = (i * W + wave) * 1024 + lane * 16, r = o / kRowBytes;
+      const int c = (o % kRowBytes / 16) ^ turn<kRowBytes>(r), rr = min(r, last);
+      if constexpr (kVec) {
+        dma_1k<false>(reinterpret_cast<const char*>(base), rr * (int)(ld * sizeof(T)) + c * 16,
+                      lds_address(tile) + (i * W + wave) * 1024);
+      } else {
+        const T* p = base + (size_t)rr * ld + c * (16 / (int)sizeof(T));
+        T x[16 / sizeof(T)];
+#pragma unroll
+        for (int e = 0; e < 16 / (int)sizeof(T); ++e) x[e] = p[e];
+        *reinterpret_cast<uint4*>(tile + o) = *reinterpret_cast<const uint4*>(x);
+      }
+    }
+  }
+};
+
+// Four consecutive columns of a row; vec: on a boundary of all four.
+template <typename T> __device__ __forceinline__ void row_store4(T* p, bool vec, float a, float b, float c, float d);
+template <> __device__ __forceinline__ void row_store4<bf16_t>(bf16_t* p, bool vec, float a, float b, float c, float d) {
+  const uint32_t x = pack_bf16x2(a, b), y = pack_bf16x2(c, d);
+  if (vec) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(x, y);
+  } else {
+    p[0] = (bf16_t)x; p[1] = (bf16_t)(x >> 16); p[2] = (bf16_t)y; p[3] = (bf16_t)(y >> 16);
+  }
+}
+template <> __device__ __forceinline__ void row_store4<float>(float* p, bool vec, float a, float b, float c, float d) {
+  if (vec) {
+    *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+  } else {
+    p[0] = a; p[1] = b; p[2] = c; p[3] = d;
+  }
+}
+
+}  // namespace jf

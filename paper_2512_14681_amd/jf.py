@@ -29,6 +29,8 @@ JF_FLAG_BAD_TOKEN, JF_FLAG_CAPACITY, JF_FLAG_SYNC, JF_FLAG_BAD_PAGE = 1, 2, 4, 8
 JF_MAX_TOP = 32        # alternatives of jf_token_logprobs at most
 JF_OPT_FUSED_ATTENTION = 1
 JF_MASK_NOISY_CONTEXT, JF_MASK_CLEAN_CONTEXT = 0, 1
+JF_MEAN_TOKENS, JF_MEAN_SEQS, JF_SUM = 0, 1, 2
+JF_POLICY_STATS = 6    # loss, then the means of policy term, KL, entropy and clipped rows, then tokens
 (JF_KERNEL_QKV, JF_KERNEL_ATTN, JF_KERNEL_O, JF_KERNEL_GATEUP, JF_KERNEL_DOWN, JF_KERNEL_LMHEAD,
  JF_KERNEL_STEP, JF_KERNEL_ATTN_BLOCK) = range(1, 9)
 STATUS_NAMES = {0: "JF_OK", -1: "JF_E_INVAL", -2: "JF_E_SHAPE", -3: "JF_E_CAPACITY",
@@ -80,6 +82,17 @@ class JfBatch(ctypes.Structure):
                 ("d_row_start", ctypes.c_void_p), ("d_ctx", ctypes.c_void_p), ("d_page_table", ctypes.c_void_p)]
 
 
+class JfPrefix(ctypes.Structure):
+    _fields_ = [("n_groups", ctypes.c_int32), ("max_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("d_seq_start", ctypes.c_void_p), ("d_pages", ctypes.c_void_p)]
+
+
+class JfPolicy(ctypes.Structure):
+    _fields_ = [("clip_low", ctypes.c_double), ("clip_high", ctypes.c_double), ("kl_weight", ctypes.c_double),
+                ("entropy_weight", ctypes.c_double), ("scale", ctypes.c_double), ("mean", ctypes.c_int32),
+                ("adv_rows", ctypes.c_int32)]
+
+
 class JfError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {msg}")
@@ -89,6 +102,7 @@ class JfError(RuntimeError):
 _LIB = None
 P, I32, U64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_size_t
 I64, F64, PB = ctypes.c_int64, ctypes.c_double, ctypes.POINTER(JfBatch)
+PX, PY = ctypes.POINTER(JfPrefix), ctypes.POINTER(JfPolicy)
 _SIGS = {
     "jf_query_sizes": (I32, [ctypes.POINTER(JfConfig), ctypes.POINTER(SZ), ctypes.POINTER(SZ), ctypes.POINTER(SZ)]),
     "jf_model_load": (I32, [ctypes.POINTER(JfConfig), ctypes.POINTER(P), I32, P, P, P, P, ctypes.POINTER(P)]),
@@ -122,6 +136,14 @@ _SIGS = {
     "jf_token_logprobs_ws_bytes": (SZ, [I32, I32, I32]),
     "jf_token_logprobs": (I32, [I32, I32, I32, P, I64, P, I32, P, P, P, P, P, P, P]),
     "jf_token_logprobs_grad": (I32, [I32, I32, I32, P, I64, P, P, P, P, P, P, I64, P]),
+    "jf_attention_causal": (I32, [I32, I32, P, I32, I32, I32, I32, P, I64, P, I64, P, I64, P, I64, P, P, P]),
+    "jf_attention_causal_grad_ws_bytes": (SZ, [I32, I32, I32, I32, I32]),
+    "jf_attention_causal_grad": (I32, [I32, I32, P, I32, I32, I32, I32, P, I64, P, I64, P, I64, P, I64, P, P, I64, P, I64,
+                                       P, I64, P, I64, P, P, P]),
+    "jf_attention_shared_ws_bytes": (SZ, [PB, PX, I32, I32, I32]),
+    "jf_attention_shared": (I32, [PB, PX, I32, I32, I32, I32, P, P, P, P, P, P, P]),
+    "jf_policy_loss_ws_bytes": (SZ, [I32, I32]),
+    "jf_policy_loss": (I32, [PY, I32, I32, P, P, P, P, P, P, P, P, P, P, P, P, P]),
 }
 EXPORTS = tuple(_SIGS)
 
@@ -504,5 +526,164 @@ def token_logprobs_grad(d_logits, d_norm, d_grad, d_tokens=None, d_entropy=None,
                                           _vec(dev, d_norm, _F32, 2 * R), _vec(dev, d_entropy, _F32, R),
                                           _vec(dev, d_g_logprob, _F32, R), _vec(dev, d_g_entropy, _F32, R),
                                           _at(dev, d_grad), ld_g, _on(dev, stream))
+    if status:
+        check(status)
+
+
+# ---- training on sampled groups: causal attention, shared prefixes, policy loss (component calls) -----
+def _starts(dev, t):
+    """(address, sequences) of row starts [n_seqs + 1] on the current GPU."""
+    if t.dtype is not _I32 or not t.is_contiguous() or t.numel() < 1:
+        raise TypeError("row starts are a contiguous int32 tensor of one element more than there are sequences")
+    return _at(dev, t), t.numel() - 1
+
+
+def _causal_rows(n_heads, n_kv_heads, head_dim, wide, narrow):
+    """(jf_dtype, rows, strides of `wide` and of `narrow`): [rows][n_heads * head_dim] and [rows][n_kv_heads * head_dim]
+    tensors of one type and as many rows as the first."""
+    n = wide[0].shape[0]
+    kinds = [_rows(t, n, n_heads * head_dim) for t in wide] + [_rows(t, n, n_kv_heads * head_dim) for t in narrow]
+    x = kinds[0][0]
+    for code, _ in kinds:
+        if code != x:
+            raise TypeError("all rows have one type")
+    return x, n, [ld for _, ld in kinds]
+
+
+def attention_causal(d_row_start, n_heads, n_kv_heads, head_dim, d_q, d_k, d_v, d_out, d_lse=None, d_flags=None,
+                     stream=None):
+    """Rows of d_q [rows][n_heads * head_dim] over those of d_k and d_v up to their own, sequence by sequence, to d_out;
+    d_lse [n_heads][rows] for attention_causal_grad."""
+    x, n, (ld_q, ld_out, ld_k, ld_v) = _causal_rows(n_heads, n_kv_heads, head_dim, (d_q, d_out), (d_k, d_v))
+    dev = _current_device()
+    start, n_seqs = _starts(dev, d_row_start)
+    _count(n, n_seqs)
+    status = lib().jf_attention_causal(n_seqs, n, start, n_heads, n_kv_heads, head_dim, x, _at(dev, d_q), ld_q,
+                                       _at(dev, d_k), ld_k, _at(dev, d_v), ld_v, _at(dev, d_out), ld_out,
+                                       _vec(dev, d_lse, _F32, n_heads * n), _vec(dev, d_flags, _I32, 1),
+                                       _on(dev, stream))
+    if status:
+        check(status)
+
+
+@functools.lru_cache(4096)
+def attention_causal_grad_ws_bytes(n_seqs, n_rows, n_heads, n_kv_heads, head_dim):
+    _count(n_seqs, n_rows)
+    n = lib().jf_attention_causal_grad_ws_bytes(n_seqs, n_rows, n_heads, n_kv_heads, head_dim)
+    if n == 0:
+        raise JfError(JF_E_SHAPE, "no rows or heads that jf_attention_causal_grad takes")
+    return n
+
+
+def attention_causal_grad(d_row_start, n_heads, n_kv_heads, head_dim, d_q, d_k, d_v, d_out, d_lse, d_g_out, d_g_q, d_g_k,
+                          d_g_v, d_ws, d_flags=None, stream=None):
+    """Gradient of sum(d_g_out * d_out) to queries, keys and values, from attention_causal's inputs and outputs."""
+    x, n, (ld_q, ld_out, ld_g, ld_gq, ld_k, ld_v, ld_gk, ld_gv) = _causal_rows(
+        n_heads, n_kv_heads, head_dim, (d_q, d_out, d_g_out, d_g_q), (d_k, d_v, d_g_k, d_g_v))
+    dev = _current_device()
+    start, n_seqs = _starts(dev, d_row_start)
+    status = lib().jf_attention_causal_grad(
+        n_seqs, n, start, n_heads, n_kv_heads, head_dim, x, _at(dev, d_q), ld_q, _at(dev, d_k), ld_k, _at(dev, d_v), ld_v,
+        _at(dev, d_out), ld_out, _vec(dev, d_lse, _F32, n_heads * n), _at(dev, d_g_out), ld_g, _at(dev, d_g_q), ld_gq,
+        _at(dev, d_g_k), ld_gk, _at(dev, d_g_v), ld_gv,
+        _buf(dev, d_ws, attention_causal_grad_ws_bytes(n_seqs, n, n_heads, n_kv_heads, head_dim)),
+        _vec(dev, d_flags, _I32, 1), _on(dev, stream))
+    if status:
+        check(status)
+
+
+class Prefix:
+    """A jf_prefix over device int32 tensors (kept alive here): seq_start [n_groups + 1] and pages [n_groups], with the
+    host's bounds on the rows and the shared pages of a group."""
+
+    def __init__(self, seq_start, pages, max_rows, max_pages):
+        _types()
+        self.tensors = (seq_start, pages)
+        for t in self.tensors:
+            if t.dtype is not _I32 or not t.is_contiguous():
+                raise TypeError("seq_start and pages are contiguous int32 tensors")
+        n = pages.numel()
+        if seq_start.numel() != n + 1:
+            raise ValueError(f"{n} groups need {n + 1} sequence starts")
+        if pages.get_device() != seq_start.get_device():
+            raise ValueError("seq_start and pages are on one device")
+        _count(n, int(max_rows), int(max_pages))
+        self.device = pages.get_device()
+        self.c = JfPrefix(n, int(max_rows), int(max_pages), seq_start.data_ptr(), pages.data_ptr())
+        self.ref = ctypes.byref(self.c)
+
+    def on(self, dev):
+        if self.device != dev:
+            raise ValueError(f"the prefix is on device {self.device}, the call runs on GPU {dev}")
+        return self.ref
+
+
+def _shared_ws_bytes(batch, prefix, shape):
+    key = shape if prefix is None else shape + (prefix.c.n_groups, prefix.c.max_rows, prefix.c.max_pages)
+    n = batch.ws.get(key)
+    if n is None:
+        n = lib().jf_attention_shared_ws_bytes(batch.ref, None if prefix is None else prefix.ref, *shape[1:])
+        batch.ws[key] = n
+    return n
+
+
+def attention_shared_ws_bytes(batch, prefix, n_heads, n_kv_heads, head_dim):
+    n = _shared_ws_bytes(batch, prefix, ("shared", n_heads, n_kv_heads, head_dim))
+    if n == 0:
+        raise JfError(JF_E_SHAPE, "no batch, prefix or heads that jf_attention_shared takes")
+    return n
+
+
+def attention_shared(batch, prefix, n_heads, n_kv_heads, head_dim, dtype, d_q, d_kv, d_out, d_ws, d_vis=None,
+                     d_flags=None, stream=None):
+    """Attention of a batch over a paged cache of dtype, the pages that groups of its sequences share read once for all
+    rows of a group (prefix None: nothing is shared)."""
+    dev, n = _current_device(), batch.n_rows
+    row = 4 * n_heads * head_dim        # bytes: fp32, or two bf16 planes
+    status = lib().jf_attention_shared(batch.on(dev), None if prefix is None else prefix.on(dev), n_heads, n_kv_heads,
+                                       head_dim, dtype, _act(dev, d_q, dtype, n * row),
+                                       _buf(dev, d_kv, _pool_bytes(batch, n_kv_heads, head_dim, dtype)),
+                                       _buf(dev, d_vis, n * 8 * JF_VIS_WORDS),
+                                       _act(dev, d_out, dtype, (n + 15) // 16 * 16 * row),  # 16 rows a tile
+                                       _buf(dev, d_ws, _shared_ws_bytes(batch, prefix,
+                                                                        ("shared", n_heads, n_kv_heads, head_dim))),
+                                       _vec(dev, d_flags, _I32, 1), _on(dev, stream))
+    if status:
+        check(status)
+
+
+@functools.lru_cache(4096)
+def policy_loss_ws_bytes(n_seqs, n_rows):
+    _count(n_seqs, n_rows)
+    n = lib().jf_policy_loss_ws_bytes(n_seqs, n_rows)
+    if n == 0:
+        raise JfError(JF_E_CAPACITY, "more sequences or rows than jf_policy_loss takes")
+    return n
+
+
+@functools.lru_cache(256)
+def _policy(*fields):
+    return JfPolicy(*fields)
+
+
+def policy_loss(d_row_start, d_tokens, d_logprob, d_old_logprob, d_advantage, d_stats, d_ws, d_ref_logprob=None,
+                d_entropy=None, d_g_logprob=None, d_g_entropy=None, clip_low=0.2, clip_high=0.2, kl_weight=0.0,
+                entropy_weight=0.0, scale=1.0, mean=JF_MEAN_TOKENS, adv_rows=False, d_flags=None, stream=None):
+    """Clipped policy loss over the tokens of sampled sequences: d_stats [JF_POLICY_STATS] and, where given, its gradient
+    to the log probabilities and entropies of token_logprobs.  d_advantage has one element a sequence, or one a row
+    (adv_rows); d_tokens None: every row has a token."""
+    _types()
+    n = d_logprob.numel()
+    dev = _current_device()
+    start, n_seqs = _starts(dev, d_row_start)
+    params = _policy(clip_low, clip_high, kl_weight, entropy_weight, scale, mean, 1 if adv_rows else 0)
+    status = lib().jf_policy_loss(ctypes.byref(params), n_seqs, n, start, _vec(dev, d_tokens, _I32, n),
+                                  _vec(dev, d_logprob, _F32, n), _vec(dev, d_old_logprob, _F32, n),
+                                  _vec(dev, d_ref_logprob, _F32, n), _vec(dev, d_entropy, _F32, n),
+                                  _vec(dev, d_advantage, _F32, n if adv_rows else n_seqs),
+                                  _vec(dev, d_stats, _F32, JF_POLICY_STATS),
+                                  _vec(dev, d_g_logprob, _F32, n),
+                                  _vec(dev, d_g_entropy, _F32, n), _buf(dev, d_ws, policy_loss_ws_bytes(n_seqs, n)),
+                                  _vec(dev, d_flags, _I32, 1), _on(dev, stream))
     if status:
         check(status)
