@@ -197,16 +197,26 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalAr
 #pragma unroll
         for (int d = 0; d < ND; ++d) mfma32(o[d], Tile::columns(values, 16 * j, d), pf);
       } else {
-        Frag<T> clean, up, down, seen;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = 16 * j + acc_row(e) <= lim ? 1.f : 0.f;
-        frag_of(p, seen);
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
-          part_finite(Tile::columns(values, 16 * j, d), clean, up, down);
-          mfma32(o[d], clean, pf);
-          add_infinite<T>(o[d], up, down, seen);
+          __builtin_amdgcn_sched_barrier(0);
+          Frag<T> v = Tile::columns(values, 16 * j, d);
+          keep_finite(v);
+          mfma32(o[d], v, pf);
+          __builtin_amdgcn_sched_barrier(0);
         }
+      }
+    }
+    if (kEdge && !finite) {
+#pragma unroll 1
+      for (int j = 0; j < 2 * KT; ++j) {
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = 16 * j + acc_row(e) <= lim ? 1.f : 0.f;
+        Frag<T> seen;
+        frag_of(p, seen);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) add_infinite<T>(o[d], Tile::columns(values, 16 * j, d), seen);
       }
     }
   };

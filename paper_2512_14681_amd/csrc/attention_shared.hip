@@ -28,6 +28,7 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.f;  // weights are 2^(s - m), m the row's maximum or up to this below it
 constexpr int kChunk = 4;      // pages of a part at least
+constexpr int kWorkgroups = 512;  // as many as run at once
 
 // Queries as operands: bf16 in two terms.
 template <typename T> struct Query;
@@ -108,10 +109,11 @@ template <typename T, int HD> struct SharedTile {
     for (int d = 0; d < ND; ++d) o[d] = zero16();
   }
 
-  // 32 KT keys in LDS (their rows in the order of key_row) and V^T beside
-  // them.  kEdge: seen holds a bit for each that the lane's query sees.
+  // 32 KT keys in LDS (in PageLoader's order) and V^T beside them.  kEdge: seen
+  // holds a bit for each that the lane's query sees.  False if there were
+  // values that are not finite, which count as 0 here.
   template <int KT, bool kEdge>
-  __device__ __forceinline__ void step(const char* keys, const char* values, uint64_t seen) {
+  __device__ __forceinline__ bool step(const char* keys, const char* values, uint64_t seen) {
     using Keys = RowTile<T, HD>;
     using Values = RowTile<T, 32 * KT>;
     const float c = kLog2e / sqrtf((float)HD);
@@ -160,6 +162,7 @@ template <typename T, int HD> struct SharedTile {
 #pragma unroll
         for (int d = 0; d < ND; ++d) magnitude(Values::rows(values, 32 * d, j), top);
       finite = !__any(!all_finite<T>(top));
+      asm volatile("" ::: "memory");  // read again rather than kept: registers
     }
 #pragma unroll
     for (int j = 0; j < 2 * KT; ++j) {
@@ -172,17 +175,30 @@ template <typename T, int HD> struct SharedTile {
 #pragma unroll
         for (int d = 0; d < ND; ++d) mul(o[d], Values::rows(values, 32 * d, j), pf);
       } else {
-        Frag<T> clean, up, down, sees;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = (bits[j / 2] >> (16 * (j % 2) + e)) & 1 ? 1.f : 0.f;
-        frag_of(p, sees);
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
-          part_finite(Values::rows(values, 32 * d, j), clean, up, down);
-          mul(o[d], clean, pf);
-          add_infinite<T>(o[d], up, down, sees);
+          __builtin_amdgcn_sched_barrier(0);
+          Frag<T> v = Values::rows(values, 32 * d, j);
+          keep_finite(v);
+          mul(o[d], v, pf);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
+    }
+    return finite;
+  }
+  // What the queries see of infinities and NaN among the values that step left out.
+  template <int KT> __device__ __forceinline__ void infinite(const char* values, uint64_t seen) {
+    seen >>= 8 * ((threadIdx.x & 63) >> 5);
+#pragma unroll 1
+    for (int j = 0; j < 2 * KT; ++j) {
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = (seen >> (16 * j + e)) & 1 ? 1.f : 0.f;
+      Frag<T> sees;
+      frag_of(p, sees);
+#pragma unroll
+      for (int d = 0; d < ND; ++d) add_infinite<T>(o[d], RowTile<T, 32 * KT>::rows(values, 32 * d, j), sees);
     }
   }
 };
@@ -193,23 +209,27 @@ template <typename T, int HD> struct SharedTile {
 // then are keys 16 j + 8 (l / 32) .. + 7.
 template <typename T, int HD, int KT, int W> struct PageLoader {
   static __device__ __forceinline__ void load(const T* keys, const T* values, int t0, int wave, char* tile) {
-    constexpr int kKeyRow = HD * (int)sizeof(T), kValueRow = 32 * KT * (int)sizeof(T);
+    constexpr int kKeyRow = HD * (int)sizeof(T), kValueRow = 32 * KT * (int)sizeof(T), kValueStride = kPage * (int)sizeof(T);
     constexpr int kPieces = 32 * KT * kKeyRow / 1024 / W;
+    static_assert(kPieces * W * 1024 == 32 * KT * kKeyRow, "whole pieces");
+    constexpr int kKeyRows = 1024 / kKeyRow, kValueRows = 1024 / kValueRow;  // rows of a 1 KB piece
+    static_assert(kKeyRows <= 16 && kValueRows >= 8, "places repeat after 16 keys and 8 dims");
     const int lane = threadIdx.x & 63;
-    const uint32_t at = lds_address(tile);
+    const uint32_t at = lds_address(tile) + wave * 1024;
+    // Few offsets in registers: they repeat every 16 keys (every 8 dims), the rest is the same for all lanes.
+    constexpr int kPeriod = std::max(16 / (kKeyRows * W), 1);
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int o = (i * W + wave) * 1024 + lane * 16, r = o / kKeyRow;
-      const int c = (o % kKeyRow / 16) ^ turn<kKeyRow>(r), key = (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1);
-      dma_1k<false>(reinterpret_cast<const char*>(keys + (size_t)t0 * HD), key * kKeyRow + c * 16, at + (i * W + wave) * 1024);
+      const int row = ((i % kPeriod * W + wave) * kKeyRows) % 16 + lane * 16 / kKeyRow;
+      const int c = (lane * 16 % kKeyRow / 16) ^ turn<kKeyRow>(row), key = (row & ~12) | ((row & 4) << 1) | ((row & 8) >> 1);
+      const int skip = (i * W + wave) * kKeyRows / 16 * 16;
+      dma_1k<false>(reinterpret_cast<const char*>(keys + (size_t)t0 * HD) + skip * kKeyRow, key * kKeyRow + c * 16, at + i * W * 1024);
     }
+    const int row = lane * 16 / kValueRow, c = (lane * 16 % kValueRow / 16) ^ turn<kValueRow>(row);
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const int o = (i * W + wave) * 1024 + lane * 16, r = o / kValueRow;
-      const int c = (o % kValueRow / 16) ^ turn<kValueRow>(r);
-      dma_1k<false>(reinterpret_cast<const char*>(values + t0), r * kPage * (int)sizeof(T) + c * 16,
-                    at + 32 * KT * kKeyRow + (i * W + wave) * 1024);
-    }
+    for (int i = 0; i < kPieces; ++i)
+      dma_1k<false>(reinterpret_cast<const char*>(values + t0) + (i * W + wave) * kValueRows * kValueStride,
+                    row * kValueStride + c * 16, at + 32 * KT * kKeyRow + i * W * 1024);
   }
 };
 
@@ -232,7 +252,7 @@ __device__ __forceinline__ void put_outputs(const SharedArgs& a, int row, int he
 template <typename T, int HD>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_shared(SharedArgs a) {
   using Tile = SharedTile<T, HD>;
-  constexpr int KT = sizeof(T) == 2 ? 2 : 1, ND = HD / 32;
+  constexpr int KT = HD * sizeof(T) == 64 ? 2 : 1, ND = HD / 32;  // a 1 KB piece of a step's keys for every wave
   constexpr int kOne = 2 * 32 * HD * (int)sizeof(T);   // 32 keys and their values
   constexpr int kBytes = std::max({4 * kOne, 2 * KT * kOne, 4 * 32 * HD * 4});
   __shared__ __align__(1024) char s_kv[kBytes];
@@ -287,7 +307,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_share
     // One tile: the waves take every fourth page, each in LDS of its own.
     w.init(a, r0, n, g, group);
     char* mine = s_kv + wave * kOne;
-    auto page = [&](auto edge, int p) {
+    bool finite = true;
+    auto page = [&](auto edge, int p, auto use) {
       const int id = batch_page_id(a.b, table[p]);
       if (id < 0) return;
       const T* keys = pool + (size_t)id * page_elems + (size_t)g * kPage * HD;
@@ -297,15 +318,23 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_share
       for (int t0 = 0; t0 < kPage; t0 += 32) {
         PageLoader<T, HD, 1, 1>::load(keys, keys + (size_t)a.G * kPage * HD, t0, 0, mine);
         wait_vm<0>();
-        w.template step<1, decltype(edge)::value>(mine, mine + kOne / 2, bits >> t0);
+        use(mine, bits >> t0);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the next load takes the place of what was read
       }
     };
     int p = p0 + wave;
 #pragma unroll 1
-    for (; p < whole; p += 4) page(std::false_type{}, p);
+    for (; p < whole; p += 4)
+      page(std::false_type{}, p, [&](const char* t, uint64_t bits) { w.template step<1, false>(t, t + kOne / 2, bits); });
+    const int edges = p;
 #pragma unroll 1
-    for (; p < p1; p += 4) page(std::true_type{}, p);
+    for (; p < p1; p += 4)
+      page(std::true_type{}, p,
+           [&](const char* t, uint64_t bits) { finite &= w.template step<1, true>(t, t + kOne / 2, bits); });
+    if (!finite)
+#pragma unroll 1
+      for (p = edges; p < p1; p += 4)
+        page(std::true_type{}, p, [&](const char* t, uint64_t bits) { w.template infinite<1>(t + kOne / 2, bits); });
     // The waves' parts, dims by queries; each wave merges a quarter of the dims.
     w.l = pair_sum(w.l);
     __syncthreads();
@@ -341,7 +370,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_share
     return;
   }
   // Four tiles, one a wave, over pages that all share.
-  constexpr int kStep = 32 * KT, kTile = KT * kOne, kPerPage = kPage / kStep;
+  constexpr int kStep = 32 * KT, kTile = KT * kOne;
   w.init(a, r0, n, g, group * 4 + wave);
   const bool work = (group * 4 + wave) * 32 < nq;
   auto entry = [&](int p) { return batch_page_id(a.b, __builtin_amdgcn_readfirstlane(table[p])); };
@@ -349,29 +378,37 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_share
     const T* keys = pool + (size_t)max(id, 0) * page_elems + (size_t)g * kPage * HD;
     PageLoader<T, HD, KT, 4>::load(keys, keys + (size_t)a.G * kPage * HD, t0, wave, s_kv + buf * kTile);
   };
-  int id = entry(p0), buf = 0;
-  load(id, 0, 0);
-  auto page = [&](auto edge, int p) {
-    const int next = p + 1 < p1 ? entry(p + 1) : -1;
-    uint64_t bits = 0;
-    if constexpr (decltype(edge)::value) bits = seen(w, p);
-#pragma unroll
-    for (int t = 0; t < kPerPage; ++t) {
-      wait_vm<0>();
-      __syncthreads();
-      if (t + 1 < kPerPage) load(id, (t + 1) * kStep, buf ^ 1);
-      else if (p + 1 < p1) load(next, 0, buf ^ 1);
-      if (work && id >= 0)
-        w.template step<KT, decltype(edge)::value>(s_kv + buf * kTile, s_kv + buf * kTile + kTile / 2, bits >> (t * kStep));
-      buf ^= 1;
+  // Pages [from, to), the next step's keys and values on their way while this one's are used.
+  auto pages = [&](auto edge, int from, int to, auto use) {
+    if (from >= to) return;
+    int id = entry(from), buf = 0;
+    load(id, 0, 0);
+#pragma unroll 1
+    for (int p = from; p < to; ++p) {
+      const int next = p + 1 < to ? entry(p + 1) : -1;
+      uint64_t bits = 0;
+      if constexpr (decltype(edge)::value) bits = seen(w, p);
+#pragma unroll 1
+      for (int t0 = 0; t0 < kPage; t0 += kStep) {
+        wait_vm<0>();
+        __syncthreads();
+        if (t0 + kStep < kPage) load(id, t0 + kStep, buf ^ 1);
+        else if (p + 1 < to) load(next, 0, buf ^ 1);
+        if (work && id >= 0) use(s_kv + buf * kTile, bits >> t0);
+        buf ^= 1;
+      }
+      id = next;
     }
-    id = next;
+    __syncthreads();
   };
-  int p = p0;
-#pragma unroll 1
-  for (; p < whole; ++p) page(std::false_type{}, p);
-#pragma unroll 1
-  for (; p < p1; ++p) page(std::true_type{}, p);
+  bool finite = true;
+  pages(std::false_type{}, p0, whole, [&](const char* t, uint64_t bits) { w.template step<KT, false>(t, t + kTile / 2, bits); });
+  if (whole < p1) {
+    pages(std::true_type{}, whole, p1,
+          [&](const char* t, uint64_t bits) { finite &= w.template step<KT, true>(t, t + kTile / 2, bits); });
+    if (__syncthreads_or(!finite))
+      pages(std::true_type{}, whole, p1, [&](const char* t, uint64_t bits) { w.template infinite<KT>(t + kTile / 2, bits); });
+  }
   if (!w.valid) return;
   w.l = pair_sum(w.l);
 #pragma unroll
@@ -397,16 +434,37 @@ __global__ void __launch_bounds__(256) k_attention_shared_merge(SharedArgs a, in
   const int c0 = part_pages(pages, a.shared_splits), c1 = part_pages(own, a.own_splits);
   const int n0 = (pages + c0 - 1) / c0, n1 = (own + c1 - 1) / c1;
   const size_t stride = (size_t)a.b.n_rows * a.H, at = (size_t)row * a.H + head;
-  float m = -INFINITY;
-  for (int i = 0; i < n0 + n1; ++i) m = fmaxf(m, a.ml_part[((i < n0 ? i : a.shared_splits + i - n0) * stride + at) * 2]);
-  float l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < n0 + n1; ++i) {
-    const size_t k = (i < n0 ? i : a.shared_splits + i - n0) * stride + at;
-    const float2 ml = *reinterpret_cast<const float2*>(a.ml_part + k * 2);
-    const float4 o = *reinterpret_cast<const float4*>(a.o_part + k * a.hd + dim);
-    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
-    l += ml.y * f;
-    v[0] += o.x * f; v[1] += o.y * f; v[2] += o.z * f; v[3] += o.w * f;
+  constexpr int kAhead = 8;  // parts in flight
+  float m = -INFINITY, l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int i0 = 0; i0 < n0 + n1; i0 += kAhead) {
+    float2 ml[kAhead];
+    float4 o[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = min(i0 + j, n0 + n1 - 1);
+      const size_t k = (i < n0 ? i : a.shared_splits + i - n0) * stride + at;
+      ml[j] = *reinterpret_cast<const float2*>(a.ml_part + k * 2);
+      o[j] = *reinterpret_cast<const float4*>(a.o_part + k * a.hd + dim);
+    }
+    float m_new = m;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (i0 + j >= n0 + n1) ml[j] = make_float2(-INFINITY, 0.f);
+      m_new = fmaxf(m_new, ml[j].x);
+    }
+    const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+    m = m_new;
+    l *= alpha;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] *= alpha;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (ml[j].x == -INFINITY && ml[j].y == 0.f) continue;  // nothing seen there (or no part)
+      const float f = __builtin_amdgcn_exp2f(ml[j].x - m);
+      l += ml[j].y * f;
+      v[0] += o[j].x * f; v[1] += o[j].y * f; v[2] += o[j].z * f; v[3] += o[j].w * f;
+    }
   }
   const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll
@@ -415,8 +473,9 @@ __global__ void __launch_bounds__(256) k_attention_shared_merge(SharedArgs a, in
 }
 
 // ---- launch --------------------------------------------------------------------------
-// Workgroups of two a compute unit, in parts of kChunk pages or more; how
-// many pages there are to split is known on the device.
+// Parts of kChunk pages or more, as many as give two workgroups a compute
+// unit; how many pages there are to split is known on the device, and the
+// host's bounds stand for it here.
 void shared_plan(SharedArgs& a) {
   const int grp = a.H / a.G;
   auto tiles = [&](int64_t rows) { return (int)((rows * grp + 31) / 32); };
@@ -426,16 +485,19 @@ void shared_plan(SharedArgs& a) {
   a.own_few = to <= 1;
   a.shared_groups = a.shared_few ? 1 : (ts + 3) / 4;
   a.own_groups = a.own_few ? 1 : (to + 3) / 4;
-  auto splits = [&](int64_t base, int pages) {
-    const int64_t want = (512 + base - 1) / base, most = (pages + kChunk - 1) / kChunk;
-    return (int)std::max<int64_t>(std::min<int64_t>({want, most, 64}), 1);
-  };
-  a.shared_splits = prefix ? splits((int64_t)a.n_groups * a.G * a.shared_groups, a.max_pages) : 0;
-  a.own_splits = splits((int64_t)a.b.n_seqs * a.G * a.own_groups, (a.b.max_ctx + kPage - 1) / kPage);
+  const int shared = prefix ? a.max_pages : 0, all = (a.b.max_ctx + kPage - 1) / kPage;
+  const int64_t base_s = prefix ? (int64_t)a.n_groups * a.G * a.shared_groups : 0;
+  const int64_t base_o = (int64_t)a.b.n_seqs * a.G * a.own_groups;
+  const int own = std::max(all - shared, 1);
+  int chunk = std::max(kChunk, (std::max(shared, all) + 63) / 64);
+  while (chunk < std::max(shared, own) &&
+         base_s * ((shared + chunk - 1) / chunk) + base_o * ((own + chunk - 1) / chunk) > kWorkgroups)
+    chunk += 4;
+  a.shared_splits = prefix ? (shared + chunk - 1) / chunk : 0;
+  a.own_splits = (own + chunk - 1) / chunk;
   a.parts = a.shared_splits + a.own_splits;
-  a.shared_jobs64 = prefix ? (int64_t)a.n_groups * a.G * a.shared_groups * a.shared_splits : 0;
-  a.own_jobs64 = (int64_t)a.b.n_seqs * a.G * a.own_groups * a.own_splits;
-  if (!prefix) a.shared_splits = 0;
+  a.shared_jobs64 = base_s * a.shared_splits;
+  a.own_jobs64 = base_o * a.own_splits;
 }
 
 template <typename T> static hipError_t shared_type(const SharedArgs& a, hipStream_t st) {

@@ -1380,6 +1380,8 @@ extern "C" jf_status jf_policy_loss(const jf_policy* policy, int32_t n_seqs, int
   a.stats = d_stats; a.g_lp = d_g_logprob; a.g_entropy = d_g_entropy;
   a.ws = d_ws;
   a.flags = d_flags;
+  a.vec = aligned16(d_tokens) && aligned16(d_logprob) && aligned16(d_old_logprob) && aligned16(d_ref_logprob) &&
+          aligned16(d_entropy) && (!a.adv_rows || aligned16(d_advantage)) && aligned16(d_g_logprob) && aligned16(d_g_entropy);
   HIP_TRY(launch_policy(a, (hipStream_t)stream));
   return JF_OK;
 }

@@ -425,6 +425,7 @@ struct PolicyArgs {
   float *stats, *g_lp, *g_entropy;               // the gradients may be null
   void* ws;
   int32_t* flags;
+  int vec;                                       // all row arrays start on 16-byte boundaries
   int blocks;
 };
 size_t policy_ws_bytes(int n_seqs, int n_rows);

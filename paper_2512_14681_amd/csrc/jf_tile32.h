@@ -142,51 +142,55 @@ template <> __device__ __forceinline__ bool all_finite<bf16_t>(uint32_t top) {
 }
 template <> __device__ __forceinline__ bool all_finite<float>(uint32_t top) { return top < 0x7F800000u; }
 
-// An operand with its infinities and NaN as 0; where they were, 1 in `up` (+inf
-// and NaN) and in `down` (-inf and NaN), which have 0 elsewhere.
-__device__ __forceinline__ void part_finite(const Frag<bf16_t>& f, Frag<bf16_t>& clean, Frag<bf16_t>& up, Frag<bf16_t>& down) {
-  const uint32_t w[4] = {f.v.x, f.v.y, f.v.z, f.v.w};
-  uint32_t c[4], u[4], d[4];
+// An operand with its infinities and NaN as 0.
+__device__ __forceinline__ void keep_finite(Frag<bf16_t>& f) {
+  uint32_t w[4] = {f.v.x, f.v.y, f.v.z, f.v.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    c[i] = u[i] = d[i] = 0;
-#pragma unroll
-    for (int s = 0; s < 32; s += 16) {
-      const uint32_t x = (w[i] >> s) & 0xFFFFu, one = 0x3F80u << s;
-      const bool bad = (x & 0x7F80u) == 0x7F80u;
-      c[i] |= bad ? 0u : x << s;
-      u[i] |= bad && x != 0xFF80u ? one : 0u;
-      d[i] |= bad && x != 0x7F80u ? one : 0u;
-    }
+    w[i] = (w[i] & 0x7F80u) == 0x7F80u ? w[i] & 0xFFFF0000u : w[i];
+    w[i] = (w[i] & 0x7F800000u) == 0x7F800000u ? w[i] & 0xFFFFu : w[i];
   }
-  clean.v = make_uint4(c[0], c[1], c[2], c[3]);
-  up.v = make_uint4(u[0], u[1], u[2], u[3]);
-  down.v = make_uint4(d[0], d[1], d[2], d[3]);
+  f.v = make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void part_finite(const Frag<float>& f, Frag<float>& clean, Frag<float>& up, Frag<float>& down) {
-  float x[8] = {f.lo.x, f.lo.y, f.lo.z, f.lo.w, f.hi.x, f.hi.y, f.hi.z, f.hi.w}, u[8], d[8];
+__device__ __forceinline__ void keep_finite(Frag<float>& f) {
+  float x[8] = {f.lo.x, f.lo.y, f.lo.z, f.lo.w, f.hi.x, f.hi.y, f.hi.z, f.hi.w};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const bool bad = (__float_as_uint(x[i]) & 0x7F800000u) == 0x7F800000u;
-    u[i] = bad && x[i] != -INFINITY ? 1.f : 0.f;
-    d[i] = bad && x[i] != INFINITY ? 1.f : 0.f;
-    x[i] = bad ? 0.f : x[i];
+  for (int i = 0; i < 8; ++i) x[i] = (__float_as_uint(x[i]) & 0x7F800000u) == 0x7F800000u ? 0.f : x[i];
+  frag_of(x, f);
+}
+// 1 where an operand is NaN or the infinity with that sign bit, else 0.
+__device__ __forceinline__ void mark_infinite(const Frag<bf16_t>& f, uint32_t sign, Frag<bf16_t>& mark) {
+  const uint32_t w[4] = {f.v.x, f.v.y, f.v.z, f.v.w}, other = 0x7F80u | (sign ? 0u : 0x8000u);
+  uint32_t m[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = w[i] & 0xFFFFu, hi = w[i] >> 16;
+    m[i] = (lo & 0x7F80u) == 0x7F80u && lo != other ? 0x3F80u : 0u;
+    m[i] |= (hi & 0x7F80u) == 0x7F80u && hi != other ? 0x3F800000u : 0u;
   }
-  frag_of(x, clean);
-  frag_of(u, up);
-  frag_of(d, down);
+  mark.v = make_uint4(m[0], m[1], m[2], m[3]);
 }
-// Adds to a column's outputs what it sees (1 in `seen`) of such values: an
-// infinity, or NaN.
-template <typename T>
-__device__ __forceinline__ void add_infinite(f32x16_t& o, const Frag<T>& up, const Frag<T>& down, const Frag<T>& seen) {
-  f32x16_t ups = zero16(), downs = zero16();
-  mfma32(ups, up, seen);
-  mfma32(downs, down, seen);
+__device__ __forceinline__ void mark_infinite(const Frag<float>& f, uint32_t sign, Frag<float>& mark) {
+  float x[8] = {f.lo.x, f.lo.y, f.lo.z, f.lo.w, f.hi.x, f.hi.y, f.hi.z, f.hi.w};
+  const float other = sign ? INFINITY : -INFINITY;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    if (ups[i] > 0.f) o[i] += INFINITY;
-    if (downs[i] > 0.f) o[i] -= INFINITY;
+  for (int i = 0; i < 8; ++i) x[i] = (__float_as_uint(x[i]) & 0x7F800000u) == 0x7F800000u && x[i] != other ? 1.f : 0.f;
+  frag_of(x, mark);
+}
+// Adds to a column's outputs what it sees (1 in `seen`) of an operand's
+// infinities and NaN.  A rare path: its parts run one after the other, so that
+// it costs the common one no registers.
+template <typename T> __device__ __forceinline__ void add_infinite(f32x16_t& o, const Frag<T>& f, const Frag<T>& seen) {
+#pragma unroll
+  for (int sign = 0; sign < 2; ++sign) {
+    __builtin_amdgcn_sched_barrier(0);
+    Frag<T> mark;
+    mark_infinite(f, sign, mark);
+    f32x16_t hit = zero16();
+    mfma32(hit, mark, seen);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[i] += hit[i] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
