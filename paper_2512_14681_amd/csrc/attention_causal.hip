@@ -115,8 +115,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalAr
   const T* kp = reinterpret_cast<const T*>(a.k) + (size_t)b.r0 * a.ld_k + w.g * HD;
   const T* vp = reinterpret_cast<const T*>(a.v) + (size_t)b.r0 * a.ld_v + w.g * HD;
   auto load = [&](int j0, int buf) {
-    Loader::load(kp + (size_t)j0 * a.ld_k, a.ld_k, last - j0, s_kv[buf][0]);
-    Loader::load(vp + (size_t)j0 * a.ld_v, a.ld_v, last - j0, s_kv[buf][1]);
+    Loader::load(kp + (size_t)j0 * a.ld_k, a.ld_k * sizeof(T), last - j0, s_kv[buf][0]);
+    Loader::load(vp + (size_t)j0 * a.ld_v, a.ld_v * sizeof(T), last - j0, s_kv[buf][1]);
   };
   load(0, 0);
   Frag<T> q[NS];
@@ -124,6 +124,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalAr
     const T* p = reinterpret_cast<const T*>(a.q) + (size_t)(b.r0 + qi) * a.ld_q + head * HD + 8 * h;
 #pragma unroll
     for (int s = 0; s < NS; ++s) q[s] = row_frag<T>(p + 16 * s, kVec);
+    settle(q);
   }
   const float c = kLog2e / sqrtf((float)HD);
   float m = -INFINITY, l = 0.f;
@@ -138,7 +139,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalAr
     if constexpr (kVec) wait_vm<0>();
     __syncthreads();
     if (j0 + kRows <= last) load(j0 + kRows, buf ^ 1);
-    const char *keys = s_kv[buf][0], *values = s_kv[buf][1];
+    const uint32_t keys = Tile::row_base(lds_address(s_kv[buf][0])), values = Tile::column_base(lds_address(s_kv[buf][1]));
     buf ^= 1;
     if (kEdge && j0 > q0 + 31) return;
     f32x16_t st[KT];
@@ -245,30 +246,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalAr
 
 // ---- gradient ------------------------------------------------------------------------
 
-// Of each row and head: log2 of its softmax's denominator in the scores' units
-// (infinite for a row without weights, whose weights then are 0), and D.
-template <typename T>
-__global__ void __launch_bounds__(256) k_causal_dots(CausalGradArgs a) {
-  const int per = a.f.hd / 8, items = 256 / per;   // threads of a row and head
-  const int64_t item = (int64_t)blockIdx.x * items + threadIdx.x / per;
-  const int first = a.f.row_start[0], end = a.f.row_start[a.f.n_seqs];
-  const int row = (int)(item / a.f.H), head = (int)(item % a.f.H), d = threadIdx.x % per * 8;
-  const bool valid = row < a.f.n_rows && row >= first && row < end;
-  float sum = 0.f;
-  if (valid) {
-    const Frag<T> x = row_frag<T>(reinterpret_cast<const T*>(a.f.out) + (size_t)row * a.f.ld_out + head * a.f.hd + d, a.vec_dot);
-    const Frag<T> y = row_frag<T>(reinterpret_cast<const T*>(a.g_out) + (size_t)row * a.ld_g_out + head * a.f.hd + d, a.vec_dot);
-    const T *xs = reinterpret_cast<const T*>(&x), *ys = reinterpret_cast<const T*>(&y);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(to_f32<T>(xs[e]), to_f32<T>(ys[e]), sum);
-  }
-  for (int s = 1; s < per; s *= 2) sum += __shfl_xor(sum, s);
-  if (valid && d == 0) {
-    const float lse = a.f.lse[(size_t)head * a.f.n_rows + row];
-    a.dots[(size_t)head * a.f.n_rows + row] = make_float2(lse == -INFINITY ? INFINITY : lse * kLog2e, sum);
-  }
-}
-
+// dq; and of each row and head, for dk and dv, what the accumulators of its
+// scores and of do v start from: -lse sqrt(hd) (-inf for a row without
+// weights, whose weights then are 0), and -D.
 template <typename T, int HD, bool kVec>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dq(CausalGradArgs a) {
   using Tile = RowTile<T, HD>;
@@ -288,8 +268,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dq(Causa
   const T* kp = reinterpret_cast<const T*>(a.f.k) + (size_t)b.r0 * a.f.ld_k + w.g * HD;
   const T* vp = reinterpret_cast<const T*>(a.f.v) + (size_t)b.r0 * a.f.ld_v + w.g * HD;
   auto load = [&](int j0, int buf) {
-    Loader::load(kp + (size_t)j0 * a.f.ld_k, a.f.ld_k, last - j0, s_kv[buf][0]);
-    Loader::load(vp + (size_t)j0 * a.f.ld_v, a.f.ld_v, last - j0, s_kv[buf][1]);
+    Loader::load(kp + (size_t)j0 * a.f.ld_k, a.f.ld_k * sizeof(T), last - j0, s_kv[buf][0]);
+    Loader::load(vp + (size_t)j0 * a.f.ld_v, a.f.ld_v * sizeof(T), last - j0, s_kv[buf][1]);
   };
   load(0, 0);
   Frag<T> q[NS], g[NS];
@@ -301,9 +281,28 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dq(Causa
       q[s] = row_frag<T>(p + 16 * s, kVec);
       g[s] = row_frag<T>(r + 16 * s, kVec);
     }
+    settle(q);
+    settle(g);
   }
-  const float2 dots = a.dots[(size_t)head * a.f.n_rows + b.r0 + qi];
   const float c = kLog2e / sqrtf((float)HD);
+  float lse, dot = 0.f;
+  {
+    const T* p = reinterpret_cast<const T*>(a.f.out) + (size_t)(b.r0 + qi) * a.f.ld_out + head * HD + 8 * h;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const Frag<T> x = row_frag<T>(p + 16 * s, a.vec_dot);
+      float xs[8], gs[8];
+      frag_values(x, xs);
+      frag_values(g[s], gs);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(xs[e], gs[e], dot);
+    }
+    dot = pair_sum(dot);
+    const size_t at = (size_t)head * a.f.n_rows + b.r0 + qi;
+    lse = a.f.lse[at];
+    if (h == 0 && q0 + lane < b.n) a.dots[at] = make_float2(lse == -INFINITY ? -INFINITY : -lse * sqrtf((float)HD), -dot);
+    lse = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  }
   f32x16_t dq[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) dq[d] = zero16();
@@ -314,7 +313,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dq(Causa
     if constexpr (kVec) wait_vm<0>();
     __syncthreads();
     if (j0 + kRows <= last) load(j0 + kRows, buf ^ 1);
-    const char *keys = s_kv[buf][0], *values = s_kv[buf][1];
+    const uint32_t keys = Tile::row_base(lds_address(s_kv[buf][0])), values = Tile::row_base(lds_address(s_kv[buf][1]));
+    const uint32_t key_columns = Tile::column_base(lds_address(s_kv[buf][0]));
     buf ^= 1;
     if (kEdge && j0 > q0 + 31) return;
     const int lim = qi - j0 - 4 * h;
@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dq(Causa
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float ds = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i], c, -dots.x)) * (dp[i] - dots.y);
+        const float ds = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i], c, -lse)) * (dp[i] - dot);
         st[i] = kEdge && 32 * kt + acc_row(i) > lim ? 0.f : ds;
       }
 #pragma unroll
@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dq(Causa
         Frag<T> pf;
         frag_of(p, pf);
 #pragma unroll
-        for (int d = 0; d < ND; ++d) mfma32(dq[d], Tile::columns(keys, 32 * kt + 16 * j, d), pf);
+        for (int d = 0; d < ND; ++d) mfma32(dq[d], Tile::columns(key_columns, 32 * kt + 16 * j, d), pf);
       }
     }
   };
@@ -396,17 +396,17 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dkv(Caus
   // The steps: every head's rows from the block's first key on, one head after the other.
   const int first = b.t * kBlock, steps = (b.n - first + kRows - 1) / kRows;
   int head = w.g * grp + part, i0 = first;
-  float2 dots = make_float2(INFINITY, 0.f);
+  float2 dots = make_float2(-INFINITY, 0.f);
   auto load = [&](int buf) {
     const int row = i0 + (int)threadIdx.x;
     if ((int)threadIdx.x < kRows) {
-      dots = make_float2(INFINITY, 0.f);
+      dots = make_float2(-INFINITY, 0.f);
       if (row < b.n) dots = a.dots[(size_t)head * a.f.n_rows + b.r0 + row];
     }
-    Loader::load(reinterpret_cast<const T*>(a.f.q) + (size_t)(b.r0 + i0) * a.f.ld_q + head * HD, a.f.ld_q, b.n - 1 - i0,
-                 s_qg[buf][0]);
-    Loader::load(reinterpret_cast<const T*>(a.g_out) + (size_t)(b.r0 + i0) * a.ld_g_out + head * HD, a.ld_g_out,
-                 b.n - 1 - i0, s_qg[buf][1]);
+    Loader::load(reinterpret_cast<const T*>(a.f.q) + (size_t)(b.r0 + i0) * a.f.ld_q + head * HD, a.f.ld_q * sizeof(T),
+                 b.n - 1 - i0, s_qg[buf][0]);
+    Loader::load(reinterpret_cast<const T*>(a.g_out) + (size_t)(b.r0 + i0) * a.ld_g_out + head * HD,
+                 a.ld_g_out * sizeof(T), b.n - 1 - i0, s_qg[buf][1]);
     i0 += kRows;
     if (i0 >= b.n) {
       i0 = first;
@@ -421,6 +421,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dkv(Caus
   };
   load(0);
   put_dots(0);
+  settle(k);
+  settle(v);
   const int heads = (grp - part + a.parts - 1) / a.parts, total = heads * steps;
   int at = first, buf = 0;
 #pragma unroll 1
@@ -428,31 +430,35 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dkv(Caus
     if constexpr (kVec) wait_vm<0>();
     __syncthreads();
     if (it + 1 < total) load(buf ^ 1);
-    const char *qs = s_qg[buf][0], *gs = s_qg[buf][1];
+    const uint32_t qs = Tile::row_base(lds_address(s_qg[buf][0])), gs = Tile::row_base(lds_address(s_qg[buf][1]));
+    const uint32_t q_columns = Tile::column_base(lds_address(s_qg[buf][0]));
+    const uint32_t g_columns = Tile::column_base(lds_address(s_qg[buf][1]));
     const bool edge = at < k0 + 31;  // rows before some of the wave's keys
     if (at + kRows > k0) {
-#pragma unroll
+#pragma unroll 1
       for (int kt = 0; kt < KT; ++kt) {
-        f32x16_t st = zero16(), dp = zero16();
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          mfma32(st, Tile::rows(qs, 32 * kt, s), k[s]);
-          mfma32(dp, Tile::rows(gs, 32 * kt, s), v[s]);
-        }
-        const int lim = ki - at - 32 * kt - 4 * h;
+        constexpr int kSkip = 32 * Tile::kRowBytes;
+        f32x16_t st, dp;
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
           const float4 x = *reinterpret_cast<const float4*>(&s_dots[buf][0][32 * kt + acc_row(i) + 4 * h]);
           const float4 y = *reinterpret_cast<const float4*>(&s_dots[buf][1][32 * kt + acc_row(i) + 4 * h]);
-          const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+          st[i] = x.x; st[i + 1] = x.y; st[i + 2] = x.z; st[i + 3] = x.w;
+          dp[i] = y.x; dp[i + 1] = y.y; dp[i + 2] = y.z; dp[i + 3] = y.w;
+        }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const bool hidden = edge && acc_row(i + e) < lim;
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i + e], c, -xs[e]));
-            const float ds = p * (dp[i + e] - ys[e]);
-            st[i + e] = hidden ? 0.f : p;
-            dp[i + e] = hidden ? 0.f : ds;
-          }
+        for (int s = 0; s < NS; ++s) {
+          mfma32(st, Tile::rows(qs + kt * kSkip, 0, s), k[s]);
+          mfma32(dp, Tile::rows(gs + kt * kSkip, 0, s), v[s]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const int lim = ki - at - 32 * kt - 4 * h;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const bool hidden = edge && acc_row(i) < lim;
+          st[i] = __builtin_amdgcn_exp2f(st[i] * c);
+          dp[i] = hidden ? 0.f : st[i] * dp[i];
+          st[i] = hidden ? 0.f : st[i];
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -467,9 +473,10 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dkv(Caus
           frag_of(y, df);
 #pragma unroll
           for (int d = 0; d < ND; ++d) {
-            mfma32(dv[d], Tile::columns(gs, 32 * kt + 16 * j, d), pf);
-            mfma32(dk[d], Tile::columns(qs, 32 * kt + 16 * j, d), df);
+            mfma32(dv[d], Tile::columns(g_columns + kt * kSkip, 16 * j, d), pf);
+            mfma32(dk[d], Tile::columns(q_columns + kt * kSkip, 16 * j, d), df);
           }
+          
         }
       }
     }
@@ -557,22 +564,18 @@ hipError_t launch_causal(int dtype, const CausalArgs& a, hipStream_t st) {
 template <typename T, int HD> static void causal_grad_vec(const CausalGradArgs& a, hipStream_t st) {
   const unsigned dq = work_grid(a.f.blocks, a.f.G, a.f.H / a.f.G), dkv = work_grid(a.f.blocks, a.f.G, a.parts);
   if (a.f.vec) {
-    k_causal_dkv<T, HD, true><<<dkv, 256, 0, st>>>(a);
     k_causal_dq<T, HD, true><<<dq, 256, 0, st>>>(a);
+    k_causal_dkv<T, HD, true><<<dkv, 256, 0, st>>>(a);
   } else {
-    k_causal_dkv<T, HD, false><<<dkv, 256, 0, st>>>(a);
     k_causal_dq<T, HD, false><<<dq, 256, 0, st>>>(a);
+    k_causal_dkv<T, HD, false><<<dkv, 256, 0, st>>>(a);
   }
 }
 template <typename T> static hipError_t causal_grad_hd(const CausalGradArgs& a, hipStream_t st) {
-  const int64_t items = (int64_t)a.f.n_rows * a.f.H * (a.f.hd / 8);
-  k_causal_dots<T><<<(unsigned)((items + 255) / 256), 256, 0, st>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
   if (a.f.hd == 32) causal_grad_vec<T, 32>(a, st);
   else if (a.f.hd == 64) causal_grad_vec<T, 64>(a, st);
   else causal_grad_vec<T, 128>(a, st);
-  e = hipGetLastError();
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.parts == 1) return e;
   const int64_t quads = (int64_t)a.f.n_rows * a.f.G * a.f.hd / 4;
   k_causal_join<T><<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(a);

@@ -39,6 +39,11 @@ __device__ __forceinline__ void load_query(const bf16_t* p, size_t plane, Query<
   q.lo = frag_load<bf16_t>(p + plane);
 }
 __device__ __forceinline__ void load_query(const float* p, size_t, Query<float>& q) { q.v = frag_load<float>(p); }
+__device__ __forceinline__ void settle_query(Query<bf16_t>& q) {
+  settle(reinterpret_cast<Frag<bf16_t>(&)[1]>(q.hi));
+  settle(reinterpret_cast<Frag<bf16_t>(&)[1]>(q.lo));
+}
+__device__ __forceinline__ void settle_query(Query<float>& q) { settle(reinterpret_cast<Frag<float>(&)[1]>(q.v)); }
 __device__ __forceinline__ void split_query(const float* x, Query<bf16_t>& q) {
   split2(x[0], x[1], q.hi.v.x, q.lo.v.x);
   split2(x[2], x[3], q.hi.v.y, q.lo.v.y);
@@ -103,6 +108,8 @@ template <typename T, int HD> struct SharedTile {
     const T* p = reinterpret_cast<const T*>(a.q) + ((size_t)(r0 + qi) * a.H + qhd) * HD + 8 * (lane >> 5);
 #pragma unroll
     for (int s = 0; s < NS; ++s) load_query(p + 16 * s, a.q_plane, q[s]);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) settle_query(q[s]);
     m = -INFINITY;
     l = 0.f;
 #pragma unroll
@@ -113,9 +120,11 @@ template <typename T, int HD> struct SharedTile {
   // holds a bit for each that the lane's query sees.  False if there were
   // values that are not finite, which count as 0 here.
   template <int KT, bool kEdge>
-  __device__ __forceinline__ bool step(const char* keys, const char* values, uint64_t seen) {
+  __device__ __forceinline__ bool step(const char* tile, uint64_t seen) {
     using Keys = RowTile<T, HD>;
     using Values = RowTile<T, 32 * KT>;
+    const uint32_t keys = Keys::row_base(lds_address(tile));
+    const uint32_t values = Values::row_base(lds_address(tile) + 32 * KT * Keys::kRowBytes);
     const float c = kLog2e / sqrtf((float)HD);
     f32x16_t st[KT];
 #pragma unroll
@@ -188,7 +197,8 @@ template <typename T, int HD> struct SharedTile {
     return finite;
   }
   // What the queries see of infinities and NaN among the values that step left out.
-  template <int KT> __device__ __forceinline__ void infinite(const char* values, uint64_t seen) {
+  template <int KT> __device__ __forceinline__ void infinite(const char* tile, uint64_t seen) {
+    const uint32_t values = RowTile<T, 32 * KT>::row_base(lds_address(tile) + 32 * KT * RowTile<T, HD>::kRowBytes);
     seen >>= 8 * ((threadIdx.x & 63) >> 5);
 #pragma unroll 1
     for (int j = 0; j < 2 * KT; ++j) {
@@ -213,23 +223,25 @@ template <typename T, int HD, int KT, int W> struct PageLoader {
     constexpr int kPieces = 32 * KT * kKeyRow / 1024 / W;
     static_assert(kPieces * W * 1024 == 32 * KT * kKeyRow, "whole pieces");
     constexpr int kKeyRows = 1024 / kKeyRow, kValueRows = 1024 / kValueRow;  // rows of a 1 KB piece
-    static_assert(kKeyRows <= 16 && kValueRows >= 8, "places repeat after 16 keys and 8 dims");
+    static_assert(kKeyRows <= 16 && kValueRows <= 16, "places repeat after 16 rows");
     const int lane = threadIdx.x & 63;
     const uint32_t at = lds_address(tile) + wave * 1024;
-    // Few offsets in registers: they repeat every 16 keys (every 8 dims), the rest is the same for all lanes.
-    constexpr int kPeriod = std::max(16 / (kKeyRows * W), 1);
+    // Few offsets in registers: they repeat every 16 rows, the rest is the same for all lanes.
+    constexpr int kKeyPeriod = std::max(16 / (kKeyRows * W), 1), kValuePeriod = std::max(16 / (kValueRows * W), 1);
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int row = ((i % kPeriod * W + wave) * kKeyRows) % 16 + lane * 16 / kKeyRow;
+      const int row = ((i % kKeyPeriod * W + wave) * kKeyRows) % 16 + lane * 16 / kKeyRow;
       const int c = (lane * 16 % kKeyRow / 16) ^ turn<kKeyRow>(row), key = (row & ~12) | ((row & 4) << 1) | ((row & 8) >> 1);
       const int skip = (i * W + wave) * kKeyRows / 16 * 16;
       dma_1k<false>(reinterpret_cast<const char*>(keys + (size_t)t0 * HD) + skip * kKeyRow, key * kKeyRow + c * 16, at + i * W * 1024);
     }
-    const int row = lane * 16 / kValueRow, c = (lane * 16 % kValueRow / 16) ^ turn<kValueRow>(row);
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i)
-      dma_1k<false>(reinterpret_cast<const char*>(values + t0) + (i * W + wave) * kValueRows * kValueStride,
-                    row * kValueStride + c * 16, at + 32 * KT * kKeyRow + i * W * 1024);
+    for (int i = 0; i < kPieces; ++i) {
+      const int row = ((i % kValuePeriod * W + wave) * kValueRows) % 16 + lane * 16 / kValueRow;
+      const int c = (lane * 16 % kValueRow / 16) ^ turn<kValueRow>(row), skip = (i * W + wave) * kValueRows / 16 * 16;
+      dma_1k<false>(reinterpret_cast<const char*>(values + t0) + skip * kValueStride, row * kValueStride + c * 16,
+                    at + 32 * KT * kKeyRow + i * W * 1024);
+    }
   }
 };
 
@@ -325,16 +337,16 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_share
     int p = p0 + wave;
 #pragma unroll 1
     for (; p < whole; p += 4)
-      page(std::false_type{}, p, [&](const char* t, uint64_t bits) { w.template step<1, false>(t, t + kOne / 2, bits); });
+      page(std::false_type{}, p, [&](const char* t, uint64_t bits) { w.template step<1, false>(t, bits); });
     const int edges = p;
 #pragma unroll 1
     for (; p < p1; p += 4)
       page(std::true_type{}, p,
-           [&](const char* t, uint64_t bits) { finite &= w.template step<1, true>(t, t + kOne / 2, bits); });
+           [&](const char* t, uint64_t bits) { finite &= w.template step<1, true>(t, bits); });
     if (!finite)
 #pragma unroll 1
       for (p = edges; p < p1; p += 4)
-        page(std::true_type{}, p, [&](const char* t, uint64_t bits) { w.template infinite<1>(t + kOne / 2, bits); });
+        page(std::true_type{}, p, [&](const char* t, uint64_t bits) { w.template infinite<1>(t, bits); });
     // The waves' parts, dims by queries; each wave merges a quarter of the dims.
     w.l = pair_sum(w.l);
     __syncthreads();
@@ -402,12 +414,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_share
     __syncthreads();
   };
   bool finite = true;
-  pages(std::false_type{}, p0, whole, [&](const char* t, uint64_t bits) { w.template step<KT, false>(t, t + kTile / 2, bits); });
+  pages(std::false_type{}, p0, whole, [&](const char* t, uint64_t bits) { w.template step<KT, false>(t, bits); });
   if (whole < p1) {
     pages(std::true_type{}, whole, p1,
-          [&](const char* t, uint64_t bits) { finite &= w.template step<KT, true>(t, t + kTile / 2, bits); });
+          [&](const char* t, uint64_t bits) { finite &= w.template step<KT, true>(t, bits); });
     if (__syncthreads_or(!finite))
-      pages(std::true_type{}, whole, p1, [&](const char* t, uint64_t bits) { w.template infinite<KT>(t + kTile / 2, bits); });
+      pages(std::true_type{}, whole, p1, [&](const char* t, uint64_t bits) { w.template infinite<KT>(t, bits); });
   }
   if (!w.valid) return;
   w.l = pair_sum(w.l);

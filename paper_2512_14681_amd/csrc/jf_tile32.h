@@ -41,6 +41,20 @@ __device__ __forceinline__ void frag_of(const float* x, Frag<float>& f) {
   f.hi = make_float4(x[4], x[5], x[6], x[7]);
 }
 
+// The values of an operand.
+__device__ __forceinline__ void frag_values(const Frag<bf16_t>& f, float (&x)[8]) {
+  const uint32_t w[4] = {f.v.x, f.v.y, f.v.z, f.v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void frag_values(const Frag<float>& f, float (&x)[8]) {
+  x[0] = f.lo.x; x[1] = f.lo.y; x[2] = f.lo.z; x[3] = f.lo.w;
+  x[4] = f.hi.x; x[5] = f.hi.y; x[6] = f.hi.z; x[7] = f.hi.w;
+}
+
 // Maximum over, and sum over, the two lanes that hold one column.
 __device__ __forceinline__ float pair_max(float v) {
   const uint32_t u = __float_as_uint(v);
@@ -54,10 +68,13 @@ __device__ __forceinline__ float pair_sum(float v) {
 }
 
 // A tile of rows in LDS, kRowBytes each, in 16-byte chunks: chunk c of row r
-// lies at place c ^ turn(r) of its row.  Eight rows' chunks of one column, and
-// four rows' pairs of chunks, then lie in different banks.
+// lies at place c ^ turn(r) of its row.  16 rows' chunks of one column, and
+// four rows' runs of four chunks, then fill the 64 banks (with turns that
+// tell apart 8 rows only, half of the cycles of LDS reads were conflicts).
 template <int kRowBytes> __device__ __forceinline__ constexpr int turn(int r) {
-  return kRowBytes >= 256 ? ((r & 3) << 1) | ((r >> 2) & 1) : kRowBytes == 128 ? ((r >> 1) & 3) << 1 : ((r >> 2) & 1) << 1;
+  return kRowBytes >= 256   ? ((r & 3) << 2) | ((r >> 2) & 3)
+         : kRowBytes == 128 ? ((r & 2) << 1) | ((r >> 2) & 3)
+                            : (r >> 2) & 3;
 }
 
 typedef __attribute__((address_space(3))) char lds_char_t;
@@ -65,57 +82,62 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(lds_char_t*)reinterpret_cast<char*>(const_cast<void*>(p));
 }
 
-// Operand reads from a row-major tile [rows][HD] of T.
+// Operand reads from a row-major tile [rows][HD] of T.  `base` is the tile's
+// LDS address (a multiple of 1024) plus the lane's part of the place, for all
+// reads of a tile the same: what else there is to it are constants, exclusive
+// or'ed where chunks are turned, and few registers hold addresses.
 template <typename T, int HD> struct RowTile {
   static constexpr int kRowBytes = HD * (int)sizeof(T);
-  static constexpr int kChunks = kRowBytes / 16;
-  static_assert(kChunks >= 4, "a row holds four chunks or more");
+  static_assert(kRowBytes >= 64, "a row holds four chunks or more");
+  template <typename V> static __device__ __forceinline__ V at(uint32_t address) {
+    return *reinterpret_cast<__attribute__((address_space(3))) V*>((uintptr_t)address);
+  }
 
-  // Rows r0 + l % 32 (r0 a multiple of 8), dims 16 s + 8 (l / 32) .. + 7.
-  static __device__ __forceinline__ Frag<T> rows(const char* tile, int r0, int s) {
+  // Rows r0 + l % 32 (r0 a multiple of 16), dims 16 s + 8 (l / 32) .. + 7.
+  static __device__ __forceinline__ uint32_t row_base(uint32_t tile) {
     const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
-    const char* p = tile + (r0 + r) * kRowBytes;
+    return tile + r * kRowBytes + (((sizeof(T) == 2 ? h : 2 * h) ^ turn<kRowBytes>(r)) << 4);
+  }
+  static __device__ __forceinline__ Frag<T> rows(uint32_t base, int r0, int s) {
     if constexpr (sizeof(T) == 2) {
-      Frag<T> f;
-      f.v = *reinterpret_cast<const uint4*>(p + (((2 * s + h) ^ turn<kRowBytes>(r)) << 4));
-      return f;
+      return Frag<T>{__builtin_bit_cast(uint4, at<u32x4_t>((base ^ (s << 5)) + r0 * kRowBytes))};
     } else {
-      Frag<T> f;
-      f.lo = *reinterpret_cast<const float4*>(p + (((4 * s + 2 * h) ^ turn<kRowBytes>(r)) << 4));
-      f.hi = *reinterpret_cast<const float4*>(p + (((4 * s + 2 * h + 1) ^ turn<kRowBytes>(r)) << 4));
-      return f;
+      return Frag<T>{__builtin_bit_cast(float4, at<f32x4v_t>((base ^ (s << 6)) + r0 * kRowBytes)),
+                     __builtin_bit_cast(float4, at<f32x4v_t>((base ^ (s << 6 | 16)) + r0 * kRowBytes))};
     }
   }
   // The transposed tile: dims 32 t + l % 32, of the 16 tile rows from r0 (a
-  // multiple of 8) those that a result's elements 0 .. 7 stand for:
-  // r0 + 8 (e / 4) + 4 (l / 32) + e % 4.
-  static __device__ __forceinline__ Frag<T> columns(const char* tile, int r0, int t) {
+  // multiple of 16) those that a result's elements 0 .. 7 stand for:
+  // r0 + 8 (e / 4) + 4 (l / 32) + e % 4.  bf16: a group of 16 lanes reads 4
+  // rows of 16 dims, and each lane gets its dim of the 4 rows.
+  static __device__ __forceinline__ uint32_t column_base(uint32_t tile) {
     const int lane = threadIdx.x & 63, h = lane >> 5;
     if constexpr (sizeof(T) == 2) {
-      // a group of 16 lanes reads 4 rows of 16 dims, and each lane gets its dim of the 4 rows
-      const int i = lane & 15, g = (lane >> 4) & 1, r = 4 * h + (i >> 2);
-      const char* p = tile + (r0 + r) * kRowBytes + (((4 * t + 2 * g + ((i & 3) >> 1)) ^ turn<kRowBytes>(r)) << 4) + (i & 1) * 8;
-      typedef short s16x4_t __attribute__((ext_vector_type(4)));
-      typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
-      const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(lds_char_t*)const_cast<char*>(p)));
-      const uint2 b = __builtin_bit_cast(
-          uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(lds_char_t*)const_cast<char*>(p + 8 * kRowBytes)));
-      Frag<T> f;
-      f.v = make_uint4(a.x, a.y, b.x, b.y);
-      return f;
+      const int i = lane & 15, r = 4 * h + (i >> 2), c = ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
+      return tile + r * kRowBytes + ((c ^ turn<kRowBytes>(r)) << 4) + (i & 1) * 8;
     } else {
       const int d = lane & 31;
+      return tile + 4 * h * kRowBytes + (((d >> 2) ^ turn<kRowBytes>(4 * h)) << 4) + (d & 3) * 4;
+    }
+  }
+  static __device__ __forceinline__ Frag<T> columns(uint32_t base, int r0, int t) {
+    if constexpr (sizeof(T) == 2) {
+      typedef short s16x4_t __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+      auto read = [&](int row) {  // 8 more rows turn the chunks by 2 more
+        const uint32_t a = (base ^ (t << 6) ^ (turn<kRowBytes>(row) << 4)) + (r0 + row) * kRowBytes;
+        return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(uintptr_t)a));
+      };
+      const uint2 a = read(0), b = read(8);
+      return Frag<T>{make_uint4(a.x, a.y, b.x, b.y)};
+    } else {
       float x[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int r = 8 * (e / 4) + 4 * h + e % 4;
-        x[e] = *reinterpret_cast<const float*>(tile + (r0 + r) * kRowBytes + (((8 * t + (d >> 2)) ^ turn<kRowBytes>(r)) << 4) +
-                                               (d & 3) * 4);
+        const int r = 8 * (e / 4) + e % 4;
+        x[e] = at<float>((base ^ (t << 7) ^ (turn<kRowBytes>(r) << 4)) + (r0 + r) * kRowBytes);
       }
-      Frag<T> f;
-      f.lo = make_float4(x[0], x[1], x[2], x[3]);
-      f.hi = make_float4(x[4], x[5], x[6], x[7]);
-      return f;
+      return Frag<T>{make_float4(x[0], x[1], x[2], x[3]), make_float4(x[4], x[5], x[6], x[7])};
     }
   }
 };
@@ -213,6 +235,21 @@ template <> __device__ __forceinline__ Frag<float> row_frag<float>(const float* 
   return f;
 }
 
+// Operands that a loop only reads, arrived before it: the compiler's waits for
+// their loads would otherwise stay in the loop, where they wait for every
+// load in flight there too.
+template <int N> __device__ __forceinline__ void settle(Frag<bf16_t> (&f)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(f[i].v.x), "+v"(f[i].v.y), "+v"(f[i].v.z), "+v"(f[i].v.w));
+}
+template <int N> __device__ __forceinline__ void settle(Frag<float> (&f)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    asm volatile("" : "+v"(f[i].lo.x), "+v"(f[i].lo.y), "+v"(f[i].lo.z), "+v"(f[i].lo.w));
+    asm volatile("" : "+v"(f[i].hi.x), "+v"(f[i].hi.y), "+v"(f[i].hi.z), "+v"(f[i].hi.w));
+  }
+}
+
 // Brings rows of a matrix (HD of its columns, ld elements a row) into an LDS
 // tile of ROWS rows, by W waves; rows past `last` repeat row `last`.  kVec:
 // rows on 16-byte boundaries go to LDS without passing registers, and the
@@ -220,23 +257,38 @@ template <> __device__ __forceinline__ Frag<float> row_frag<float>(const float* 
 template <typename T, int HD, int ROWS, int W, bool kVec> struct RowLoader {
   static constexpr int kRowBytes = HD * (int)sizeof(T);
   static constexpr int kPieces = ROWS * kRowBytes / 1024 / W;  // 1 KB pieces a wave
-  static_assert(ROWS * kRowBytes % (1024 * W) == 0, "whole pieces");
+  static constexpr int kPieceRows = 1024 / kRowBytes;
+  static constexpr int kPeriod = kPieceRows * W >= 16 ? 1 : 16 / (kPieceRows * W);  // chunks are turned alike every 16 rows
+  static_assert(ROWS * kRowBytes % (1024 * W) == 0 && kPieceRows <= 16, "whole pieces");
 
-  static __device__ __forceinline__ void load(const T* base, size_t ld, int last, char* tile) {
+  // `stride` is ld in bytes.
+  static __device__ __forceinline__ void load(const T* base, size_t stride, int last, char* tile) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const char* p = reinterpret_cast<const char*>(base);
+    const uint32_t at = lds_address(tile) + wave * 1024;
+    auto chunk = [&](int i) {  // of the lane's row in piece i: its row within 16 of them decides
+      return (lane * 16 % kRowBytes / 16) ^ turn<kRowBytes>((i * W + wave) * kPieceRows % 16 + lane * 16 / kRowBytes);
+    };
+    if (kVec && last >= ROWS - 1) {  // few offsets in registers, the rest is the same for all lanes
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const int row = (i % kPeriod * W + wave) * kPieceRows + lane * 16 / kRowBytes;
+        dma_1k<false>(p + (size_t)(i / kPeriod * kPeriod * W * kPieceRows) * stride, row * (int)stride + chunk(i % kPeriod) * 16,
+                      at + i * W * 1024);
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int o = (i * W + wave) * 1024 + lane * 16, r = o / kRowBytes;
-      const int c = (o % kRowBytes / 16) ^ turn<kRowBytes>(r), rr = min(r, last);
+      const int row = min((i * W + wave) * kPieceRows + lane * 16 / kRowBytes, last);
       if constexpr (kVec) {
-        dma_1k<false>(reinterpret_cast<const char*>(base), rr * (int)(ld * sizeof(T)) + c * 16,
-                      lds_address(tile) + (i * W + wave) * 1024);
+        dma_1k<false>(p, row * (int)stride + chunk(i) * 16, at + i * W * 1024);
       } else {
-        const T* p = base + (size_t)rr * ld + c * (16 / (int)sizeof(T));
+        const T* from = reinterpret_cast<const T*>(p + row * stride + chunk(i) * 16);
         T x[16 / sizeof(T)];
 #pragma unroll
-        for (int e = 0; e < 16 / (int)sizeof(T); ++e) x[e] = p[e];
-        *reinterpret_cast<uint4*>(tile + o) = *reinterpret_cast<const uint4*>(x);
+        for (int e = 0; e < 16 / (int)sizeof(T); ++e) x[e] = from[e];
+        *reinterpret_cast<uint4*>(tile + (i * W + wave) * 1024 + lane * 16) = *reinterpret_cast<const uint4*>(x);
       }
     }
   }
