@@ -19,6 +19,7 @@
 // inputs there are (2^-9 of each of many terms of a sum; the result is
 // rounded to as much itself).  Sums, maxima and statistics are fp32.
 #include <algorithm>
+#include <type_traits>
 
 #include "jf_internal.h"
 #include "jf_tile32.h"
@@ -87,9 +88,11 @@ static unsigned work_grid(int blocks, int G, int heads) {
 }
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// Weights are 2^(s - m), m the row's maximum or up to kSlack below it: most
-// steps leave the sums and outputs as they are.
-constexpr float kSlack = 8.f;
+// Weights are 2^(s - m - kDown).  m follows a row's maximum only when a lane's
+// weights of a step sum to more than kMost: most steps look for no maximum
+// and leave sums and outputs as they are.  kDown keeps sums of weights below
+// 1, so that no sum of values overflows that has a finite mean.
+constexpr float kDown = 32.f, kMost = 0x1p-22f;
 
 template <typename T> struct Steps {
   static constexpr int KT = sizeof(T) == 2 ? 2 : 1;  // 32-row tiles of a step
@@ -103,17 +106,17 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalAr
   using Loader = RowLoader<T, HD, kRows, 4, kVec>;
   __shared__ __align__(1024) char s_kv[2][2][kRows * HD * sizeof(T)];
   const int grp = a.H / a.G;
-  const Work w = work_of(a.G, grp);
+  const Work job = work_of(a.G, grp);
   RowBlock b;
-  if (!find_block(a, w.rank, b)) return;
+  if (!find_block(a, job.rank, b)) return;
   b.t = b.blocks - 1 - b.t;  // the longest first
-  const int head = w.g * grp + w.h;
+  const int head = job.g * grp + job.h;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
   const int q0 = b.t * kBlock + wave * 32;             // the wave's queries
   const int qi = min(q0 + (lane & 31), b.n - 1);       // the lane's: past the end the last one again
   const int last = min(b.t * kBlock + kBlock, b.n) - 1;
-  const T* kp = reinterpret_cast<const T*>(a.k) + (size_t)b.r0 * a.ld_k + w.g * HD;
-  const T* vp = reinterpret_cast<const T*>(a.v) + (size_t)b.r0 * a.ld_v + w.g * HD;
+  const T* kp = reinterpret_cast<const T*>(a.k) + (size_t)b.r0 * a.ld_k + job.g * HD;
+  const T* vp = reinterpret_cast<const T*>(a.v) + (size_t)b.r0 * a.ld_v + job.g * HD;
   auto load = [&](int j0, int buf) {
     Loader::load(kp + (size_t)j0 * a.ld_k, a.ld_k * sizeof(T), last - j0, s_kv[buf][0]);
     Loader::load(vp + (size_t)j0 * a.ld_v, a.ld_v * sizeof(T), last - j0, s_kv[buf][1]);
@@ -132,15 +135,15 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalAr
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = zero16();
 
-  int buf = 0;
-  auto step = [&](auto edge, int j0) {
+  auto step = [&](auto edge, auto which, int j0) {
     constexpr bool kEdge = decltype(edge)::value;
+    constexpr int kBuf = decltype(which)::value;
     // every wave's pieces have arrived, and its work on the step before is done
     if constexpr (kVec) wait_vm<0>();
     __syncthreads();
-    if (j0 + kRows <= last) load(j0 + kRows, buf ^ 1);
-    const uint32_t keys = Tile::row_base(lds_address(s_kv[buf][0])), values = Tile::column_base(lds_address(s_kv[buf][1]));
-    buf ^= 1;
+    if (j0 + kRows <= last) load(j0 + kRows, kBuf ^ 1);
+    const uint32_t keys = Tile::row_base(lds_address(s_kv)) + kBuf * 2 * Tile::kRowBytes * kRows;
+    const uint32_t values = Tile::column_base(lds_address(s_kv)) + (kBuf * 2 + 1) * Tile::kRowBytes * kRows;
     if (kEdge && j0 > q0 + 31) return;
     f32x16_t st[KT];
 #pragma unroll
@@ -156,28 +159,34 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalAr
 #pragma unroll
         for (int i = 0; i < 16; ++i) st[kt][i] = 32 * kt + acc_row(i) <= lim ? st[kt][i] : -INFINITY;
     }
-    float mx = st[0][0];
+    f32x16_t w[KT];
+    float sum;
+    auto weights = [&](float off) {
+      sum = 0.f;
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
+      for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[kt][i]);
-    mx = pair_max(mx) * c;
-    if (__any(mx > m + kSlack)) {
-      const float m_new = fmaxf(m, mx);
-      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+        for (int i = 0; i < 16; ++i) {
+          w[kt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][i], c, off));
+          sum += w[kt][i];
+        }
+    };
+    weights(-kDown - m);  // nothing seen yet: infinite or NaN
+    if (__builtin_expect(__any(!(sum <= kMost)), 0)) {
+      float mx = st[0][0];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[kt][i]);
+      const float m_new = fmaxf(m, pair_max(mx) * c), m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m - m_use);
       m = m_new;
       l *= alpha;
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[d] *= alpha;
+      weights(-kDown - m_use);
     }
-    const float off = m == -INFINITY ? 0.f : -m;
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        st[kt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][i], c, off));
-        l += st[kt][i];
-      }
+    l += sum;
     bool finite = true;
     if constexpr (kEdge) {  // 0 times a value that is not finite would reach rows that do not see it
       uint32_t top = 0;
@@ -191,7 +200,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalAr
     for (int j = 0; j < 2 * KT; ++j) {
       float p[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = st[j / 2][8 * (j % 2) + e];
+      for (int e = 0; e < 8; ++e) p[e] = w[j / 2][8 * (j % 2) + e];
       Frag<T> pf;
       frag_of(p, pf);
       if (!kEdge || finite) {
@@ -221,11 +230,21 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalAr
       }
     }
   };
+  // The buffers by turns, in pairs of steps: their addresses are constants.
+  using First = std::integral_constant<int, 0>;
+  using Second = std::integral_constant<int, 1>;
+  static_assert(kBlock % (2 * kRows) == 0, "whole pairs before the edge");
   int j0 = 0;
 #pragma unroll 1
-  for (; j0 + kRows - 1 <= b.t * kBlock; j0 += kRows) step(std::false_type{}, j0);
+  for (; j0 < b.t * kBlock; j0 += 2 * kRows) {
+    step(std::false_type{}, First{}, j0);
+    step(std::false_type{}, Second{}, j0 + kRows);
+  }
 #pragma unroll 1
-  for (; j0 <= last; j0 += kRows) step(std::true_type{}, j0);
+  for (; j0 <= last; j0 += 2 * kRows) {
+    step(std::true_type{}, First{}, j0);
+    if (j0 + kRows <= last) step(std::true_type{}, Second{}, j0 + kRows);
+  }
 
   if (q0 + (lane & 31) >= b.n) return;
   l = pair_sum(l);
@@ -241,7 +260,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalAr
       row_store4<T>(out + 32 * d + acc_row(i), a.vec_out, v[0], v[1], v[2], v[3]);
     }
   if (a.lse && h == 0)
-    a.lse[(size_t)head * a.n_rows + b.r0 + qi] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    a.lse[(size_t)head * a.n_rows + b.r0 + qi] = l == 0.f ? -INFINITY : (m + kDown + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // ---- gradient ------------------------------------------------------------------------
@@ -307,15 +326,15 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dq(Causa
 #pragma unroll
   for (int d = 0; d < ND; ++d) dq[d] = zero16();
 
-  int buf = 0;
-  auto step = [&](auto edge, int j0) {
+  auto step = [&](auto edge, auto which, int j0) {
     constexpr bool kEdge = decltype(edge)::value;
+    constexpr int kBuf = decltype(which)::value;
     if constexpr (kVec) wait_vm<0>();
     __syncthreads();
-    if (j0 + kRows <= last) load(j0 + kRows, buf ^ 1);
-    const uint32_t keys = Tile::row_base(lds_address(s_kv[buf][0])), values = Tile::row_base(lds_address(s_kv[buf][1]));
-    const uint32_t key_columns = Tile::column_base(lds_address(s_kv[buf][0]));
-    buf ^= 1;
+    if (j0 + kRows <= last) load(j0 + kRows, kBuf ^ 1);
+    const uint32_t keys = Tile::row_base(lds_address(s_kv)) + kBuf * 2 * Tile::kRowBytes * kRows;
+    const uint32_t values = keys + Tile::kRowBytes * kRows;
+    const uint32_t key_columns = Tile::column_base(lds_address(s_kv)) + kBuf * 2 * Tile::kRowBytes * kRows;
     if (kEdge && j0 > q0 + 31) return;
     const int lim = qi - j0 - 4 * h;
 #pragma unroll
@@ -343,11 +362,21 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dq(Causa
       }
     }
   };
+  // The buffers by turns, in pairs of steps: their addresses are constants.
+  using First = std::integral_constant<int, 0>;
+  using Second = std::integral_constant<int, 1>;
+  static_assert(kBlock % (2 * kRows) == 0, "whole pairs before the edge");
   int j0 = 0;
 #pragma unroll 1
-  for (; j0 + kRows - 1 <= b.t * kBlock; j0 += kRows) step(std::false_type{}, j0);
+  for (; j0 < b.t * kBlock; j0 += 2 * kRows) {
+    step(std::false_type{}, First{}, j0);
+    step(std::false_type{}, Second{}, j0 + kRows);
+  }
 #pragma unroll 1
-  for (; j0 <= last; j0 += kRows) step(std::true_type{}, j0);
+  for (; j0 <= last; j0 += 2 * kRows) {
+    step(std::true_type{}, First{}, j0);
+    if (j0 + kRows <= last) step(std::true_type{}, Second{}, j0 + kRows);
+  }
 
   if (q0 + (lane & 31) >= b.n) return;
   const float f = 1.f / sqrtf((float)HD);
