@@ -26,8 +26,6 @@
 
 namespace jf {
 
-constexpr int kBlock = 128;  // queries of a workgroup (keys, for dk and dv): 32 a wave
-
 // A block of a sequence's rows: rows r0 .. r0 + n - 1 of the row tensors are
 // the sequence's, block t (of `blocks`) is meant.
 struct RowBlock {
@@ -37,7 +35,7 @@ struct RowBlock {
 // Block number `rank` of all sequences' blocks, one after the other.  The
 // first workgroup raises JF_FLAG_CAPACITY for row starts beyond the rows or
 // decreasing ones; no address is formed from those.
-__device__ __forceinline__ bool find_block(const CausalArgs& a, int rank, RowBlock& b) {
+template <int kBlock> __device__ __forceinline__ bool find_block(const CausalArgs& a, int rank, RowBlock& b) {
   const int lane = threadIdx.x & 63;
   const bool first = blockIdx.x == 0;
   int base = 0;
@@ -94,27 +92,72 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // 1, so that no sum of values overflows that has a finite mean.
 constexpr float kDown = 32.f, kMost = 0x1p-22f;
 
-template <typename T> struct Steps {
-  static constexpr int KT = sizeof(T) == 2 ? 2 : 1;  // 32-row tiles of a step
-  static constexpr int kRows = 32 * KT;
+// Four waves work on blocks of 32 NQ queries (keys, for dk and dv): NQ = 4
+// gives each wave 32 of its own; with fewer, kShare waves have the same ones
+// and take other rows of each step, and join at the end.  A step brings kRows
+// rows, 32 kTiles for a wave.
+template <typename T, int NQ> struct Shape {
+  static constexpr int kBlock = 32 * NQ, kShare = 4 / NQ;
+  static constexpr int kTiles = NQ == 4 && sizeof(T) == 2 ? 2 : 1;
+  static constexpr int kRows = 32 * kTiles * kShare;
 };
+// Workgroups of a compute unit: registers and LDS of fp32 tiles hold one.
+template <typename T> constexpr int kResident = sizeof(T) == 2 ? 2 : 1;
+using First = std::integral_constant<int, 0>;
+using Second = std::integral_constant<int, 1>;
 
-template <typename T, int HD, bool kVec>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalArgs a) {
+// Steps over the keys up to `last` for queries from `first` on, those before
+// it without masks.  The buffers by turns, in pairs of steps: their addresses
+// are constants.
+template <int kRows, typename F> __device__ __forceinline__ void all_steps(int first, int last, F step) {
+  int j0 = 0;
+#pragma unroll 1
+  for (; j0 + 2 * kRows - 1 <= first; j0 += 2 * kRows) {
+    step(std::false_type{}, First{}, j0);
+    step(std::false_type{}, Second{}, j0 + kRows);
+  }
+#pragma unroll 1
+  for (; j0 <= last; j0 += 2 * kRows) {
+    step(std::true_type{}, First{}, j0);
+    if (j0 + kRows <= last) step(std::true_type{}, Second{}, j0 + kRows);
+  }
+}
+
+// Values of the waves that share a block's rows, as columns of 32 lanes: slot
+// 0 .. kShare - 2 of them in LDS.
+template <int ND> __device__ __forceinline__ void put_shared(float* at, const f32x16_t (&x)[ND]) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) at[(32 * d + acc_row(i) + 4 * (lane >> 5)) * 32 + (lane & 31)] = x[d][i];
+}
+template <int ND> __device__ __forceinline__ void add_shared(const float* at, float f, f32x16_t (&x)[ND]) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[d][i] += f * at[(32 * d + acc_row(i) + 4 * (lane >> 5)) * 32 + (lane & 31)];
+}
+
+template <typename T, int HD, int NQ, bool kVec>
+__global__ void __launch_bounds__(256, kResident<T>) k_causal(CausalArgs a) {
   using Tile = RowTile<T, HD>;
-  constexpr int KT = Steps<T>::KT, kRows = Steps<T>::kRows, NS = HD / 16, ND = HD / 32;
+  using S = Shape<T, NQ>;
+  constexpr int KT = S::kTiles, kRows = S::kRows, NS = HD / 16, ND = HD / 32, kTileBytes = Tile::kRowBytes * kRows;
   using Loader = RowLoader<T, HD, kRows, 4, kVec>;
-  __shared__ __align__(1024) char s_kv[2][2][kRows * HD * sizeof(T)];
+  __shared__ __align__(1024) char s_kv[2][2][kTileBytes];
   const int grp = a.H / a.G;
   const Work job = work_of(a.G, grp);
   RowBlock b;
-  if (!find_block(a, job.rank, b)) return;
+  if (!find_block<S::kBlock>(a, job.rank, b)) return;
   b.t = b.blocks - 1 - b.t;  // the longest first
   const int head = job.g * grp + job.h;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
-  const int q0 = b.t * kBlock + wave * 32;             // the wave's queries
+  const int share = wave / NQ, from = share * 32 * KT; // the wave's rows of a step
+  const int q0 = b.t * S::kBlock + wave % NQ * 32;     // the wave's queries
   const int qi = min(q0 + (lane & 31), b.n - 1);       // the lane's: past the end the last one again
-  const int last = min(b.t * kBlock + kBlock, b.n) - 1;
+  const int last = min(b.t * S::kBlock + S::kBlock, b.n) - 1;
   const T* kp = reinterpret_cast<const T*>(a.k) + (size_t)b.r0 * a.ld_k + job.g * HD;
   const T* vp = reinterpret_cast<const T*>(a.v) + (size_t)b.r0 * a.ld_v + job.g * HD;
   auto load = [&](int j0, int buf) {
@@ -142,17 +185,15 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalAr
     if constexpr (kVec) wait_vm<0>();
     __syncthreads();
     if (j0 + kRows <= last) load(j0 + kRows, kBuf ^ 1);
-    const uint32_t keys = Tile::row_base(lds_address(s_kv)) + kBuf * 2 * Tile::kRowBytes * kRows;
-    const uint32_t values = Tile::column_base(lds_address(s_kv)) + (kBuf * 2 + 1) * Tile::kRowBytes * kRows;
-    if (kEdge && j0 > q0 + 31) return;
+    const uint32_t keys = Tile::row_base(lds_address(s_kv) + from * Tile::kRowBytes) + kBuf * 2 * kTileBytes;
+    const uint32_t values = Tile::column_base(lds_address(s_kv) + from * Tile::kRowBytes) + (kBuf * 2 + 1) * kTileBytes;
+    if (kEdge && j0 + from > q0 + 31) return;
     f32x16_t st[KT];
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      st[kt] = zero16();
-#pragma unroll
-      for (int s = 0; s < NS; ++s) mfma32(st[kt], Tile::rows(keys, 32 * kt, s), q[s]);
-    }
-    const int lim = qi - j0 - 4 * h;
+    for (int kt = 0; kt < KT; ++kt) st[kt] = zero16();
+    stream<T, KT * NS, kAhead<T>>([&](int n) { return Tile::rows(keys, n % KT * 32, n / KT); },
+                                  [&](int n, const Frag<T>& k) { mfma32(st[n % KT], k, q[n / KT]); });
+    const int lim = qi - j0 - from - 4 * h;
     if constexpr (kEdge) {
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
@@ -191,33 +232,28 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalAr
     if constexpr (kEdge) {  // 0 times a value that is not finite would reach rows that do not see it
       uint32_t top = 0;
 #pragma unroll
-      for (int j = 0; j < 2 * KT; ++j)
-#pragma unroll
-        for (int d = 0; d < ND; ++d) magnitude(Tile::columns(values, 16 * j, d), top);
+      for (int n = 0; n < 2 * KT * ND; ++n) magnitude(Tile::columns(values, n / ND * 16, n % ND), top);
       finite = !__any(!all_finite<T>(top));
     }
+    Frag<T> pf[2 * KT];
 #pragma unroll
     for (int j = 0; j < 2 * KT; ++j) {
       float p[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[e] = w[j / 2][8 * (j % 2) + e];
-      Frag<T> pf;
-      frag_of(p, pf);
-      if (!kEdge || finite) {
-#pragma unroll
-        for (int d = 0; d < ND; ++d) mfma32(o[d], Tile::columns(values, 16 * j, d), pf);
-      } else {
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          __builtin_amdgcn_sched_barrier(0);
-          Frag<T> v = Tile::columns(values, 16 * j, d);
-          keep_finite(v);
-          mfma32(o[d], v, pf);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
+      frag_of(p, pf[j]);
     }
-    if (kEdge && !finite) {
+    if (!kEdge || finite) {
+      stream<T, 2 * KT * ND, kAhead<T>>([&](int n) { return Tile::columns(values, n / ND * 16, n % ND); },
+                                        [&](int n, const Frag<T>& v) { mfma32(o[n % ND], v, pf[n / ND]); });
+    } else {
+#pragma unroll
+      for (int n = 0; n < 2 * KT * ND; ++n) {
+        __builtin_amdgcn_sched_barrier(0);
+        Frag<T> v = Tile::columns(values, n / ND * 16, n % ND);
+        keep_finite(v);
+        mfma32(o[n % ND], v, pf[n / ND]);
+      }
 #pragma unroll 1
       for (int j = 0; j < 2 * KT; ++j) {
         float p[8];
@@ -230,24 +266,39 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalAr
       }
     }
   };
-  // The buffers by turns, in pairs of steps: their addresses are constants.
-  using First = std::integral_constant<int, 0>;
-  using Second = std::integral_constant<int, 1>;
-  static_assert(kBlock % (2 * kRows) == 0, "whole pairs before the edge");
-  int j0 = 0;
-#pragma unroll 1
-  for (; j0 < b.t * kBlock; j0 += 2 * kRows) {
-    step(std::false_type{}, First{}, j0);
-    step(std::false_type{}, Second{}, j0 + kRows);
-  }
-#pragma unroll 1
-  for (; j0 <= last; j0 += 2 * kRows) {
-    step(std::true_type{}, First{}, j0);
-    if (j0 + kRows <= last) step(std::true_type{}, Second{}, j0 + kRows);
-  }
+  all_steps<kRows>(b.t * S::kBlock, last, step);
 
-  if (q0 + (lane & 31) >= b.n) return;
   l = pair_sum(l);
+  if constexpr (S::kShare > 1) {
+    __shared__ float s_ml[S::kShare - 1][NQ][2][32];
+    float* s_o = reinterpret_cast<float*>(s_kv);
+    static_assert((S::kShare - 1) * NQ * 32 * HD * 4 <= (int)sizeof(s_kv), "the parts fit");
+    __syncthreads();
+    if (share > 0) {
+      put_shared<ND>(s_o + ((share - 1) * NQ + wave % NQ) * 32 * HD, o);
+      if (h == 0) {
+        s_ml[share - 1][wave % NQ][0][lane] = m;
+        s_ml[share - 1][wave % NQ][1][lane] = l;
+      }
+    }
+    __syncthreads();
+    if (share > 0) return;
+    float m_all = m;
+#pragma unroll
+    for (int i = 0; i < S::kShare - 1; ++i) m_all = fmaxf(m_all, s_ml[i][wave][0][lane & 31]);
+    const float m_use = m_all == -INFINITY ? 0.f : m_all, f = __builtin_amdgcn_exp2f(m - m_use);
+    l *= f;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) o[d] *= f;
+#pragma unroll
+    for (int i = 0; i < S::kShare - 1; ++i) {
+      const float fi = __builtin_amdgcn_exp2f(s_ml[i][wave][0][lane & 31] - m_use);
+      l += fi * s_ml[i][wave][1][lane & 31];
+      add_shared<ND>(s_o + (i * NQ + wave) * 32 * HD, fi, o);
+    }
+    m = m_all;
+  }
+  if (q0 + (lane & 31) >= b.n) return;
   const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
   T* out = reinterpret_cast<T*>(a.out) + (size_t)(b.r0 + qi) * a.ld_out + head * HD + 4 * h;
 #pragma unroll
@@ -268,24 +319,26 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal(CausalAr
 // dq; and of each row and head, for dk and dv, what the accumulators of its
 // scores and of do v start from: -lse sqrt(hd) (-inf for a row without
 // weights, whose weights then are 0), and -D.
-template <typename T, int HD, bool kVec>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dq(CausalGradArgs a) {
+template <typename T, int HD, int NQ, bool kVec>
+__global__ void __launch_bounds__(256, kResident<T>) k_causal_dq(CausalGradArgs a) {
   using Tile = RowTile<T, HD>;
-  constexpr int KT = Steps<T>::KT, kRows = Steps<T>::kRows, NS = HD / 16, ND = HD / 32;
+  using S = Shape<T, NQ>;
+  constexpr int KT = S::kTiles, kRows = S::kRows, NS = HD / 16, ND = HD / 32, kTileBytes = Tile::kRowBytes * kRows;
   using Loader = RowLoader<T, HD, kRows, 4, kVec>;
-  __shared__ __align__(1024) char s_kv[2][2][kRows * HD * sizeof(T)];
+  __shared__ __align__(1024) char s_kv[2][2][kTileBytes];
   const int grp = a.f.H / a.f.G;
-  const Work w = work_of(a.f.G, grp);
+  const Work job = work_of(a.f.G, grp);
   RowBlock b;
-  if (!find_block(a.f, w.rank, b)) return;
+  if (!find_block<S::kBlock>(a.f, job.rank, b)) return;
   b.t = b.blocks - 1 - b.t;  // the longest first
-  const int head = w.g * grp + w.h;
+  const int head = job.g * grp + job.h;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
-  const int q0 = b.t * kBlock + wave * 32;
+  const int share = wave / NQ, from = share * 32 * KT;
+  const int q0 = b.t * S::kBlock + wave % NQ * 32;
   const int qi = min(q0 + (lane & 31), b.n - 1);
-  const int last = min(b.t * kBlock + kBlock, b.n) - 1;
-  const T* kp = reinterpret_cast<const T*>(a.f.k) + (size_t)b.r0 * a.f.ld_k + w.g * HD;
-  const T* vp = reinterpret_cast<const T*>(a.f.v) + (size_t)b.r0 * a.f.ld_v + w.g * HD;
+  const int last = min(b.t * S::kBlock + S::kBlock, b.n) - 1;
+  const T* kp = reinterpret_cast<const T*>(a.f.k) + (size_t)b.r0 * a.f.ld_k + job.g * HD;
+  const T* vp = reinterpret_cast<const T*>(a.f.v) + (size_t)b.r0 * a.f.ld_v + job.g * HD;
   auto load = [&](int j0, int buf) {
     Loader::load(kp + (size_t)j0 * a.f.ld_k, a.f.ld_k * sizeof(T), last - j0, s_kv[buf][0]);
     Loader::load(vp + (size_t)j0 * a.f.ld_v, a.f.ld_v * sizeof(T), last - j0, s_kv[buf][1]);
@@ -319,7 +372,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dq(Causa
     dot = pair_sum(dot);
     const size_t at = (size_t)head * a.f.n_rows + b.r0 + qi;
     lse = a.f.lse[at];
-    if (h == 0 && q0 + lane < b.n) a.dots[at] = make_float2(lse == -INFINITY ? -INFINITY : -lse * sqrtf((float)HD), -dot);
+    if (share == 0 && h == 0 && q0 + lane < b.n)
+      a.dots[at] = make_float2(lse == -INFINITY ? -INFINITY : -lse * sqrtf((float)HD), -dot);
     lse = lse == -INFINITY ? INFINITY : lse * kLog2e;
   }
   f32x16_t dq[ND];
@@ -332,11 +386,11 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dq(Causa
     if constexpr (kVec) wait_vm<0>();
     __syncthreads();
     if (j0 + kRows <= last) load(j0 + kRows, kBuf ^ 1);
-    const uint32_t keys = Tile::row_base(lds_address(s_kv)) + kBuf * 2 * Tile::kRowBytes * kRows;
-    const uint32_t values = keys + Tile::kRowBytes * kRows;
-    const uint32_t key_columns = Tile::column_base(lds_address(s_kv)) + kBuf * 2 * Tile::kRowBytes * kRows;
-    if (kEdge && j0 > q0 + 31) return;
-    const int lim = qi - j0 - 4 * h;
+    const uint32_t tile = lds_address(s_kv) + from * Tile::kRowBytes;
+    const uint32_t keys = Tile::row_base(tile) + kBuf * 2 * kTileBytes, values = keys + kTileBytes;
+    const uint32_t key_columns = Tile::column_base(tile) + kBuf * 2 * kTileBytes;
+    if (kEdge && j0 + from > q0 + 31) return;
+    const int lim = qi - j0 - from - 4 * h;
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
       f32x16_t st = zero16(), dp = zero16();
@@ -362,22 +416,18 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dq(Causa
       }
     }
   };
-  // The buffers by turns, in pairs of steps: their addresses are constants.
-  using First = std::integral_constant<int, 0>;
-  using Second = std::integral_constant<int, 1>;
-  static_assert(kBlock % (2 * kRows) == 0, "whole pairs before the edge");
-  int j0 = 0;
-#pragma unroll 1
-  for (; j0 < b.t * kBlock; j0 += 2 * kRows) {
-    step(std::false_type{}, First{}, j0);
-    step(std::false_type{}, Second{}, j0 + kRows);
-  }
-#pragma unroll 1
-  for (; j0 <= last; j0 += 2 * kRows) {
-    step(std::true_type{}, First{}, j0);
-    if (j0 + kRows <= last) step(std::true_type{}, Second{}, j0 + kRows);
-  }
+  all_steps<kRows>(b.t * S::kBlock, last, step);
 
+  if constexpr (S::kShare > 1) {
+    float* s_o = reinterpret_cast<float*>(s_kv);
+    static_assert((S::kShare - 1) * NQ * 32 * HD * 4 <= (int)sizeof(s_kv), "the parts fit");
+    __syncthreads();
+    if (share > 0) put_shared<ND>(s_o + ((share - 1) * NQ + wave % NQ) * 32 * HD, dq);
+    __syncthreads();
+    if (share > 0) return;
+#pragma unroll
+    for (int i = 0; i < S::kShare - 1; ++i) add_shared<ND>(s_o + (i * NQ + wave) * 32 * HD, 1.f, dq);
+  }
   if (q0 + (lane & 31) >= b.n) return;
   const float f = 1.f / sqrtf((float)HD);
   T* out = reinterpret_cast<T*>(a.g_q) + (size_t)(b.r0 + qi) * a.ld_g_q + head * HD + 4 * h;
@@ -388,27 +438,29 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dq(Causa
       row_store4<T>(out + 32 * d + acc_row(i), a.vec_q, dq[d][i] * f, dq[d][i + 1] * f, dq[d][i + 2] * f, dq[d][i + 3] * f);
 }
 
-// dk and dv of 128 keys of a KV head, over the queries of the heads of `part`
-// (part, part + parts, ... of the group's).
-template <typename T, int HD, bool kVec>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dkv(CausalGradArgs a) {
+// dk and dv of a block of keys of a KV head, over the queries of the heads of
+// `part` (part, part + parts, ... of the group's).
+template <typename T, int HD, int NQ, bool kVec>
+__global__ void __launch_bounds__(256, kResident<T>) k_causal_dkv(CausalGradArgs a) {
   using Tile = RowTile<T, HD>;
-  constexpr int KT = Steps<T>::KT, kRows = Steps<T>::kRows, NS = HD / 16, ND = HD / 32;
+  using S = Shape<T, NQ>;
+  constexpr int KT = S::kTiles, kRows = S::kRows, NS = HD / 16, ND = HD / 32;
   using Loader = RowLoader<T, HD, kRows, 4, kVec>;
-  __shared__ __align__(1024) char s_qg[2][2][kRows * HD * sizeof(T)];
+  __shared__ __align__(1024) char s_qg[2][2][Tile::kRowBytes * kRows];
   __shared__ __align__(16) float s_dots[2][2][kRows];
   const int grp = a.f.H / a.f.G;
-  const Work w = work_of(a.f.G, a.parts);
+  const Work job = work_of(a.f.G, a.parts);
   RowBlock b;
-  if (!find_block(a.f, w.rank, b)) return;  // in order: the first keys have the most queries
-  const int part = w.h;
+  if (!find_block<S::kBlock>(a.f, job.rank, b)) return;  // in order: the first keys have the most queries
+  const int part = job.h;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
-  const int k0 = b.t * kBlock + wave * 32;
+  const int share = wave / NQ, from = share * 32 * KT;  // the wave's rows of a step
+  const int k0 = b.t * S::kBlock + wave % NQ * 32;
   const int ki = min(k0 + (lane & 31), b.n - 1);
   Frag<T> k[NS], v[NS];
   {
-    const T* p = reinterpret_cast<const T*>(a.f.k) + (size_t)(b.r0 + ki) * a.f.ld_k + w.g * HD + 8 * h;
-    const T* r = reinterpret_cast<const T*>(a.f.v) + (size_t)(b.r0 + ki) * a.f.ld_v + w.g * HD + 8 * h;
+    const T* p = reinterpret_cast<const T*>(a.f.k) + (size_t)(b.r0 + ki) * a.f.ld_k + job.g * HD + 8 * h;
+    const T* r = reinterpret_cast<const T*>(a.f.v) + (size_t)(b.r0 + ki) * a.f.ld_v + job.g * HD + 8 * h;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
       k[s] = row_frag<T>(p + 16 * s, kVec);
@@ -423,8 +475,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dkv(Caus
     dv[d] = zero16();
   }
   // The steps: every head's rows from the block's first key on, one head after the other.
-  const int first = b.t * kBlock, steps = (b.n - first + kRows - 1) / kRows;
-  int head = w.g * grp + part, i0 = first;
+  const int first = b.t * S::kBlock, steps = (b.n - first + kRows - 1) / kRows;
+  int head = job.g * grp + part, i0 = first;
   float2 dots = make_float2(-INFINITY, 0.f);
   auto load = [&](int buf) {
     const int row = i0 + (int)threadIdx.x;
@@ -459,29 +511,31 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dkv(Caus
     if constexpr (kVec) wait_vm<0>();
     __syncthreads();
     if (it + 1 < total) load(buf ^ 1);
-    const uint32_t qs = Tile::row_base(lds_address(s_qg[buf][0])), gs = Tile::row_base(lds_address(s_qg[buf][1]));
-    const uint32_t q_columns = Tile::column_base(lds_address(s_qg[buf][0]));
-    const uint32_t g_columns = Tile::column_base(lds_address(s_qg[buf][1]));
-    const bool edge = at < k0 + 31;  // rows before some of the wave's keys
-    if (at + kRows > k0) {
+    const int mine = at + from;          // the wave's first row
+    const bool edge = mine < k0 + 31;    // rows before some of the wave's keys
+    if (mine + 32 * KT > k0 && mine < b.n) {
 #pragma unroll 1
-      for (int kt = 0; kt < KT; ++kt) {
-        constexpr int kSkip = 32 * Tile::kRowBytes;
+      for (int kt = 0; kt < KT; ++kt) {  // not unrolled: registers
+        const int skip = from + 32 * kt;
+        const uint32_t q_tile = lds_address(s_qg[buf][0]) + skip * Tile::kRowBytes;
+        const uint32_t g_tile = lds_address(s_qg[buf][1]) + skip * Tile::kRowBytes;
+        const uint32_t qs = Tile::row_base(q_tile), gs = Tile::row_base(g_tile);
+        const uint32_t q_columns = Tile::column_base(q_tile), g_columns = Tile::column_base(g_tile);
         f32x16_t st, dp;
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-          const float4 x = *reinterpret_cast<const float4*>(&s_dots[buf][0][32 * kt + acc_row(i) + 4 * h]);
-          const float4 y = *reinterpret_cast<const float4*>(&s_dots[buf][1][32 * kt + acc_row(i) + 4 * h]);
+          const float4 x = *reinterpret_cast<const float4*>(&s_dots[buf][0][skip + acc_row(i) + 4 * h]);
+          const float4 y = *reinterpret_cast<const float4*>(&s_dots[buf][1][skip + acc_row(i) + 4 * h]);
           st[i] = x.x; st[i + 1] = x.y; st[i + 2] = x.z; st[i + 3] = x.w;
           dp[i] = y.x; dp[i + 1] = y.y; dp[i + 2] = y.z; dp[i + 3] = y.w;
         }
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-          mfma32(st, Tile::rows(qs + kt * kSkip, 0, s), k[s]);
-          mfma32(dp, Tile::rows(gs + kt * kSkip, 0, s), v[s]);
+          mfma32(st, Tile::rows(qs, 0, s), k[s]);
+          mfma32(dp, Tile::rows(gs, 0, s), v[s]);
         }
         __builtin_amdgcn_sched_barrier(0);
-        const int lim = ki - at - 32 * kt - 4 * h;
+        const int lim = ki - at - skip - 4 * h;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const bool hidden = edge && acc_row(i) < lim;
@@ -502,10 +556,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dkv(Caus
           frag_of(y, df);
 #pragma unroll
           for (int d = 0; d < ND; ++d) {
-            mfma32(dv[d], Tile::columns(g_columns + kt * kSkip, 16 * j, d), pf);
-            mfma32(dk[d], Tile::columns(q_columns + kt * kSkip, 16 * j, d), df);
+            mfma32(dv[d], Tile::columns(g_columns, 16 * j, d), pf);
+            mfma32(dk[d], Tile::columns(q_columns, 16 * j, d), df);
           }
-          
         }
       }
     }
@@ -515,9 +568,25 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_causal_dkv(Caus
     if (at >= b.n) at = first;
   }
 
+  if constexpr (S::kShare > 1) {
+    float* s_o = reinterpret_cast<float*>(s_qg);
+    static_assert((S::kShare - 1) * NQ * 64 * HD * 4 <= (int)sizeof(s_qg), "the parts fit");
+    __syncthreads();
+    if (share > 0) {
+      put_shared<ND>(s_o + ((share - 1) * NQ + wave % NQ) * 64 * HD, dk);
+      put_shared<ND>(s_o + ((share - 1) * NQ + wave % NQ) * 64 * HD + 32 * HD, dv);
+    }
+    __syncthreads();
+    if (share > 0) return;
+#pragma unroll
+    for (int i = 0; i < S::kShare - 1; ++i) {
+      add_shared<ND>(s_o + (i * NQ + wave) * 64 * HD, 1.f, dk);
+      add_shared<ND>(s_o + (i * NQ + wave) * 64 * HD + 32 * HD, 1.f, dv);
+    }
+  }
   if (k0 + (lane & 31) >= b.n) return;
   const float f = 1.f / sqrtf((float)HD);
-  const int col = w.g * HD + 4 * h;
+  const int col = job.g * HD + 4 * h;
   if (a.parts == 1) {
     T* pk = reinterpret_cast<T*>(a.g_k) + (size_t)(b.r0 + ki) * a.ld_g_k + col;
     T* pv = reinterpret_cast<T*>(a.g_v) + (size_t)(b.r0 + ki) * a.ld_g_v + col;
@@ -565,53 +634,82 @@ __global__ void __launch_bounds__(256) k_causal_join(CausalGradArgs a) {
 }
 
 // ---- launch --------------------------------------------------------------------------
-int causal_blocks(int n_rows, int n_seqs) {
-  return (int)std::min<int64_t>((int64_t)n_rows / kBlock + std::min(n_seqs, n_rows), n_rows);
+static int blocks_of(int n_rows, int n_seqs, int rows) {
+  return (int)std::min<int64_t>((int64_t)n_rows / rows + std::min(n_seqs, n_rows), n_rows);
 }
 
-// One part where the workgroups fill the chip; else one head a workgroup, and
-// a pass that adds the heads' shares.
-int causal_parts(int n_rows, int n_seqs, int H, int G) {
-  return (int64_t)causal_blocks(n_rows, n_seqs) * G >= 1024 ? 1 : H / G;
+// Wide blocks read the keys least often; narrow ones make the longest
+// workgroup short, which counts where there are too few to fill the chip.
+// Blocks of 128 rows from kWide workgroups on (28 heads of 128, bf16: 1024
+// rows 24.3 us in blocks of 128, 21.1 of 64; 2048 rows 47.4 and 50.9; the
+// gradient of 2048 rows 190 and 160, of 4096 467 and 496), of 32 where these
+// all run at once (4 heads of 32, fp32, 2048 rows: 87, 47 and 27 us in blocks
+// of 128, 64 and 32).  At head_dim 128 blocks of 32 rows fill the LDS, or gain
+// nothing (20.1 us for 512 rows, blocks of 64 12.7).
+static int causal_groups(int n_rows, int n_seqs, int H, int hd, bool f32, bool grad) {
+  const int wide = f32 ? 1000 : hd == 128 ? (grad ? 450 : 320) : grad ? 900 : 600;
+  if ((int64_t)blocks_of(n_rows, n_seqs, 128) * H >= wide) return 4;
+  return (int64_t)blocks_of(n_rows, n_seqs, 32) * H > 512 || hd == 128 ? 2 : 1;
+}
+static void causal_shape(CausalArgs& a, bool grad) {
+  a.groups = causal_groups(a.n_rows, a.n_seqs, a.H, a.hd, a.f32, grad);
+  a.blocks = blocks_of(a.n_rows, a.n_seqs, 32 * a.groups);
+}
+void causal_plan(CausalArgs& a) { causal_shape(a, false); }
+// dk and dv: one part where its workgroups fill the chip, else a group's heads
+// in parts of as many as leave enough of them, and a pass that adds the parts
+// (28 query and 4 KV heads, 4096 rows: one part 1500 us, a head a part 471; 32
+// sequences of 500 rows: 383 and 540).
+void causal_grad_plan(CausalGradArgs& a) {
+  causal_shape(a.f, true);
+  const int64_t one = (int64_t)a.f.blocks * a.f.G, grp = a.f.H / a.f.G;
+  const int64_t heads = one >= 500 ? grp : std::max<int64_t>(grp * one / 1024, 1);
+  a.parts = (int)((grp + heads - 1) / heads);
 }
 
-template <typename T, int HD> static void causal_vec(const CausalArgs& a, hipStream_t st) {
-  const unsigned grid = work_grid(a.blocks, a.G, a.H / a.G);
-  if (a.vec) k_causal<T, HD, true><<<grid, 256, 0, st>>>(a);
-  else k_causal<T, HD, false><<<grid, 256, 0, st>>>(a);
-}
-template <typename T> static hipError_t causal_hd(const CausalArgs& a, hipStream_t st) {
-  if (a.hd == 32) causal_vec<T, 32>(a, st);
-  else if (a.hd == 64) causal_vec<T, 64>(a, st);
-  else causal_vec<T, 128>(a, st);
+template <typename F> static hipError_t with_shape(int hd, int groups, bool vec, F f) {
+  auto by_vec = [&](auto d, auto n) {
+    if (vec) f(d, n, std::true_type{});
+    else f(d, n, std::false_type{});
+  };
+  auto by_groups = [&](auto d) {
+    if (groups == 4) by_vec(d, std::integral_constant<int, 4>{});
+    else if (groups == 2) by_vec(d, std::integral_constant<int, 2>{});
+    else by_vec(d, std::integral_constant<int, 1>{});
+  };
+  if (hd == 32) by_groups(std::integral_constant<int, 32>{});
+  else if (hd == 64) by_groups(std::integral_constant<int, 64>{});
+  else by_groups(std::integral_constant<int, 128>{});
   return hipGetLastError();
 }
+// No kernel for what causal_groups does not choose.
+template <int HD, int NQ> constexpr int kGroups = HD == 128 && NQ == 1 ? 2 : NQ;
+
+template <typename T> static hipError_t causal_type(const CausalArgs& a, hipStream_t st) {
+  const unsigned grid = work_grid(a.blocks, a.G, a.H / a.G);
+  return with_shape(a.hd, a.groups, a.vec, [&](auto hd, auto nq, auto vec) {
+    constexpr int HD = decltype(hd)::value;
+    k_causal<T, HD, kGroups<HD, decltype(nq)::value>, decltype(vec)::value><<<grid, 256, 0, st>>>(a);
+  });
+}
 hipError_t launch_causal(int dtype, const CausalArgs& a, hipStream_t st) {
-  return dtype == 0 ? causal_hd<float>(a, st) : causal_hd<bf16_t>(a, st);
+  return dtype == 0 ? causal_type<float>(a, st) : causal_type<bf16_t>(a, st);
 }
 
-template <typename T, int HD> static void causal_grad_vec(const CausalGradArgs& a, hipStream_t st) {
+template <typename T> static hipError_t causal_grad_type(const CausalGradArgs& a, hipStream_t st) {
   const unsigned dq = work_grid(a.f.blocks, a.f.G, a.f.H / a.f.G), dkv = work_grid(a.f.blocks, a.f.G, a.parts);
-  if (a.f.vec) {
-    k_causal_dq<T, HD, true><<<dq, 256, 0, st>>>(a);
-    k_causal_dkv<T, HD, true><<<dkv, 256, 0, st>>>(a);
-  } else {
-    k_causal_dq<T, HD, false><<<dq, 256, 0, st>>>(a);
-    k_causal_dkv<T, HD, false><<<dkv, 256, 0, st>>>(a);
-  }
-}
-template <typename T> static hipError_t causal_grad_hd(const CausalGradArgs& a, hipStream_t st) {
-  if (a.f.hd == 32) causal_grad_vec<T, 32>(a, st);
-  else if (a.f.hd == 64) causal_grad_vec<T, 64>(a, st);
-  else causal_grad_vec<T, 128>(a, st);
-  const hipError_t e = hipGetLastError();
+  const hipError_t e = with_shape(a.f.hd, a.f.groups, a.f.vec, [&](auto hd, auto nq, auto vec) {
+    constexpr int HD = decltype(hd)::value, NQ = kGroups<HD, decltype(nq)::value>;
+    k_causal_dq<T, HD, NQ, decltype(vec)::value><<<dq, 256, 0, st>>>(a);
+    k_causal_dkv<T, HD, NQ, decltype(vec)::value><<<dkv, 256, 0, st>>>(a);
+  });
   if (e != hipSuccess || a.parts == 1) return e;
   const int64_t quads = (int64_t)a.f.n_rows * a.f.G * a.f.hd / 4;
   k_causal_join<T><<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 hipError_t launch_causal_grad(int dtype, const CausalGradArgs& a, hipStream_t st) {
-  return dtype == 0 ? causal_grad_hd<float>(a, st) : causal_grad_hd<bf16_t>(a, st);
+  return dtype == 0 ? causal_grad_type<float>(a, st) : causal_grad_type<bf16_t>(a, st);
 }
 
 }  // namespace jf

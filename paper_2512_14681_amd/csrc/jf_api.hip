@@ -1189,8 +1189,10 @@ static jf_status check_causal(int n_seqs, int n_rows, const int32_t* d_row_start
   *none = n_seqs == 0 || n_rows == 0;
   if (*none) return JF_OK;
   if (!d_row_start) return fail(JF_E_INVAL, "null pointer argument");
-  if (((int64_t)causal_blocks(n_rows, n_seqs) + 8) * n_heads > kMaxBlocks ||
-      ((int64_t)n_rows * n_heads * (head_dim / 8) + 255) / 256 > 4 * kMaxBlocks)
+  CausalArgs a{};
+  a.n_seqs = n_seqs; a.n_rows = n_rows; a.H = n_heads; a.hd = head_dim; a.f32 = dtype == JF_F32;
+  causal_plan(a);
+  if (((int64_t)a.blocks + 8) * n_heads > kMaxBlocks || (int64_t)n_rows * n_kv_heads * head_dim / 1024 > kMaxBlocks)
     return fail(JF_E_CAPACITY, "%d rows of %d heads exceed one launch", n_rows, n_heads);
   return JF_OK;
 }
@@ -1208,7 +1210,7 @@ static void causal_args(CausalArgs* a, int n_seqs, int n_rows, const int32_t* d_
   a->out = d_out; a->ld_out = (size_t)ld_out;
   a->vec_out = vector4(d_out, ld_out, esz);
   a->lse = d_lse;
-  a->blocks = causal_blocks(n_rows, n_seqs);
+  a->f32 = esz == 4;
 }
 
 extern "C" jf_status jf_attention_causal(int32_t n_seqs, int32_t n_rows, const int32_t* d_row_start, int32_t n_heads,
@@ -1225,6 +1227,7 @@ extern "C" jf_status jf_attention_causal(int32_t n_seqs, int32_t n_rows, const i
   CausalArgs a{};
   causal_args(&a, n_seqs, n_rows, d_row_start, n_heads, n_kv_heads, head_dim, dtype == JF_BF16 ? 2 : 4, d_q, ld_q, d_k,
               ld_k, d_v, ld_v, d_out, ld_out, d_lse, d_flags);
+  causal_plan(a);
   HIP_TRY(launch_causal(dtype, a, (hipStream_t)stream));
   return JF_OK;
 }
@@ -1238,8 +1241,13 @@ extern "C" size_t jf_attention_causal_grad_ws_bytes(int32_t n_seqs, int32_t n_ro
   static const int32_t some = 0;
   if (check_causal(n_seqs, n_rows, &some, n_heads, n_kv_heads, head_dim, JF_F32, &none) != JF_OK) return 0;
   if (none) return 256;
-  const int parts = causal_parts(n_rows, n_seqs, n_heads, n_kv_heads);
-  const size_t part = parts > 1 ? (size_t)2 * parts * n_rows * n_kv_heads * head_dim * 4 : 0;
+  size_t part = 0;  // the larger of what both types need
+  for (int f32 = 0; f32 < 2; ++f32) {
+    CausalGradArgs a{};
+    a.f.n_seqs = n_seqs; a.f.n_rows = n_rows; a.f.H = n_heads; a.f.G = n_kv_heads; a.f.hd = head_dim; a.f.f32 = f32;
+    causal_grad_plan(a);
+    if (a.parts > 1) part = std::max(part, (size_t)2 * a.parts * n_rows * n_kv_heads * head_dim * 4);
+  }
   return causal_dots_bytes(n_rows, n_heads) + part + 256;
 }
 
@@ -1272,7 +1280,7 @@ extern "C" jf_status jf_attention_causal_grad(int32_t n_seqs, int32_t n_rows, co
   a.vec_kv = vector4(d_g_k, ld_g_k, esz) && vector4(d_g_v, ld_g_v, esz);
   a.dots = (float2*)d_ws;
   a.kv_part = (float*)((char*)d_ws + causal_dots_bytes(n_rows, n_heads));
-  a.parts = causal_parts(n_rows, n_seqs, n_heads, n_kv_heads);
+  causal_grad_plan(a);
   HIP_TRY(launch_causal_grad(dtype, a, (hipStream_t)stream));
   return JF_OK;
 }

@@ -371,9 +371,12 @@ struct CausalArgs {
   size_t ld_out;
   int vec_out;               // every four elements from a multiple of 4 are aligned
   float* lse;                // [H][n_rows]; may be null in the forward pass
-  int blocks;                // bound on the blocks of rows of all sequences (causal_blocks)
+  int f32;                   // the rows' type
+  // the plan (causal_plan)
+  int groups;                // rows of a block / 32
+  int blocks;                // bound on the blocks of all sequences
 };
-int causal_blocks(int n_rows, int n_seqs);
+void causal_plan(CausalArgs& a);           // from n_rows, n_seqs, H, hd, f32
 hipError_t launch_causal(int dtype, const CausalArgs& a, hipStream_t stream);
 struct CausalGradArgs {
   CausalArgs f;              // out: read
@@ -385,9 +388,9 @@ struct CausalGradArgs {
   int vec_q, vec_kv;         // every four elements from a multiple of 4 are aligned
   float2* dots;              // [H][n_rows]
   float* kv_part;            // [2][parts][n_rows][G * hd], with more than one part
-  int parts;                 // shares of a group's heads (causal_parts)
+  int parts;                 // shares of a group's heads
 };
-int causal_parts(int n_rows, int n_seqs, int H, int G);
+void causal_grad_plan(CausalGradArgs& a);  // also parts
 hipError_t launch_causal_grad(int dtype, const CausalGradArgs& a, hipStream_t stream);
 
 // attention_shared.hip

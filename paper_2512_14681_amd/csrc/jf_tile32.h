@@ -250,6 +250,23 @@ template <int N> __device__ __forceinline__ void settle(Frag<float> (&f)[N]) {
   }
 }
 
+// mul(n, read(n)) for n < N, in a fixed order: reads run D - 1 ahead of the
+// matrix instructions that take them.  (The compiler's own order waits for
+// most reads right before their use.)
+template <typename T, int N, int D, typename R, typename M> __device__ __forceinline__ void stream(R read, M mul) {
+  Frag<T> f[D];
+#pragma unroll
+  for (int n = 0; n < D - 1 && n < N; ++n) f[n] = read(n);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    if (n + D - 1 < N) f[(n + D - 1) % D] = read(n + D - 1);
+    mul(n, f[n % D]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+template <typename T> constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;
+
 // Brings rows of a matrix (HD of its columns, ld elements a row) into an LDS
 // tile of ROWS rows, by W waves; rows past `last` repeat row `last`.  kVec:
 // rows on 16-byte boundaries go to LDS without passing registers, and the
