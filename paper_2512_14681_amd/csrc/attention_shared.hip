@@ -26,9 +26,13 @@ namespace jf {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kSlack = 8.f;  // weights are 2^(s - m), m the row's maximum or up to this below it
+// Weights are 2^(s - m - kDown).  m follows a row's maximum only when a lane's
+// weights of a step sum to more than kMost.  kDown keeps sums of weights below
+// 1, so that no sum of values overflows that has a finite mean.
+constexpr float kDown = 32.f, kMost = 0x1p-22f;
 constexpr int kChunk = 4;      // pages of a part at least
 constexpr int kWorkgroups = 512;  // as many as run at once
+constexpr int kFewTiles = 32;     // tiles of a group's or sequence's queries that have workgroups of their own
 
 // Queries as operands: bf16 in two terms.
 template <typename T> struct Query;
@@ -82,6 +86,8 @@ __device__ __forceinline__ bool shared_pages(const SharedArgs& a, int s, const S
   if (!ok && a.b.flags && threadIdx.x == 0) atomicOr(a.b.flags, kFlagCapacity);
   return ok;
 }
+// Values that all lanes share, in scalar registers.
+__device__ __forceinline__ int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
 // Pages of a part, when `splits` parts at most share n pages.
 __device__ __forceinline__ int part_pages(int n, int splits) {
   return max((n + splits - 1) / max(splits, 1), kChunk);
@@ -116,23 +122,21 @@ template <typename T, int HD> struct SharedTile {
     for (int d = 0; d < ND; ++d) o[d] = zero16();
   }
 
-  // 32 KT keys in LDS (in PageLoader's order) and V^T beside them.  kEdge: seen
-  // holds a bit for each that the lane's query sees.  False if there were
-  // values that are not finite, which count as 0 here.
-  template <int KT, bool kEdge>
-  __device__ __forceinline__ bool step(const char* tile, uint64_t seen) {
-    using Keys = RowTile<T, HD>;
+  // Scores of 32 KT keys in LDS (in PageLoader's order).
+  template <int KT> __device__ __forceinline__ void scores(const char* tile, f32x16_t (&st)[KT]) const {
+    const uint32_t keys = RowTile<T, HD>::row_base(lds_address(tile));
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) st[kt] = zero16();
+    stream<T, KT * NS, kAhead<T>>([&](int n) { return RowTile<T, HD>::rows(keys, n % KT * 32, n / KT); },
+                                  [&](int n, const Frag<T>& k) { mul(st[n % KT], k, q[n / KT]); });
+  }
+  // Their weights, and the weighted values (V^T in LDS, there once arrive() is
+  // back).  kEdge: seen holds a bit for each key that the lane's query sees.
+  // False if there were values that are not finite, which count as 0 here.
+  template <int KT, bool kEdge, typename F>
+  __device__ __forceinline__ bool outputs(f32x16_t (&st)[KT], const char* tile, uint64_t seen, F arrive) {
     using Values = RowTile<T, 32 * KT>;
-    const uint32_t keys = Keys::row_base(lds_address(tile));
-    const uint32_t values = Values::row_base(lds_address(tile) + 32 * KT * Keys::kRowBytes);
     const float c = kLog2e / sqrtf((float)HD);
-    f32x16_t st[KT];
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      st[kt] = zero16();
-#pragma unroll
-      for (int s = 0; s < NS; ++s) mul(st[kt], Keys::rows(keys, 32 * kt, s), q[s]);
-    }
     seen >>= 8 * ((threadIdx.x & 63) >> 5);
     const uint32_t bits[2] = {(uint32_t)seen, (uint32_t)(seen >> 32)};
     if constexpr (kEdge) {
@@ -141,28 +145,36 @@ template <typename T, int HD> struct SharedTile {
 #pragma unroll
         for (int i = 0; i < 16; ++i) st[kt][i] = (bits[kt] >> (16 * (i / 8) + i % 8)) & 1 ? st[kt][i] : -INFINITY;
     }
-    float mx = st[0][0];
+    float sum;
+    f32x16_t w[KT];
+    auto weights = [&](float off) {
+      sum = 0.f;
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
+      for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[kt][i]);
-    mx = pair_max(mx) * c;
-    if (__any(mx > m + kSlack)) {
-      const float m_new = fmaxf(m, mx);
-      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+        for (int i = 0; i < 16; ++i) {
+          w[kt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][i], c, off));
+          sum += w[kt][i];
+        }
+    };
+    weights(-kDown - m);  // nothing seen yet: infinite or NaN
+    if (__builtin_expect(__any(!(sum <= kMost)), 0)) {
+      float mx = st[0][0];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[kt][i]);
+      const float m_new = fmaxf(m, pair_max(mx) * c), m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m - m_use);
       m = m_new;
       l *= alpha;
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[d] *= alpha;
+      weights(-kDown - m_use);
     }
-    const float off = m == -INFINITY ? 0.f : -m;
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        st[kt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][i], c, off));
-        l += st[kt][i];
-      }
+    l += sum;
+    arrive();
+    const uint32_t values = Values::row_base(lds_address(tile));
     bool finite = true;
     if constexpr (kEdge) {  // 0 times a value that is not finite would reach rows that do not see it
       uint32_t top = 0;
@@ -173,32 +185,31 @@ template <typename T, int HD> struct SharedTile {
       finite = !__any(!all_finite<T>(top));
       asm volatile("" ::: "memory");  // read again rather than kept: registers
     }
+    Query<T> pf[2 * KT];
 #pragma unroll
     for (int j = 0; j < 2 * KT; ++j) {
       float p[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = st[j / 2][8 * (j % 2) + e];
-      Query<T> pf;
-      split_query(p, pf);
-      if (!kEdge || finite) {
+      for (int e = 0; e < 8; ++e) p[e] = w[j / 2][8 * (j % 2) + e];
+      split_query(p, pf[j]);
+    }
+    if (!kEdge || finite) {
+      stream<T, 2 * KT * ND, kAhead<T>>([&](int n) { return Values::rows(values, n % ND * 32, n / ND); },
+                                        [&](int n, const Frag<T>& v) { mul(o[n % ND], v, pf[n / ND]); });
+    } else {
 #pragma unroll
-        for (int d = 0; d < ND; ++d) mul(o[d], Values::rows(values, 32 * d, j), pf);
-      } else {
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          __builtin_amdgcn_sched_barrier(0);
-          Frag<T> v = Values::rows(values, 32 * d, j);
-          keep_finite(v);
-          mul(o[d], v, pf);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+      for (int n = 0; n < 2 * KT * ND; ++n) {
+        __builtin_amdgcn_sched_barrier(0);
+        Frag<T> v = Values::rows(values, n % ND * 32, n / ND);
+        keep_finite(v);
+        mul(o[n % ND], v, pf[n / ND]);
       }
     }
     return finite;
   }
-  // What the queries see of infinities and NaN among the values that step left out.
+  // What the queries see of infinities and NaN among the values that outputs left out.
   template <int KT> __device__ __forceinline__ void infinite(const char* tile, uint64_t seen) {
-    const uint32_t values = RowTile<T, 32 * KT>::row_base(lds_address(tile) + 32 * KT * RowTile<T, HD>::kRowBytes);
+    const uint32_t values = RowTile<T, 32 * KT>::row_base(lds_address(tile));
     seen >>= 8 * ((threadIdx.x & 63) >> 5);
 #pragma unroll 1
     for (int j = 0; j < 2 * KT; ++j) {
@@ -218,29 +229,34 @@ template <typename T, int HD> struct SharedTile {
 // with bits 2 and 3 of r exchanged: a result's elements 8 j .. + 7 of lane l
 // then are keys 16 j + 8 (l / 32) .. + 7.
 template <typename T, int HD, int KT, int W> struct PageLoader {
-  static __device__ __forceinline__ void load(const T* keys, const T* values, int t0, int wave, char* tile) {
-    constexpr int kKeyRow = HD * (int)sizeof(T), kValueRow = 32 * KT * (int)sizeof(T), kValueStride = kPage * (int)sizeof(T);
-    constexpr int kPieces = 32 * KT * kKeyRow / 1024 / W;
-    static_assert(kPieces * W * 1024 == 32 * KT * kKeyRow, "whole pieces");
-    constexpr int kKeyRows = 1024 / kKeyRow, kValueRows = 1024 / kValueRow;  // rows of a 1 KB piece
-    static_assert(kKeyRows <= 16 && kValueRows <= 16, "places repeat after 16 rows");
+  static constexpr int kKeyRow = HD * (int)sizeof(T), kValueRow = 32 * KT * (int)sizeof(T);
+  static constexpr int kBytes = 32 * KT * kKeyRow;                     // of the keys, and of the values
+  static constexpr int kPieces = kBytes / 1024 / W;                    // 1 KB pieces a wave, of either
+  static constexpr int kKeyRows = 1024 / kKeyRow, kValueRows = 1024 / kValueRow;  // rows of a piece
+  static_assert(kPieces * W * 1024 == kBytes, "whole pieces");
+  static_assert(kKeyRows <= 16 && kValueRows <= 16, "places repeat after 16 rows");
+  // Few offsets in registers: they repeat every 16 rows, the rest is the same for all lanes.
+  static __device__ __forceinline__ void keys(const T* page, int t0, int wave, char* tile) {
+    constexpr int kPeriod = std::max(16 / (kKeyRows * W), 1);
     const int lane = threadIdx.x & 63;
     const uint32_t at = lds_address(tile) + wave * 1024;
-    // Few offsets in registers: they repeat every 16 rows, the rest is the same for all lanes.
-    constexpr int kKeyPeriod = std::max(16 / (kKeyRows * W), 1), kValuePeriod = std::max(16 / (kValueRows * W), 1);
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int row = ((i % kKeyPeriod * W + wave) * kKeyRows) % 16 + lane * 16 / kKeyRow;
+      const int row = ((i % kPeriod * W + wave) * kKeyRows) % 16 + lane * 16 / kKeyRow;
       const int c = (lane * 16 % kKeyRow / 16) ^ turn<kKeyRow>(row), key = (row & ~12) | ((row & 4) << 1) | ((row & 8) >> 1);
       const int skip = (i * W + wave) * kKeyRows / 16 * 16;
-      dma_1k<false>(reinterpret_cast<const char*>(keys + (size_t)t0 * HD) + skip * kKeyRow, key * kKeyRow + c * 16, at + i * W * 1024);
+      dma_1k<false>(reinterpret_cast<const char*>(page + (size_t)t0 * HD) + skip * kKeyRow, key * kKeyRow + c * 16, at + i * W * 1024);
     }
+  }
+  static __device__ __forceinline__ void values(const T* page, int t0, int wave, char* tile) {
+    constexpr int kPeriod = std::max(16 / (kValueRows * W), 1), kStride = kPage * (int)sizeof(T);
+    const int lane = threadIdx.x & 63;
+    const uint32_t at = lds_address(tile) + wave * 1024;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int row = ((i % kValuePeriod * W + wave) * kValueRows) % 16 + lane * 16 / kValueRow;
+      const int row = ((i % kPeriod * W + wave) * kValueRows) % 16 + lane * 16 / kValueRow;
       const int c = (lane * 16 % kValueRow / 16) ^ turn<kValueRow>(row), skip = (i * W + wave) * kValueRows / 16 * 16;
-      dma_1k<false>(reinterpret_cast<const char*>(values + t0) + skip * kValueStride, row * kValueStride + c * 16,
-                    at + 32 * KT * kKeyRow + i * W * 1024);
+      dma_1k<false>(reinterpret_cast<const char*>(page + t0) + skip * kStride, row * kStride + c * 16, at + i * W * 1024);
     }
   }
 };
@@ -266,7 +282,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_share
   using Tile = SharedTile<T, HD>;
   constexpr int KT = HD * sizeof(T) == 64 ? 2 : 1, ND = HD / 32;  // a 1 KB piece of a step's keys for every wave
   constexpr int kOne = 2 * 32 * HD * (int)sizeof(T);   // 32 keys and their values
-  constexpr int kBytes = std::max({4 * kOne, 2 * KT * kOne, 4 * 32 * HD * 4});
+  constexpr int kBytes = std::max(4 * KT * kOne, 4 * 32 * HD * 4);  // 4 waves' steps, or 4 stages; the waves' outputs
   __shared__ __align__(1024) char s_kv[kBytes];
   __shared__ float s_ml[4][2][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
@@ -309,44 +325,74 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_share
   if (p0 >= p1 || group * (few ? 32 : 128) >= nq) return;
   const int whole = shared ? p1 : max(min(q.C / kPage, p1), p0);   // pages below are seen by all
   const T* pool = reinterpret_cast<const T*>(a.kv);
-  const size_t page_elems = (size_t)2 * a.G * kPage * HD;
+  const size_t page_elems = (size_t)2 * a.G * kPage * HD, values_at = (size_t)a.G * kPage * HD;
   // slots of page p that the lane's query sees
   auto seen = [&](const Tile& w, int p) {
     return seen_bits(a.vis ? a.vis + (size_t)(r0 + w.qi) * kVisWords : nullptr, w.qi, n, p * kPage - q.C);
   };
   Tile w;
   if (few) {
-    // One tile: the waves take every fourth page, each in LDS of its own.
+    // One tile (few of them read a page): the waves take every fourth page, each in LDS of its own, half
+    // a page a step.  The next step's keys come as soon as this one's scores
+    // are done, its values once this one's are used.
+    using Loader = PageLoader<T, HD, 1, 1>;
     w.init(a, r0, n, g, group);
-    char* mine = s_kv + wave * kOne;
+    constexpr int kFly = Loader::kPieces;
+    char *keys = s_kv + wave * kOne, *values = keys + kOne / 2;
+    auto entry = [&](int p) { return table[min(p, p1 - 1)]; };
+    auto read_done = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };  // before a load takes the place
     bool finite = true;
-    auto page = [&](auto edge, int p, auto use) {
-      const int id = batch_page_id(a.b, table[p]);
-      if (id < 0) return;
-      const T* keys = pool + (size_t)id * page_elems + (size_t)g * kPage * HD;
-      uint64_t bits = 0;
-      if constexpr (decltype(edge)::value) bits = seen(w, p);
+    // Pages p, p + 4, ... below `to`.
+    auto pages = [&](auto edge, int p, int to) {
+      if (p >= to) return;
+      constexpr bool kEdge = decltype(edge)::value;
+      int id = batch_page_id(a.b, same(entry(p))), after = entry(p + 4);
+      const T* page = pool + (size_t)max(id, 0) * page_elems + (size_t)g * kPage * HD;
+      Loader::keys(page, 0, 0, keys);
+      Loader::values(page + values_at, 0, 0, values);
 #pragma unroll 1
-      for (int t0 = 0; t0 < kPage; t0 += 32) {
-        PageLoader<T, HD, 1, 1>::load(keys, keys + (size_t)a.G * kPage * HD, t0, 0, mine);
-        wait_vm<0>();
-        use(mine, bits >> t0);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the next load takes the place of what was read
+      for (; p < to; p += 4) {
+        uint64_t bits = 0;
+        if constexpr (kEdge) bits = id >= 0 ? seen(w, p) : 0;
+        const int next = p + 4 < to ? batch_page_id(a.b, same(after)) : id;
+        after = entry(p + 8);
+        const T* next_page = pool + (size_t)max(next, 0) * page_elems + (size_t)g * kPage * HD;
+#pragma unroll 1
+        for (int t0 = 0; t0 < kPage; t0 += 32) {
+          const T* from = t0 ? next_page : page;  // where the next step's are (once more the last one's at the end)
+          const int at = t0 ? 0 : 32;
+          f32x16_t st[1];
+          wait_vm<kFly>();
+          w.template scores<1>(keys, st);
+          read_done();
+          Loader::keys(from, at, 0, keys);
+          if (kEdge || id >= 0) finite &= w.template outputs<1, kEdge>(st, values, bits >> t0, [] { wait_vm<kFly>(); });
+          else wait_vm<kFly>();  // a bad page's slots are seen by nobody
+          read_done();
+          Loader::values(from + values_at, at, 0, values);
+        }
+        id = next;
+        page = next_page;
       }
+      wait_vm<0>();
     };
-    int p = p0 + wave;
-#pragma unroll 1
-    for (; p < whole; p += 4)
-      page(std::false_type{}, p, [&](const char* t, uint64_t bits) { w.template step<1, false>(t, bits); });
-    const int edges = p;
-#pragma unroll 1
-    for (; p < p1; p += 4)
-      page(std::true_type{}, p,
-           [&](const char* t, uint64_t bits) { finite &= w.template step<1, true>(t, bits); });
+    pages(std::false_type{}, p0 + wave, whole);
+    const int edges = p0 + wave + (max(whole - p0 - wave, 0) + 3) / 4 * 4;
+    pages(std::true_type{}, edges, p1);
     if (!finite)
 #pragma unroll 1
-      for (p = edges; p < p1; p += 4)
-        page(std::true_type{}, p, [&](const char* t, uint64_t bits) { w.template infinite<1>(t, bits); });
+      for (int p = edges; p < p1; p += 4) {
+        const int id = batch_page_id(a.b, same(entry(p)));
+        if (id < 0) continue;
+        const uint64_t bits = seen(w, p);
+#pragma unroll 1
+        for (int t0 = 0; t0 < kPage; t0 += 32) {
+          Loader::values(pool + (size_t)id * page_elems + (size_t)g * kPage * HD + values_at, t0, 0, values);
+          wait_vm<0>();
+          w.template infinite<1>(values, bits >> t0);
+          read_done();
+        }
+      }
     // The waves' parts, dims by queries; each wave merges a quarter of the dims.
     w.l = pair_sum(w.l);
     __syncthreads();
@@ -381,45 +427,63 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_share
     }
     return;
   }
-  // Four tiles, one a wave, over pages that all share.
-  constexpr int kStep = 32 * KT, kTile = KT * kOne;
+  // Four tiles, one a wave, over pages that all share: steps of 32 KT keys,
+  // kStages - 1 of them on their way.
+  using Loader = PageLoader<T, HD, KT, 4>;
+  constexpr int kStep = 32 * KT, kTile = KT * kOne, kStages = 4, kFly = 2 * Loader::kPieces, kPerPage = kPage / kStep;
   w.init(a, r0, n, g, group * 4 + wave);
   const bool work = (group * 4 + wave) * 32 < nq;
-  auto entry = [&](int p) { return batch_page_id(a.b, __builtin_amdgcn_readfirstlane(table[p])); };
-  auto load = [&](int id, int t0, int buf) {
-    const T* keys = pool + (size_t)max(id, 0) * page_elems + (size_t)g * kPage * HD;
-    PageLoader<T, HD, KT, 4>::load(keys, keys + (size_t)a.G * kPage * HD, t0, wave, s_kv + buf * kTile);
-  };
-  // Pages [from, to), the next step's keys and values on their way while this one's are used.
+  // Pages [from, to).
   auto pages = [&](auto edge, int from, int to, auto use) {
+    constexpr bool kEdge = decltype(edge)::value;
     if (from >= to) return;
-    int id = entry(from), buf = 0;
-    load(id, 0, 0);
-#pragma unroll 1
-    for (int p = from; p < to; ++p) {
-      const int next = p + 1 < to ? entry(p + 1) : -1;
-      uint64_t bits = 0;
-      if constexpr (decltype(edge)::value) bits = seen(w, p);
-#pragma unroll 1
-      for (int t0 = 0; t0 < kPage; t0 += kStep) {
-        wait_vm<0>();
-        __syncthreads();
-        if (t0 + kStep < kPage) load(id, t0 + kStep, buf ^ 1);
-        else if (p + 1 < to) load(next, 0, buf ^ 1);
-        if (work && id >= 0) use(s_kv + buf * kTile, bits >> t0);
-        buf ^= 1;
+    const int steps = (to - from) * kPerPage;
+    auto entry = [&](int p) { return table[min(p, to - 1)]; };
+    // what is to be loaded next: its page, and the entry after that
+    int ahead = 0, id = batch_page_id(a.b, same(entry(from))), after = entry(from + 1);
+    uint32_t good = 0;   // whether the steps' pages can be used, the latest at bit 0
+    auto load = [&] {
+      const T* page = pool + (size_t)max(id, 0) * page_elems + (size_t)g * kPage * HD;
+      char* tile = s_kv + ahead % kStages * kTile;
+      const int t0 = ahead % kPerPage * kStep;
+      Loader::keys(page, t0, wave, tile);
+      Loader::values(page + values_at, t0, wave, tile + kTile / 2);
+      good = good << 1 | (id >= 0 ? 1 : 0);
+      if (++ahead % kPerPage == 0 && ahead < steps) {
+        id = batch_page_id(a.b, same(after));
+        after = entry(from + ahead / kPerPage + 1);
       }
-      id = next;
+    };
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) load();   // past the end: the last page once more
+    uint64_t bits = 0;
+#pragma unroll 1
+    for (int i = 0; i < steps; ++i) {
+      if constexpr (kEdge)
+        if (i % kPerPage == 0) bits = seen(w, from + i / kPerPage);
+      wait_vm<(kStages - 2) * kFly>();
+      __syncthreads();
+      const bool usable = work && (good >> (kStages - 2) & 1);
+      load();
+      if (usable) use(s_kv + i % kStages * kTile, bits >> (i % kPerPage * kStep));
     }
+    wait_vm<0>();
     __syncthreads();
   };
   bool finite = true;
-  pages(std::false_type{}, p0, whole, [&](const char* t, uint64_t bits) { w.template step<KT, false>(t, bits); });
+  pages(std::false_type{}, p0, whole, [&](const char* t, uint64_t bits) {
+    f32x16_t st[KT];
+    w.template scores<KT>(t, st);
+    w.template outputs<KT, false>(st, t + kTile / 2, bits, [] {});
+  });
   if (whole < p1) {
-    pages(std::true_type{}, whole, p1,
-          [&](const char* t, uint64_t bits) { finite &= w.template step<KT, true>(t, bits); });
+    pages(std::true_type{}, whole, p1, [&](const char* t, uint64_t bits) {
+      f32x16_t st[KT];
+      w.template scores<KT>(t, st);
+      finite &= w.template outputs<KT, true>(st, t + kTile / 2, bits, [] {});
+    });
     if (__syncthreads_or(!finite))
-      pages(std::true_type{}, whole, p1, [&](const char* t, uint64_t bits) { w.template infinite<KT>(t, bits); });
+      pages(std::true_type{}, whole, p1, [&](const char* t, uint64_t bits) { w.template infinite<KT>(t + kTile / 2, bits); });
   }
   if (!w.valid) return;
   w.l = pair_sum(w.l);
@@ -432,37 +496,41 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_share
     }
 }
 
-// Merges a row's parts in order, four dims of one row and head a thread.
-template <typename T>
+// Merges a row's parts, four dims of one row and head a thread.  SG threads
+// share an item, each taking every SG-th part, and join in LDS: the order does
+// not depend on timing.
+template <typename T, int SG>
 __global__ void __launch_bounds__(256) k_attention_shared_merge(SharedArgs a, int blocks) {
+  __shared__ float s_part[SG > 1 ? 256 : 1][6];
   const int s = blockIdx.x / blocks;
   Seq q;
   int pages;
   if (!batch_seq(a.b, s, q) || !shared_pages(a, s, q, pages)) return;
-  const int chunks = a.hd / 4, item = (blockIdx.x % blocks * 256 + threadIdx.x) / chunks, dim = threadIdx.x % chunks * 4;
-  if (item >= q.n * a.H) return;
-  const int head = item % a.H, row = q.r0 + item / a.H;
+  const int chunks = a.hd / 4, per = 256 / (chunks * SG), tid = threadIdx.x;
+  const int item = blockIdx.x % blocks * per + tid / (chunks * SG), group = tid / chunks % SG, dim = tid % chunks * 4;
+  const bool valid = item < q.n * a.H;
+  const int head = valid ? item % a.H : 0, row = q.r0 + (valid ? item / a.H : 0);
   const int own = (q.C + q.n + kPage - 1) / kPage - pages;
   const int c0 = part_pages(pages, a.shared_splits), c1 = part_pages(own, a.own_splits);
-  const int n0 = (pages + c0 - 1) / c0, n1 = (own + c1 - 1) / c1;
+  const int n0 = (pages + c0 - 1) / c0, n = n0 + (own + c1 - 1) / c1;
   const size_t stride = (size_t)a.b.n_rows * a.H, at = (size_t)row * a.H + head;
-  constexpr int kAhead = 8;  // parts in flight
+  constexpr int kFlight = 8;  // parts on their way at once
   float m = -INFINITY, l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-  for (int i0 = 0; i0 < n0 + n1; i0 += kAhead) {
-    float2 ml[kAhead];
-    float4 o[kAhead];
+  for (int i0 = group; i0 < n; i0 += kFlight * SG) {
+    float2 ml[kFlight];
+    float4 o[kFlight];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      const int i = min(i0 + j, n0 + n1 - 1);
+    for (int j = 0; j < kFlight; ++j) {
+      const int i = min(i0 + j * SG, n - 1);
       const size_t k = (i < n0 ? i : a.shared_splits + i - n0) * stride + at;
       ml[j] = *reinterpret_cast<const float2*>(a.ml_part + k * 2);
       o[j] = *reinterpret_cast<const float4*>(a.o_part + k * a.hd + dim);
     }
     float m_new = m;
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      if (i0 + j >= n0 + n1) ml[j] = make_float2(-INFINITY, 0.f);
+    for (int j = 0; j < kFlight; ++j) {
+      if (i0 + j * SG >= n) ml[j] = make_float2(-INFINITY, 0.f);
       m_new = fmaxf(m_new, ml[j].x);
     }
     const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
@@ -471,13 +539,33 @@ __global__ void __launch_bounds__(256) k_attention_shared_merge(SharedArgs a, in
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] *= alpha;
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
+    for (int j = 0; j < kFlight; ++j) {
       if (ml[j].x == -INFINITY && ml[j].y == 0.f) continue;  // nothing seen there (or no part)
       const float f = __builtin_amdgcn_exp2f(ml[j].x - m);
       l += ml[j].y * f;
       v[0] += o[j].x * f; v[1] += o[j].y * f; v[2] += o[j].z * f; v[3] += o[j].w * f;
     }
   }
+  if constexpr (SG > 1) {
+    float* p = s_part[tid];
+    p[0] = m; p[1] = l; p[2] = v[0]; p[3] = v[1]; p[4] = v[2]; p[5] = v[3];
+    __syncthreads();
+    if (group) return;
+    const float* x = s_part[tid];  // the groups' shares are `chunks` threads apart
+#pragma unroll
+    for (int j = 1; j < SG; ++j) m = fmaxf(m, x[j * chunks * 6]);
+    l = v[0] = v[1] = v[2] = v[3] = 0.f;
+#pragma unroll
+    for (int j = 0; j < SG; ++j) {
+      const float* y = x + j * chunks * 6;
+      if (y[0] == -INFINITY && y[1] == 0.f) continue;
+      const float f = __builtin_amdgcn_exp2f(y[0] - m);
+      l += y[1] * f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += y[2 + e] * f;
+    }
+  }
+  if (!valid) return;
   const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] = inv == 0.f ? 0.f : v[e] * inv;
@@ -485,18 +573,23 @@ __global__ void __launch_bounds__(256) k_attention_shared_merge(SharedArgs a, in
 }
 
 // ---- launch --------------------------------------------------------------------------
+// Up to kFewTiles tiles of queries have a workgroup each, whose waves split
+// its pages and join in LDS; more of them go four to a workgroup, one a wave,
+// which read a page once for all (7b heads, 128 shared pages: 64 sequences of
+// 2 rows, 28 tiles, 52 us and 57; of 4 rows, 56 tiles, 84 and 66).
 // Parts of kChunk pages or more, as many as give two workgroups a compute
-// unit; how many pages there are to split is known on the device, and the
-// host's bounds stand for it here.
+// unit (64 sequences of one row: 37 us, with twice as many parts 53); how many
+// pages there are to split is known on the device, and the host's bounds stand
+// for it here.
 void shared_plan(SharedArgs& a) {
   const int grp = a.H / a.G;
   auto tiles = [&](int64_t rows) { return (int)((rows * grp + 31) / 32); };
   const bool prefix = a.n_groups > 0 && a.max_pages > 0 && a.max_group_rows > 0;
   const int ts = prefix ? tiles(a.max_group_rows) : 0, to = tiles(a.b.max_rows);
-  a.shared_few = ts <= 1;
-  a.own_few = to <= 1;
-  a.shared_groups = a.shared_few ? 1 : (ts + 3) / 4;
-  a.own_groups = a.own_few ? 1 : (to + 3) / 4;
+  a.shared_few = ts <= kFewTiles;
+  a.own_few = to <= kFewTiles;
+  a.shared_groups = a.shared_few ? std::max(ts, 1) : (ts + 3) / 4;
+  a.own_groups = a.own_few ? to : (to + 3) / 4;
   const int shared = prefix ? a.max_pages : 0, all = (a.b.max_ctx + kPage - 1) / kPage;
   const int64_t base_s = prefix ? (int64_t)a.n_groups * a.G * a.shared_groups : 0;
   const int64_t base_o = (int64_t)a.b.n_seqs * a.G * a.own_groups;
@@ -519,8 +612,10 @@ template <typename T> static hipError_t shared_type(const SharedArgs& a, hipStre
   else k_attention_shared<T, 128><<<jobs, 256, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.parts == 1) return e;
-  const int per = 256 / (a.hd / 4), blocks = (a.b.max_rows * a.H + per - 1) / per;
-  k_attention_shared_merge<T><<<(unsigned)(a.b.n_seqs * blocks), 256, 0, st>>>(a, blocks);
+  const bool many = a.parts > 8;
+  const int per = 256 / (a.hd / 4 * (many ? 4 : 1)), blocks = (a.b.max_rows * a.H + per - 1) / per;
+  if (many) k_attention_shared_merge<T, 4><<<(unsigned)(a.b.n_seqs * blocks), 256, 0, st>>>(a, blocks);
+  else k_attention_shared_merge<T, 1><<<(unsigned)(a.b.n_seqs * blocks), 256, 0, st>>>(a, blocks);
   return hipGetLastError();
 }
 hipError_t launch_attention_shared(int dtype, SharedArgs& a, hipStream_t st) {

@@ -1310,7 +1310,7 @@ static jf_status shared_args(const jf_batch* batch, const jf_prefix* prefix, int
   shared_plan(*a);
   if (a->shared_jobs64 > kMaxBlocks || a->shared_jobs64 + a->own_jobs64 > kMaxBlocks)
     return fail(JF_E_CAPACITY, "the batch's workgroups exceed the %lld of a launch", (long long)kMaxBlocks);
-  return check_blocks(((int64_t)batch->max_rows * n_heads * (head_dim / 4) + 255) / 256, batch->n_seqs);
+  return check_blocks(((int64_t)batch->max_rows * n_heads * (head_dim / 4) * 4 + 255) / 256, batch->n_seqs);
 }
 
 // Parts' outputs, then (max, sum).

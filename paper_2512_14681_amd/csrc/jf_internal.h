@@ -409,7 +409,7 @@ struct SharedArgs {
   float* o_part;             // [parts][n_rows * H][hd]
   float* ml_part;            // [parts][n_rows * H][2]
   // the plan (shared_plan)
-  int shared_few, own_few;   // one tile of queries: the waves of a workgroup split its pages
+  int shared_few, own_few;   // a workgroup has one tile of queries, and its waves split the pages
   int shared_groups, own_groups;   // workgroups along the queries
   int shared_splits, own_splits;   // parts of the pages at most
   int parts;                 // their sum; 1: nothing to merge
