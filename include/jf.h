@@ -526,7 +526,8 @@ jf_status jf_token_logprobs_grad(int32_t R, int32_t V, int32_t dtype, const void
  * read nor written.  A captured call takes new starts at every replay.  A
  * sequence whose start or end lies outside [0, n_rows], or whose end lies
  * before its start, is left as it was and JF_FLAG_CAPACITY is raised in
- * d_flags (optional, one int32, ORed; the caller clears it).
+ * d_flags (optional, one int32, ORed; the caller clears it); among more than
+ * 64 sequences others may then be left as they were too.
  * d_q, d_out [n_rows][n_heads * head_dim], d_k, d_v [n_rows][n_kv_heads *
  * head_dim] are rows of dtype (JF_F32 or JF_BF16), ld_* elements apart (views
  * into one fused projection, for instance); query head j reads KV head j /
@@ -549,8 +550,10 @@ jf_status jf_attention_causal(int32_t n_seqs, int32_t n_rows, const int32_t *d_r
  * tensors are of dtype; the gradients must overlap no input (but may be
  * columns of one tensor).  Nothing depends on the order in which workgroups
  * run.  An infinity or NaN among a sequence's inputs may reach every gradient
- * of that sequence, and none of another's.  d_ws, on a 16-byte boundary,
- * holds jf_attention_causal_grad_ws_bytes(...) bytes, needs no clearing and
+ * of that sequence, and none of another's.  Weights are computed anew from
+ * d_lse, whose fp32 digits hold them for scores up to 2^20 or so (beyond,
+ * they are still at most 1).  d_ws, on a 16-byte boundary, holds
+ * jf_attention_causal_grad_ws_bytes(...) bytes, needs no clearing and
  * may be shared by calls that do not overlap. */
 size_t jf_attention_causal_grad_ws_bytes(int32_t n_seqs, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads,
                                          int32_t head_dim);

@@ -32,44 +32,85 @@ struct RowBlock {
   int r0, n, t, blocks;
 };
 
-// Block number `rank` of all sequences' blocks, one after the other.  The
-// first workgroup raises JF_FLAG_CAPACITY for row starts beyond the rows or
-// decreasing ones; no address is formed from those.
-template <int kBlock> __device__ __forceinline__ bool find_block(const CausalArgs& a, int rank, RowBlock& b) {
+// The block that workgroup number `rank` works on (none: no blocks).  Among up to
+// 64 sequences the ones with the most work come first: work grows with a
+// block's number (kFirst: with its distance from the sequence's end).  Among
+// more, sequence s's blocks have the numbers from (its start) / kBlock + s on,
+// which no two sequences share, and s is searched for, 64 places at a time.
+// The first workgroup raises JF_FLAG_CAPACITY for row starts beyond the rows
+// or decreasing ones; no address is formed from those.
+template <int kBlock, bool kFirst> __device__ __forceinline__ RowBlock search_block(const CausalArgs& a, int rank) {
+  constexpr int kMostSearched = 256;  // blocks of a sequence, for which the order is looked for
   const int lane = threadIdx.x & 63;
-  const bool first = blockIdx.x == 0;
-  int base = 0;
-  bool found = false, bad = false;
-  for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-    const int s = s0 + lane;
-    int r0 = 0, r1 = 0;
-    if (s < a.n_seqs) {
-      r0 = a.row_start[s];
-      r1 = a.row_start[s + 1];
-    }
-    const bool ok = r0 >= 0 && r1 >= r0 && r1 <= a.n_rows;
-    bad |= !ok;
-    const int blocks = ok ? (r1 - r0 + kBlock - 1) / kBlock : 0;
-    int upto = blocks;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int v = __shfl_up(upto, d);
-      if (lane >= d) upto += v;
-    }
-    const uint64_t hit = __ballot(base + upto > rank);
-    if (!found && hit) {
-      const int l = __builtin_ctzll(hit);
-      b.blocks = __builtin_amdgcn_readlane(blocks, l);
-      b.t = rank - base - (__builtin_amdgcn_readlane(upto, l) - b.blocks);
-      b.r0 = __builtin_amdgcn_readlane(r0, l);
-      b.n = __builtin_amdgcn_readlane(r1, l) - b.r0;
-      found = true;
-      if (!first) break;
-    }
-    base += __builtin_amdgcn_readlane(upto, 63);
+  const uint64_t before = (1ull << lane) - 1;
+  auto valid = [&](int r0, int r1) { return r0 >= 0 && r1 >= r0 && r1 <= a.n_rows; };
+  if (blockIdx.x == 0 && a.flags) {
+    bool bad = false;
+    for (int s = threadIdx.x; s < a.n_seqs; s += 256) bad |= !valid(a.row_start[s], a.row_start[s + 1]);
+    if (bad) atomicOr(a.flags, kFlagCapacity);
   }
-  if (first && a.flags && (__any(bad) || base > a.blocks) && threadIdx.x == 0) atomicOr(a.flags, kFlagCapacity);
-  return found;
+  if (a.n_seqs <= 64) {
+    int r0 = 0, r1 = 0;
+    if (lane < a.n_seqs) {
+      r0 = a.row_start[lane];
+      r1 = a.row_start[lane + 1];
+    }
+    const int blocks = valid(r0, r1) ? (r1 - r0 + kBlock - 1) / kBlock : 0;
+    int total = blocks, most = blocks;
+    if (a.n_seqs > 1) {
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        total += __shfl_xor(total, d);
+        most = max(most, __shfl_xor(most, d));
+      }
+    }
+    total = __builtin_amdgcn_readfirstlane(total);
+    most = __builtin_amdgcn_readfirstlane(most);
+    if (rank >= total) return RowBlock{0, 0, 0, 0};
+    int l = 0, u = most - 1 - rank;  // of one sequence
+    if (a.n_seqs > 1) {
+      int left = rank;
+      if (most <= kMostSearched) {   // of every sequence its longest, then of every one its next, ...
+        for (u = most - 1;; --u) {
+          const int n = __builtin_popcountll(__ballot(blocks > u));
+          if (left < n) break;
+          left -= n;
+        }
+        const uint64_t has = __ballot(blocks > u);
+        l = __builtin_ctzll(__ballot(blocks > u && __builtin_popcountll(has & before) == left));
+      } else {                       // one sequence after the other
+        for (;; ++l) {
+          const int n = __builtin_amdgcn_readlane(blocks, l);
+          if (left < n) break;
+          left -= n;
+        }
+        u = __builtin_amdgcn_readlane(blocks, l) - 1 - left;
+      }
+    }
+    const int n = __builtin_amdgcn_readlane(blocks, l), at = __builtin_amdgcn_readlane(r0, l);
+    return RowBlock{at, __builtin_amdgcn_readlane(r1, l) - at, kFirst ? n - 1 - u : u, n};
+  }
+  // the last sequence whose blocks start at `rank` or before: in [lo, lo + span)
+  const int r = a.row_start[0];
+  int lo = 0, span = a.n_seqs;
+  auto number = [&](int s) { return (int)(((int64_t)a.row_start[s] - r) / kBlock) + s; };
+  while (span > 1) {
+    const int step = (span + 63) / 64, at = lane * step;
+    const uint64_t has = __ballot(at < span && number(lo + at) <= rank);
+    if (!has) return RowBlock{0, 0, 0, 0};
+    const int l = 63 - __builtin_clzll(has);
+    span = min(step, span - l * step);
+    lo += l * step;
+  }
+  const int r0 = a.row_start[lo], r1 = a.row_start[lo + 1], t = rank - number(lo);
+  const int blocks = valid(r0, r1) ? (r1 - r0 + kBlock - 1) / kBlock : 0;
+  return t >= 0 && t < blocks ? RowBlock{r0, r1 - r0, kFirst ? t : blocks - 1 - t, blocks} : RowBlock{0, 0, 0, 0};
+}
+template <int kBlock, bool kFirst> __device__ __forceinline__ bool find_block(const CausalArgs& a, int rank, RowBlock& b) {
+  const RowBlock x = search_block<kBlock, kFirst>(a, rank);
+  b = RowBlock{__builtin_amdgcn_readfirstlane(x.r0), __builtin_amdgcn_readfirstlane(x.n),   // in scalar registers,
+               __builtin_amdgcn_readfirstlane(x.t), __builtin_amdgcn_readfirstlane(x.blocks)};  // as loads to LDS take them
+  return b.blocks > 0;
 }
 
 // Workgroups go around the 8 XCDs in order: the heads of a group, which read
@@ -90,7 +131,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // weights of a step sum to more than kMost: most steps look for no maximum
 // and leave sums and outputs as they are.  kDown keeps sums of weights below
 // 1, so that no sum of values overflows that has a finite mean.
-constexpr float kDown = 32.f, kMost = 0x1p-22f;
+// A maximum beyond kFar is too coarse to hold kDown beside it: the weights are
+// held below 2^(4 - kDown) one by one.
+constexpr float kDown = 32.f, kMost = 0x1p-22f, kFar = 1 << 20;
 
 // Four waves work on blocks of 32 NQ queries (keys, for dk and dv): NQ = 4
 // gives each wave 32 of its own; with fewer, kShare waves have the same ones
@@ -150,8 +193,7 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal(CausalArgs a) {
   const int grp = a.H / a.G;
   const Work job = work_of(a.G, grp);
   RowBlock b;
-  if (!find_block<S::kBlock>(a, job.rank, b)) return;
-  b.t = b.blocks - 1 - b.t;  // the longest first
+  if (!find_block<S::kBlock, false>(a, job.rank, b)) return;
   const int head = job.g * grp + job.h;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
   const int share = wave / NQ, from = share * 32 * KT; // the wave's rows of a step
@@ -174,6 +216,7 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal(CausalArgs a) {
   }
   const float c = kLog2e / sqrtf((float)HD);
   float m = -INFINITY, l = 0.f;
+  bool far = false;
   f32x16_t o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = zero16();
@@ -213,19 +256,36 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal(CausalArgs a) {
         }
     };
     weights(-kDown - m);  // nothing seen yet: infinite or NaN
-    if (__builtin_expect(__any(!(sum <= kMost)), 0)) {
+    if (__builtin_expect(__any(!(sum <= kMost)) || far, 0)) {
       float mx = st[0][0];
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[kt][i]);
-      const float m_new = fmaxf(m, pair_max(mx) * c), m_use = m_new == -INFINITY ? 0.f : m_new;
+      mx = pair_max(mx);
+      float top = mx * c;
+      // beyond 2^24 the rounded product may lie far above the score itself, which would lose all weight
+      if (__builtin_fmaf(mx, c, -top) < -1.f) top -= fabsf(top) * 0x1p-23f;
+      const float m_new = fmaxf(m, top), m_use = m_new == -INFINITY ? 0.f : m_new;
       const float alpha = __builtin_amdgcn_exp2f(m - m_use);
       m = m_new;
       l *= alpha;
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[d] *= alpha;
-      weights(-kDown - m_use);
+      far = __any(fabsf(m_use) > kFar);
+      if (far) {
+        sum = 0.f;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float d = __builtin_fmaf(st[kt][i], c, -m_use);
+            w[kt][i] = __builtin_amdgcn_exp2f((d > 4.f ? 4.f : d) - kDown);  // NaN stays
+            sum += w[kt][i];
+          }
+      } else {
+        weights(-kDown - m_use);
+      }
     }
     l += sum;
     bool finite = true;
@@ -316,6 +376,9 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal(CausalArgs a) {
 
 // ---- gradient ------------------------------------------------------------------------
 
+// 2^x, at most 1: scores beyond 2^20 are too coarse beside the rounded lse.
+__device__ __forceinline__ float weight(float x) { return __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(x), 0.f, 1.f); }
+
 // dq; and of each row and head, for dk and dv, what the accumulators of its
 // scores and of do v start from: -lse sqrt(hd) (-inf for a row without
 // weights, whose weights then are 0), and -D.
@@ -329,8 +392,7 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dq(CausalGradArgs 
   const int grp = a.f.H / a.f.G;
   const Work job = work_of(a.f.G, grp);
   RowBlock b;
-  if (!find_block<S::kBlock>(a.f, job.rank, b)) return;
-  b.t = b.blocks - 1 - b.t;  // the longest first
+  if (!find_block<S::kBlock, false>(a.f, job.rank, b)) return;
   const int head = job.g * grp + job.h;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
   const int share = wave / NQ, from = share * 32 * KT;
@@ -401,7 +463,7 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dq(CausalGradArgs 
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float ds = __builtin_amdgcn_exp2f(__builtin_fmaf(st[i], c, -lse)) * (dp[i] - dot);
+        const float ds = weight(__builtin_fmaf(st[i], c, -lse)) * (dp[i] - dot);
         st[i] = kEdge && 32 * kt + acc_row(i) > lim ? 0.f : ds;
       }
 #pragma unroll
@@ -451,7 +513,7 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dkv(CausalGradArgs
   const int grp = a.f.H / a.f.G;
   const Work job = work_of(a.f.G, a.parts);
   RowBlock b;
-  if (!find_block<S::kBlock>(a.f, job.rank, b)) return;  // in order: the first keys have the most queries
+  if (!find_block<S::kBlock, true>(a.f, job.rank, b)) return;  // the first keys have the most queries
   const int part = job.h;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
   const int share = wave / NQ, from = share * 32 * KT;  // the wave's rows of a step
@@ -539,7 +601,7 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dkv(CausalGradArgs
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const bool hidden = edge && acc_row(i) < lim;
-          st[i] = __builtin_amdgcn_exp2f(st[i] * c);
+          st[i] = weight(st[i] * c);
           dp[i] = hidden ? 0.f : st[i] * dp[i];
           st[i] = hidden ? 0.f : st[i];
         }

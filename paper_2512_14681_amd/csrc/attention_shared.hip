@@ -28,8 +28,10 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 // Weights are 2^(s - m - kDown).  m follows a row's maximum only when a lane's
 // weights of a step sum to more than kMost.  kDown keeps sums of weights below
-// 1, so that no sum of values overflows that has a finite mean.
-constexpr float kDown = 32.f, kMost = 0x1p-22f;
+// 1, so that no sum of values overflows that has a finite mean.  A maximum
+// beyond kFar is too coarse to hold kDown beside it: the weights are held
+// below 2^(4 - kDown) one by one.
+constexpr float kDown = 32.f, kMost = 0x1p-22f, kFar = 1 << 20;
 constexpr int kChunk = 4;      // pages of a part at least
 constexpr int kWorkgroups = 512;  // as many as run at once
 constexpr int kFewTiles = 32;     // tiles of a group's or sequence's queries that have workgroups of their own
@@ -101,7 +103,7 @@ template <typename T, int HD> struct SharedTile {
   static constexpr int NS = HD / 16, ND = HD / 32;
   Query<T> q[NS];
   int qi, qhd;    // the lane's query: row among the job's, head
-  bool valid;
+  bool valid, far;  // far (of all lanes): maxima beyond kFar
   float m, l;
   f32x16_t o[ND];
 
@@ -118,6 +120,7 @@ template <typename T, int HD> struct SharedTile {
     for (int s = 0; s < NS; ++s) settle_query(q[s]);
     m = -INFINITY;
     l = 0.f;
+    far = false;
 #pragma unroll
     for (int d = 0; d < ND; ++d) o[d] = zero16();
   }
@@ -158,19 +161,36 @@ template <typename T, int HD> struct SharedTile {
         }
     };
     weights(-kDown - m);  // nothing seen yet: infinite or NaN
-    if (__builtin_expect(__any(!(sum <= kMost)), 0)) {
+    if (__builtin_expect(__any(!(sum <= kMost)) || far, 0)) {
       float mx = st[0][0];
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[kt][i]);
-      const float m_new = fmaxf(m, pair_max(mx) * c), m_use = m_new == -INFINITY ? 0.f : m_new;
+      mx = pair_max(mx);
+      float top = mx * c;
+      // beyond 2^24 the rounded product may lie far above the score itself, which would lose all weight
+      if (__builtin_fmaf(mx, c, -top) < -1.f) top -= fabsf(top) * 0x1p-23f;
+      const float m_new = fmaxf(m, top), m_use = m_new == -INFINITY ? 0.f : m_new;
       const float alpha = __builtin_amdgcn_exp2f(m - m_use);
       m = m_new;
       l *= alpha;
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[d] *= alpha;
-      weights(-kDown - m_use);
+      far = __any(fabsf(m_use) > kFar);
+      if (far) {
+        sum = 0.f;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float d = __builtin_fmaf(st[kt][i], c, -m_use);
+            w[kt][i] = __builtin_amdgcn_exp2f((d > 4.f ? 4.f : d) - kDown);  // NaN stays
+            sum += w[kt][i];
+          }
+      } else {
+        weights(-kDown - m_use);
+      }
     }
     l += sum;
     arrive();
@@ -597,7 +617,7 @@ void shared_plan(SharedArgs& a) {
   int chunk = std::max(kChunk, (std::max(shared, all) + 63) / 64);
   while (chunk < std::max(shared, own) &&
          base_s * ((shared + chunk - 1) / chunk) + base_o * ((own + chunk - 1) / chunk) > kWorkgroups)
-    chunk += 4;
+    chunk += std::max(chunk / 8, 4) / 4 * 4;
   a.shared_splits = prefix ? (shared + chunk - 1) / chunk : 0;
   a.own_splits = (own + chunk - 1) / chunk;
   a.parts = a.shared_splits + a.own_splits;

@@ -297,19 +297,19 @@ __global__ void __launch_bounds__(256) k_policy(PolicyArgs a) {
 // The workgroups' sums, in order.  A launch of its own: that the workgroup
 // which ends last does it needs a release by each of them, which writes its
 // L2's changed lines back (960 thousand rows: 49 us for k_policy, 11 without).
-__global__ void __launch_bounds__(1024) k_policy_stats(PolicyArgs a) {
-  __shared__ double s_part[16][kTerms];
+__global__ void __launch_bounds__(256) k_policy_stats(PolicyArgs a) {
+  __shared__ double s_part[4][kTerms];
   __shared__ int s_bad;
   const PolicyWs ws = policy_ws(a);
   if (threadIdx.x == 0) s_bad = 0;
   __syncthreads();
   double t[kTerms] = {0, 0, 0, 0, 0};
-  for (int b = threadIdx.x; b < a.blocks; b += 1024) {
+  for (int b = threadIdx.x; b < a.blocks; b += 256) {
     if (ws.block[b] < 0) s_bad = 1;
 #pragma unroll
     for (int i = 0; i < kTerms; ++i) t[i] += ws.part[(size_t)b * kTerms + i];
   }
-  block_sum<1024>(t, s_part);
+  block_sum<256>(t, s_part);
   if (threadIdx.x == 0) {
     if (s_bad) policy_bad(a);
     else policy_stats(a, t);
@@ -325,7 +325,7 @@ hipError_t launch_policy(PolicyArgs& a, hipStream_t st) {
   if (a.mean == 1) k_policy_clear<<<(unsigned)((a.n_seqs + 255) / 256), 256, 0, st>>>(a);
   k_policy_count<<<(unsigned)a.blocks, 256, 0, st>>>(a);
   k_policy<<<(unsigned)a.blocks, 256, 0, st>>>(a);
-  k_policy_stats<<<1, 1024, 0, st>>>(a);
+  k_policy_stats<<<1, 256, 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -262,6 +262,76 @@ def test_large_scores():
     assert bool(((got["out"] - value).abs() <= bound).all())
 
 
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_beyond_what_fp32_tells_apart(name, sign):
+    """Scores of 2^31 and more (exact in fp32), in even steps of 2^25: the largest one that a row sees has all the weight;
+    equal ones share it.  The gradients there have no digits but stay finite."""
+    torch = _torch()
+    dims, n, hd = "one", 60, 64
+    c = case([n], dims, name, seed=31)
+    for t in ("q", "k"):
+        c[t].zero_()
+    c["q"][:, 0] = 2.0 ** 17
+    c["k"][:, 0] = sign * 2.0 ** 17 * (1 + torch.arange(n) / 64)
+    call = Call(c, [0, n], dims, name)
+    call.forward()
+    call.backward()
+    got = call.results()
+    v = c["v"].double()
+    assert bool((got["out"] == (v if sign > 0 else v[:1].expand(n, -1))).all())
+    assert all(bool(got[t].isfinite().all()) for t in got)
+    c["k"][:, 0] = sign * 2.0 ** 17
+    call = Call(c, [0, n], dims, name)
+    call.forward()
+    u = 2.0 ** -8 if name == "bf16" else 2.0 ** -24
+    mean = v.cumsum(0) / torch.arange(1, n + 1)[:, None]
+    mag = v.abs().cumsum(0) / torch.arange(1, n + 1)[:, None]
+    assert bool(((call.results()["out"] - mean).abs() <= (2 * u + 100 * 2.0 ** -24) * (mag + mean.abs())).all())
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+def test_values_next_to_the_largest(name):
+    """Sums of many values of 2^127 have a mean that fits, whatever the order of the maxima."""
+    torch = _torch()
+    dims, n = "grp3", 500
+    c = case([n], dims, name, seed=32)
+    c["v"] = (2.0 ** 127 * torch.sign(c["v"].double() + 2.5)).to(c["v"].dtype)
+    want = reference(dict(c, do=c["do"] * 0), [n], dims, name)["out"]
+    call = Call(c, [0, n], dims, name)
+    call.forward()
+    got = call.results()["out"]
+    assert bool(((got - want[0]).abs() <= want[1]).all())
+
+
+def test_thousands_of_short_sequences():
+    torch = _torch()
+    g = torch.Generator().manual_seed(33)
+    lens = torch.randint(0, 4, (5000,), generator=g).tolist()
+    lens[4000] = 300
+    dims, name = "one", "bf16"
+    c = case(lens, dims, name, seed=34)
+    call = Call(c, np.cumsum([0] + lens).tolist(), dims, name)
+    call.forward()
+    call.backward()
+    close(call.results(), reference(c, lens, dims, name))
+    assert int(call.flags) == 0
+
+
+def test_bad_starts_among_many_sequences():
+    """More than 64 sequences: flagged, and nothing outside the good ones is written."""
+    from paper_2512_14681_amd import jf
+    R, dims, name = 300, "grp3", "bf16"
+    c = case([R], dims, name, seed=35)
+    starts = list(range(0, 3 * 80, 3)) + [500, 250, 260]
+    call = Call(c, starts, dims, name)
+    call.forward()
+    call.backward()
+    got = call.results()
+    assert int(call.flags) == jf.JF_FLAG_CAPACITY
+    assert bool((got["out"][260:] == 7.0).all()) and bool((got["dk"][260:] == 7.0).all())
+
+
 @pytest.mark.parametrize("starts", [[0, 300, 410], [0, -5, 410], [-1, 200, 410], [0, 200, 411], [0, 250, 200]])
 def test_bad_starts_are_flagged_and_left_alone(starts):
     """Sequences inside the rows are computed; what does not fit raises JF_FLAG_CAPACITY, nothing outside is written."""

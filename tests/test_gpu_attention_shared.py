@@ -254,6 +254,40 @@ def test_what_a_row_does_not_see_does_not_reach_it(name, rows):
     assert ok.all()
 
 
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 30])   # slots below 128: 1 + slot / 128 is a bf16 number
+def test_scores_beyond_what_fp32_tells_apart(name, rows):
+    """Scores of 2^31 and more, in even steps, the largest in the shared pages or in a sequence's own: it has all the
+    weight; sums of values of 2^126 have a mean that fits."""
+    torch = _torch()
+    for sign in (1, -1):
+        c = Call([(1, [(30, rows), (3, 2)])], "grp3", name, seed=20)
+        n = c.G * PAGE * c.hd
+        c.q.zero_()
+        c.q[0, :, :, 0] = 2.0 ** 17
+        c.q64 = c.q.double().sum(0).cpu()
+        for s, (p, ctx, r) in enumerate(c.members):
+            for b in range((p * PAGE + ctx + r + PAGE - 1) // PAGE):
+                slots = torch.arange(b * PAGE, b * PAGE + PAGE)
+                page = int(c.table_np[s, b])
+                c.k[page] = 0.0
+                c.k[page, :, :, 0] = sign * 2.0 ** 17 * (1 + slots / 128)
+                c.v[page] = torch.where(c.v[page].isnan(), c.v[page], 2.0 ** 126 * torch.sign(c.v[page]))
+        c.kv[:, :n] = c.k.reshape(len(c.k), -1).to(c.kv.dtype).cuda()
+        c.kv[:, n:] = c.v.transpose(2, 3).reshape(len(c.v), -1).to(c.kv.dtype).cuda()
+        c.run()
+        got = c.result()
+        for s, (p, ctx, r) in enumerate(c.members):
+            for i in range(r):
+                at = p * PAGE + ctx + i if sign > 0 else 0
+                v = c.v[int(c.table_np[s, at // PAGE]), :, at % PAGE].repeat_interleave(c.H // c.G, 0)
+                assert bool((got[int(c.starts[s]) + i] == v).all()), (sign, s, i)
+        c.q.zero_()      # equal scores: the mean
+        c.q64 = c.q.double().sum(0).cpu()
+        c.flags.zero_()
+        c.run().check()
+
+
 def test_bad_pages_are_skipped():
     """Entries outside the pool: flagged, their slots seen by nobody; a shared page's by the whole group."""
     from paper_2512_14681_amd import jf
