@@ -536,9 +536,13 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dkv(CausalGradArgs
     dk[d] = zero16();
     dv[d] = zero16();
   }
-  // The steps: every head's rows from the block's first key on, one head after the other.
-  const int first = b.t * S::kBlock, steps = (b.n - first + kRows - 1) / kRows;
-  int head = job.g * grp + part, i0 = first;
+  // The steps: every head's rows from the sequence's end to the block's first
+  // key, one head after the other.  From the end, as workgroups that run at
+  // once then read the same rows at about the same time (4096 rows, 28 query
+  // and 4 KV heads: 27% of the accesses miss the L2, in the other order 56%,
+  // and a forward and backward pass takes 1.3% longer).
+  const int first = b.t * S::kBlock, steps = (b.n - first + kRows - 1) / kRows, top = first + (steps - 1) * kRows;
+  int head = job.g * grp + part, i0 = top;
   float2 dots = make_float2(-INFINITY, 0.f);
   auto load = [&](int buf) {
     const int row = i0 + (int)threadIdx.x;
@@ -550,9 +554,9 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dkv(CausalGradArgs
                  b.n - 1 - i0, s_qg[buf][0]);
     Loader::load(reinterpret_cast<const T*>(a.g_out) + (size_t)(b.r0 + i0) * a.ld_g_out + head * HD,
                  a.ld_g_out * sizeof(T), b.n - 1 - i0, s_qg[buf][1]);
-    i0 += kRows;
-    if (i0 >= b.n) {
-      i0 = first;
+    i0 -= kRows;
+    if (i0 < first) {
+      i0 = top;
       head += a.parts;
     }
   };
@@ -567,7 +571,7 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dkv(CausalGradArgs
   settle(k);
   settle(v);
   const int heads = (grp - part + a.parts - 1) / a.parts, total = heads * steps;
-  int at = first, buf = 0;
+  int at = top, buf = 0;
 #pragma unroll 1
   for (int it = 0; it < total; ++it) {
     if constexpr (kVec) wait_vm<0>();
@@ -626,8 +630,8 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dkv(CausalGradArgs
     }
     if (it + 1 < total) put_dots(buf ^ 1);
     buf ^= 1;
-    at += kRows;
-    if (at >= b.n) at = first;
+    at -= kRows;
+    if (at < first) at = top;
   }
 
   if constexpr (S::kShare > 1) {

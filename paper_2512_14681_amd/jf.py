@@ -538,23 +538,18 @@ def _starts(dev, t):
     return _at(dev, t), t.numel() - 1
 
 
-def _causal_rows(n_heads, n_kv_heads, head_dim, wide, narrow):
-    """(jf_dtype, rows, strides of `wide` and of `narrow`): [rows][n_heads * head_dim] and [rows][n_kv_heads * head_dim]
-    tensors of one type and as many rows as the first."""
-    n = wide[0].shape[0]
-    kinds = [_rows(t, n, n_heads * head_dim) for t in wide] + [_rows(t, n, n_kv_heads * head_dim) for t in narrow]
-    x = kinds[0][0]
-    for code, _ in kinds:
-        if code != x:
-            raise TypeError("all rows have one type")
-    return x, n, [ld for _, ld in kinds]
-
-
 def attention_causal(d_row_start, n_heads, n_kv_heads, head_dim, d_q, d_k, d_v, d_out, d_lse=None, d_flags=None,
                      stream=None):
     """Rows of d_q [rows][n_heads * head_dim] over those of d_k and d_v up to their own, sequence by sequence, to d_out;
     d_lse [n_heads][rows] for attention_causal_grad."""
-    x, n, (ld_q, ld_out, ld_k, ld_v) = _causal_rows(n_heads, n_kv_heads, head_dim, (d_q, d_out), (d_k, d_v))
+    wide, narrow = n_heads * head_dim, n_kv_heads * head_dim
+    x, ld_q = _rows(d_q, 0, wide)
+    n = d_q.shape[0]
+    xo, ld_out = _rows(d_out, n, wide)
+    xk, ld_k = _rows(d_k, n, narrow)
+    xv, ld_v = _rows(d_v, n, narrow)
+    if not x == xo == xk == xv:
+        raise TypeError("all rows have one type")
     dev = _current_device()
     start, n_seqs = _starts(dev, d_row_start)
     _count(n, n_seqs)
@@ -578,8 +573,14 @@ def attention_causal_grad_ws_bytes(n_seqs, n_rows, n_heads, n_kv_heads, head_dim
 def attention_causal_grad(d_row_start, n_heads, n_kv_heads, head_dim, d_q, d_k, d_v, d_out, d_lse, d_g_out, d_g_q, d_g_k,
                           d_g_v, d_ws, d_flags=None, stream=None):
     """Gradient of sum(d_g_out * d_out) to queries, keys and values, from attention_causal's inputs and outputs."""
-    x, n, (ld_q, ld_out, ld_g, ld_gq, ld_k, ld_v, ld_gk, ld_gv) = _causal_rows(
-        n_heads, n_kv_heads, head_dim, (d_q, d_out, d_g_out, d_g_q), (d_k, d_v, d_g_k, d_g_v))
+    wide, narrow = n_heads * head_dim, n_kv_heads * head_dim
+    x, ld_q = _rows(d_q, 0, wide)
+    n = d_q.shape[0]
+    (xo, ld_out), (xg, ld_g), (x1, ld_gq) = _rows(d_out, n, wide), _rows(d_g_out, n, wide), _rows(d_g_q, n, wide)
+    (xk, ld_k), (xv, ld_v) = _rows(d_k, n, narrow), _rows(d_v, n, narrow)
+    (x2, ld_gk), (x3, ld_gv) = _rows(d_g_k, n, narrow), _rows(d_g_v, n, narrow)
+    if not x == xo == xg == x1 == xk == xv == x2 == x3:
+        raise TypeError("all rows have one type")
     dev = _current_device()
     start, n_seqs = _starts(dev, d_row_start)
     status = lib().jf_attention_causal_grad(
