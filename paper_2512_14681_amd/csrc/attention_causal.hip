@@ -16,8 +16,8 @@
 // they are, and read transposed.
 //
 // bf16: weights p and ds enter the second products rounded to bf16, as the
-// inputs there are (2^-9 of each of many terms of a sum; the result is
-// rounded to as much itself).  Sums, maxima and statistics are fp32.
+// inputs there are (2^-8 at most of each of many terms of a sum; the result
+// is rounded to as much itself).  Sums, maxima and statistics are fp32.
 #include <algorithm>
 #include <type_traits>
 
@@ -677,30 +677,36 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dkv(CausalGradArgs
   }
 }
 
-// Sums the parts in order, four columns a thread.
-template <typename T>
-__global__ void __launch_bounds__(256) k_causal_join(CausalGradArgs a) {
-  const int width = a.f.G * a.f.hd, chunks = width / 4;
-  const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int row = (int)(item / chunks), col = (int)(item % chunks) * 4;
-  if (row >= a.f.n_rows || row < a.f.row_start[0] || row >= a.f.row_start[a.f.n_seqs]) return;
-  const size_t plane = (size_t)a.f.n_rows * width;
-  const float* p = a.kv_part + (size_t)row * width + col;
-#pragma unroll
-  for (int which = 0; which < 2; ++which) {
+// Sums the parts of a block's rows in order, four columns a thread; kSlices
+// workgroups share a block.
+constexpr int kSlices = 8;
+template <typename T, int NQ> __global__ void __launch_bounds__(256) k_causal_join(CausalGradArgs a) {
+  const Work job = work_of(a.f.G, kSlices);
+  RowBlock b;
+  if (!find_block<32 * NQ, true>(a.f, job.rank, b)) return;
+  constexpr int kRows = 32 * NQ / kSlices;
+  const int chunks = a.f.hd / 4, col = job.g * a.f.hd + threadIdx.x % chunks * 4;
+  const size_t width = (size_t)a.f.G * a.f.hd, plane = a.f.n_rows * width;
+  for (int i = threadIdx.x / chunks; i < 2 * kRows; i += 256 / chunks) {  // the keys', then the values'
+    const int r = b.t * 32 * NQ + job.h * kRows + i % kRows;
+    if (r >= b.n) continue;
+    const size_t row = b.r0 + r;
+    const float* p = a.kv_part + row * width + col + (i < kRows ? 0 : a.parts * plane);
     float4 s = *reinterpret_cast<const float4*>(p);
-    for (int i = 1; i < a.parts; ++i) {
-      const float4 x = *reinterpret_cast<const float4*>(p + i * plane);
+    for (int k = 1; k < a.parts; ++k) {
+      const float4 x = *reinterpret_cast<const float4*>(p + k * plane);
       s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
     }
-    T* out = which ? reinterpret_cast<T*>(a.g_v) + (size_t)row * a.ld_g_v : reinterpret_cast<T*>(a.g_k) + (size_t)row * a.ld_g_k;
+    T* out = i < kRows ? reinterpret_cast<T*>(a.g_k) + row * a.ld_g_k : reinterpret_cast<T*>(a.g_v) + row * a.ld_g_v;
     row_store4<T>(out + col, a.vec_kv, s.x, s.y, s.z, s.w);
-    p += a.parts * plane;
   }
 }
 
 // ---- launch --------------------------------------------------------------------------
+// Bound on the blocks' numbers (search_block): among more than 64 sequences
+// empty ones count too.
 static int blocks_of(int n_rows, int n_seqs, int rows) {
+  if (n_seqs > 64) return (int)std::min<int64_t>((int64_t)n_rows / rows + n_seqs, 1 << 30);
   return (int)std::min<int64_t>((int64_t)n_rows / rows + std::min(n_seqs, n_rows), n_rows);
 }
 
@@ -770,8 +776,10 @@ template <typename T> static hipError_t causal_grad_type(const CausalGradArgs& a
     k_causal_dkv<T, HD, NQ, decltype(vec)::value><<<dkv, 256, 0, st>>>(a);
   });
   if (e != hipSuccess || a.parts == 1) return e;
-  const int64_t quads = (int64_t)a.f.n_rows * a.f.G * a.f.hd / 4;
-  k_causal_join<T><<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(a);
+  const unsigned join = work_grid(a.f.blocks, a.f.G, kSlices);
+  if (a.f.groups == 4) k_causal_join<T, 4><<<join, 256, 0, st>>>(a);
+  else if (a.f.groups == 2) k_causal_join<T, 2><<<join, 256, 0, st>>>(a);
+  else k_causal_join<T, 1><<<join, 256, 0, st>>>(a);
   return hipGetLastError();
 }
 hipError_t launch_causal_grad(int dtype, const CausalGradArgs& a, hipStream_t st) {

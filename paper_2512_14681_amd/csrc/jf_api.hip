@@ -1192,7 +1192,7 @@ static jf_status check_causal(int n_seqs, int n_rows, const int32_t* d_row_start
   CausalArgs a{};
   a.n_seqs = n_seqs; a.n_rows = n_rows; a.H = n_heads; a.hd = head_dim; a.f32 = dtype == JF_F32;
   causal_plan(a);
-  if (((int64_t)a.blocks + 8) * n_heads > kMaxBlocks || (int64_t)n_rows * n_kv_heads * head_dim / 1024 > kMaxBlocks)
+  if (((int64_t)a.blocks + 8) * n_heads > kMaxBlocks)
     return fail(JF_E_CAPACITY, "%d rows of %d heads exceed one launch", n_rows, n_heads);
   return JF_OK;
 }

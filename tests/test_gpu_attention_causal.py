@@ -318,6 +318,19 @@ def test_thousands_of_short_sequences():
     assert int(call.flags) == 0
 
 
+@pytest.mark.parametrize("lens", [[0] * 90 + [1, 5], [1] * 60 + [0] * 60 + [70], [0, 3] * 50 + [0] * 100 + [2] * 3],
+                         ids=["front", "middle", "mixed"])
+def test_more_sequences_than_rows(lens):
+    """Empty sequences among more than 64: the last ones' blocks have numbers beyond the rows'."""
+    dims, name = "grp3", "bf16"
+    c = case(lens, dims, name, seed=36)
+    call = Call(c, np.cumsum([0] + lens).tolist(), dims, name)
+    call.forward()
+    call.backward()
+    close(call.results(), reference(c, lens, dims, name))
+    assert int(call.flags) == 0
+
+
 def test_bad_starts_among_many_sequences():
     """More than 64 sequences: flagged, and nothing outside the good ones is written."""
     from paper_2512_14681_amd import jf
@@ -332,7 +345,7 @@ def test_bad_starts_among_many_sequences():
     assert bool((got["out"][260:] == 7.0).all()) and bool((got["dk"][260:] == 7.0).all())
 
 
-@pytest.mark.parametrize("starts", [[0, 300, 410], [0, -5, 410], [-1, 200, 410], [0, 200, 411], [0, 250, 200]])
+@pytest.mark.parametrize("starts", [[0, 300, 410], [0, -5, 410], [-1, 200, 410], [0, 200, 411], [0, 250, 200], [50, 411, 60, 90]])
 def test_bad_starts_are_flagged_and_left_alone(starts):
     """Sequences inside the rows are computed; what does not fit raises JF_FLAG_CAPACITY, nothing outside is written."""
     from paper_2512_14681_amd import jf
@@ -351,7 +364,8 @@ def test_bad_starts_are_flagged_and_left_alone(starts):
             part = {n: t[a:b] for n, t in c.items()}
             want = reference(part, [b - a], dims, name)["out"]
             assert bool(((got["out"][a:b] - want[0]).abs() <= want[1]).all())
-    assert bool((got["out"][~covered] == 7.0).all())
+    for n in ("out", "dq", "dk", "dv"):
+        assert bool((got[n][~covered] == 7.0).all()), n
 
 
 def test_the_gradient_is_that_of_differences():
