@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal(CausalArgs a) {
       row_store4<T>(out + 32 * d + acc_row(i), a.vec_out, v[0], v[1], v[2], v[3]);
     }
   if (a.lse && h == 0)
-    a.lse[(size_t)head * a.n_rows + b.r0 + qi] = l == 0.f ? -INFINITY : (m + kDown + __builtin_amdgcn_logf(l)) * kLn2;
+    a.lse[(size_t)head * a.n_rows + b.r0 + qi] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l * 0x1p32f)) * kLn2;
 }
 
 // ---- gradient ------------------------------------------------------------------------

@@ -291,6 +291,20 @@ def test_scores_beyond_what_fp32_tells_apart(name, sign):
 
 
 @pytest.mark.parametrize("name", ["bf16", "f32"])
+def test_log_sums_of_equal_scores_have_their_digits(name):
+    """Scores of zero: row i's lse is ln(i + 1).  Its sum is exact; the logarithm to base 2 is off by 2 steps of 2^-24 at
+    most, ln 2 and the product by one each, all relative to the result; 6 cover terms of second order."""
+    torch = _torch()
+    dims, n = "grp3", 700
+    c = case([n], dims, name, seed=36)
+    c["q"].zero_()
+    call = Call(c, [0, n], dims, name)
+    call.forward()
+    want = torch.log(torch.arange(1, n + 1, dtype=torch.float64))
+    assert bool(((call.results()["lse"] - want).abs() <= 6 * 2.0 ** -24 * want).all())
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
 def test_values_next_to_the_largest(name):
     """Sums of many values of 2^127 have a mean that fits, whatever the order of the maxima."""
     torch = _torch()
