@@ -618,7 +618,8 @@ jf_status jf_attention_shared(const jf_batch *batch, const jf_prefix *prefix, in
  * with w = 1 / tokens (JF_MEAN_TOKENS), 1 / (sequences with tokens * tokens of
  * the row's) (JF_MEAN_SEQS) or 1 (JF_SUM).  Clipped rows (A > 0 and r > 1 +
  * clip_high, or A < 0 and r < 1 - clip_low) have no gradient of the policy
- * term.  Differences and exponentials are computed in 64 bits; the order of
+ * term; a weight of 0 leaves its term out of loss and gradient, whatever its
+ * value.  Differences and exponentials are computed in 64 bits; the order of
  * the sums is fixed.
  *   d_stats[JF_POLICY_STATS]: the loss, then sum w of policy, kl, entropy and
  *     clipped rows, then the number of tokens (no tokens: all 0);

@@ -76,7 +76,7 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& a, const PolicyRow&
     const double e = exp(k) - 1.0;
     const bool small = fabs(k) < 0.02;
     sum[1] += w * (small ? series : e - k);
-    g -= a.kl_weight * (small ? k + series : e);
+    if (a.kl_weight != 0.0) g -= a.kl_weight * (small ? k + series : e);  // an infinite e among others
   }
   if (a.entropy) sum[2] += w * (double)x.entropy;
   sum[3] += clipped ? w : 0.0;
@@ -85,7 +85,7 @@ __device__ __forceinline__ void policy_row(const PolicyArgs& a, const PolicyRow&
   g_entropy = (float)(-a.scale * a.entropy_weight * w);
 }
 __device__ __forceinline__ void policy_stats(const PolicyArgs& a, const double (&t)[kTerms]) {
-  const double loss = t[0] + (a.ref ? a.kl_weight * t[1] : 0.0) - (a.entropy ? a.entropy_weight * t[2] : 0.0);
+  const double loss = t[0] + (a.kl_weight != 0.0 ? a.kl_weight * t[1] : 0.0) - (a.entropy_weight != 0.0 ? a.entropy_weight * t[2] : 0.0);
   a.stats[0] = (float)(a.scale * loss);
 #pragma unroll
   for (int i = 0; i < kTerms; ++i) a.stats[1 + i] = (float)t[i];

@@ -299,3 +299,19 @@ def test_from_logits_to_their_gradient():
     assert abs(float(stats[0]) - loss.item()) < 1e-5 * (1 + abs(loss.item()))
     err = (grad.double().cpu() - y.grad).norm(dim=1)
     assert bool((err <= 1e-5 * y.grad.norm(dim=1) + 1e-9).all()), float(err.max())
+
+
+@pytest.mark.parametrize("size", [20, 6000])
+def test_weights_of_zero_leave_their_terms_out(size):
+    """The KL term and the entropy, infinite in places, are only reported."""
+    c = case([size], seed=9, beta=0.0, ent_w=0.0, none=0.0)
+    c["ref"][::3] = -np.inf
+    c["ref"][1] = 500.0  # e^k beyond fp32's largest
+    c["entropy"][2] = np.inf
+    call = Call(c).run()
+    got, g = call.stats.cpu().numpy(), call.g_lp.cpu().numpy()
+    assert np.isinf(got[2]) and np.isinf(got[3])
+    c["use_ref"] = c["use_entropy"] = False
+    alone = Call(c).run()
+    assert (g == alone.g_lp.cpu().numpy()).all()
+    assert got[0] == alone.stats.cpu().numpy()[0] and np.isfinite(got[0])
