@@ -587,13 +587,17 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dkv(CausalGradArgs
         const uint32_t g_tile = lds_address(s_qg[buf][1]) + skip * Tile::kRowBytes;
         const uint32_t qs = Tile::row_base(q_tile), gs = Tile::row_base(g_tile);
         const uint32_t q_columns = Tile::column_base(q_tile), g_columns = Tile::column_base(g_tile);
-        f32x16_t st, dp;
+        f32x16_t st, dp, off;
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
           const float4 x = *reinterpret_cast<const float4*>(&s_dots[buf][0][skip + acc_row(i) + 4 * h]);
           const float4 y = *reinterpret_cast<const float4*>(&s_dots[buf][1][skip + acc_row(i) + 4 * h]);
           st[i] = x.x; st[i + 1] = x.y; st[i + 2] = x.z; st[i + 3] = x.w;
           dp[i] = y.x; dp[i + 1] = y.y; dp[i + 2] = y.z; dp[i + 3] = y.w;
+        }
+        if constexpr (sizeof(T) == 4) {  // sums next to lse sqrt(hd) would lose last digits of fp32 scores
+          off = st;
+          st = zero16();
         }
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
@@ -605,7 +609,7 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dkv(CausalGradArgs
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const bool hidden = edge && acc_row(i) < lim;
-          st[i] = weight(st[i] * c);
+          st[i] = weight(sizeof(T) == 4 ? (st[i] + off[i]) * c : st[i] * c);
           dp[i] = hidden ? 0.f : st[i] * dp[i];
           st[i] = hidden ? 0.f : st[i];
         }
