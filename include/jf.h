@@ -526,8 +526,9 @@ jf_status jf_token_logprobs_grad(int32_t R, int32_t V, int32_t dtype, const void
  * read nor written.  A captured call takes new starts at every replay.  A
  * sequence whose start or end lies outside [0, n_rows], or whose end lies
  * before its start, is left as it was and JF_FLAG_CAPACITY is raised in
- * d_flags (optional, one int32, ORed; the caller clears it); among more than
- * 64 sequences others may then be left as they were too.
+ * d_flags (optional, one int32, ORed; the caller clears it); others may then
+ * be left as they were too (among more than 64 sequences, or where those
+ * that remain overlap).
  * d_q, d_out [n_rows][n_heads * head_dim], d_k, d_v [n_rows][n_kv_heads *
  * head_dim] are rows of dtype (JF_F32 or JF_BF16), ld_* elements apart (views
  * into one fused projection, for instance); query head j reads KV head j /

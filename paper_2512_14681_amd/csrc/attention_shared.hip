@@ -297,6 +297,14 @@ __device__ __forceinline__ void put_outputs(const SharedArgs& a, int row, int he
   }
 }
 
+// 64 samples of one row over 128 shared pages and 1 to 500 slots of their own
+// (28 query and 4 KV heads of 128 dims, bf16): 32 us.  The shared pages are a
+// product of 448 queries a KV head with two terms of each operand (16 GFLOP),
+// the rest reads 44 MB: neither fills the chip.  What bounds it is the length
+// of a wave's chain (table entry, page, scores, weights, outputs) over every
+// fourth page of a part, 8 of 32 here: shorter parts are more than run at once
+// or more than the merge can join as fast.  Three samples of two rows in fp32:
+// 11 us, one such chain.
 template <typename T, int HD>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_shared(SharedArgs a) {
   using Tile = SharedTile<T, HD>;
@@ -518,7 +526,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_share
 
 // Merges a row's parts, four dims of one row and head a thread.  SG threads
 // share an item, each taking every SG-th part, and join in LDS: the order does
-// not depend on timing.
+// not depend on timing.  Bound by two loads that depend on each other (the
+// batch's tables, then the parts) and its launch: 4 to 7 us.
 template <typename T, int SG>
 __global__ void __launch_bounds__(256) k_attention_shared_merge(SharedArgs a, int blocks) {
   __shared__ float s_part[SG > 1 ? 256 : 1][6];

