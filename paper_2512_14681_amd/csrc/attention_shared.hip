@@ -607,9 +607,14 @@ __global__ void __launch_bounds__(256) k_attention_shared_merge(SharedArgs a, in
 // which read a page once for all (7b heads, 128 shared pages: 64 sequences of
 // 2 rows, 28 tiles, 52 us and 57; of 4 rows, 56 tiles, 84 and 66).
 // Parts of kChunk pages or more, as many as give two workgroups a compute
-// unit (64 sequences of one row: 37 us, with twice as many parts 53); how many
+// unit (64 sequences of one row: 37 us, with twice as many parts 46); how many
 // pages there are to split is known on the device, and the host's bounds stand
-// for it here.
+// for it here.  Where the sequences' own pages alone take those places, shared
+// pages are split all the same, into as many as give one workgroup a compute
+// unit, or two by parts of 32 pages and more (16 with four tiles a workgroup):
+// the sequences' own parts, which come last, then start later, which costs
+// less than long parts do (128 shared pages: 64 sequences of 8 rows 275 us with
+// one part, 98; 8 of 64 rows 273 and 96).
 void shared_plan(SharedArgs& a) {
   const int grp = a.H / a.G;
   auto tiles = [&](int64_t rows) { return (int)((rows * grp + 31) / 32); };
@@ -623,12 +628,18 @@ void shared_plan(SharedArgs& a) {
   const int64_t base_s = prefix ? (int64_t)a.n_groups * a.G * a.shared_groups : 0;
   const int64_t base_o = (int64_t)a.b.n_seqs * a.G * a.own_groups;
   const int own = std::max(all - shared, 1);
-  int chunk = std::max(kChunk, (std::max(shared, all) + 63) / 64);
-  while (chunk < std::max(shared, own) &&
-         base_s * ((shared + chunk - 1) / chunk) + base_o * ((own + chunk - 1) / chunk) > kWorkgroups)
-    chunk += std::max(chunk / 8, 4) / 4 * 4;
-  a.shared_splits = prefix ? (shared + chunk - 1) / chunk : 0;
-  a.own_splits = (own + chunk - 1) / chunk;
+  auto parts = [](int pages, int chunk) { return (pages + chunk - 1) / chunk; };
+  auto longer = [](int chunk) { return chunk + std::max(chunk / 8, 4) / 4 * 4; };
+  const int least = std::max(kChunk, (std::max(shared, all) + 63) / 64);
+  int chunk = least;
+  while (chunk < std::max(shared, own) && base_s * parts(shared, chunk) + base_o * parts(own, chunk) > kWorkgroups)
+    chunk = longer(chunk);
+  int chunk_s = least;
+  const int enough = a.shared_few ? 32 : 16;
+  while (chunk_s < chunk && base_s * parts(shared, chunk_s) > (chunk_s < enough ? kWorkgroups / 2 : kWorkgroups))
+    chunk_s = longer(chunk_s);
+  a.shared_splits = prefix ? parts(shared, chunk_s) : 0;
+  a.own_splits = parts(own, chunk);
   a.parts = a.shared_splits + a.own_splits;
   a.shared_jobs64 = base_s * a.shared_splits;
   a.own_jobs64 = base_o * a.own_splits;
@@ -641,7 +652,7 @@ template <typename T> static hipError_t shared_type(const SharedArgs& a, hipStre
   else k_attention_shared<T, 128><<<jobs, 256, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.parts == 1) return e;
-  const bool many = a.parts > 8;
+  const bool many = a.parts > 16;
   const int per = 256 / (a.hd / 4 * (many ? 4 : 1)), blocks = (a.b.max_rows * a.H + per - 1) / per;
   if (many) k_attention_shared_merge<T, 4><<<(unsigned)(a.b.n_seqs * blocks), 256, 0, st>>>(a, blocks);
   else k_attention_shared_merge<T, 1><<<(unsigned)(a.b.n_seqs * blocks), 256, 0, st>>>(a, blocks);

@@ -194,6 +194,16 @@ def test_long_prefix_many_samples():
     Call([(40, [(900, 1)] * 3)], "grp8", "f32", seed=4).run().check()
 
 
+@pytest.mark.parametrize("dims,name", [("7b", "bf16"), ("tiny", "f32")])
+def test_few_rows_over_many_parts(dims, name):
+    Call([(80, [(300, 1)] * 2), (75, [(1, 3), (1200, 1)])], dims, name, seed=12).run().check()
+
+
+def test_shared_parts_beside_many_sequences():
+    """The sequences' own pages alone take all places of the chip; the shared ones come in parts all the same."""
+    Call([(36, [(40, 8)] * 64)], "7b", "bf16", seed=13).run().check()
+
+
 def test_sequences_of_no_group():
     Call([(3, [(10, 2), (100, 1)])], "grp3", "bf16", seed=5, loners=[(0, 1), (200, 7), (64, 1)]).run().check()
     Call([], "grp3", "bf16", seed=6, loners=[(33, 2), (200, 7)]).run().check()
