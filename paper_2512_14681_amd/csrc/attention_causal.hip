@@ -191,8 +191,8 @@ template <int ND> __device__ __forceinline__ void add_shared(const float* at, fl
 
 // Outputs, in one pass over the keys.  Bound by the matrix and vector
 // instructions, which two waves a SIMD overlap in part: 8192 rows of 7b heads
-// (481 GFLOP) take 465 us, 1035 TFLOP/s; the matrix cores are busy in 59% of
-// the cycles, at 1.8 GHz (the chip's power sets the clock), and no LDS access
+// (481 GFLOP) take 465 us, 1035 TFLOP/s; the matrix cores are busy in about 60%
+// of the cycles, at 1.8 GHz (the chip's power sets the clock), and no LDS access
 // waits for a bank.  2048 rows take 49 us: 448 workgroups on 512 places, of
 // which the longest has 32 steps.  A wave holds its 32 queries (32 registers),
 // 64 x 32 scores and weights (64) and 32 outputs of 128 dims (64); the keys'
