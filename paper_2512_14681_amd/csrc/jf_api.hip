@@ -1204,7 +1204,7 @@ static void causal_args(CausalArgs* a, int n_seqs, int n_rows, const int32_t* d_
   a->flags = d_flags;
   a->q = d_q; a->k = d_k; a->v = d_v;
   a->ld_q = (size_t)ld_q; a->ld_k = (size_t)ld_k; a->ld_v = (size_t)ld_v;
-  constexpr int64_t kMostStride = 1 << 22;  // 64 rows stay within 32-bit offsets
+  constexpr int64_t kMostStride = 1 << 22;  // 128 rows, as many as a step brings, stay within 32-bit offsets
   a->vec = rows16(d_q, ld_q, esz) && rows16(d_k, ld_k, esz) && rows16(d_v, ld_v, esz) && ld_q <= kMostStride &&
            ld_k <= kMostStride && ld_v <= kMostStride;
   a->out = d_out; a->ld_out = (size_t)ld_out;
