@@ -19,9 +19,9 @@
 // inputs there are (2^-8 at most of each of many terms of a sum; the result
 // is rounded to as much itself).  Sums, maxima and statistics are fp32.  Each
 // of these two roundings adds 0.0015 to 0.0017 to the gradients' relative
-// error, D from the rounded outputs 0.001, and the gradients' own rounding
-// 0.0017 (errors that add up as squares); two terms for each would double the
-// second products.
+// error, D from the rounded outputs 0.001 to that of dq, and the gradients' own
+// rounding 0.0017 (errors that add up as squares); two terms for each would
+// double the second products.
 //
 // Figures below are of traced launches, 7b heads being 28 query and 4 KV heads
 // of 128 dims in bf16; a matrix product of 8192^3 reaches 1236 TFLOP/s.
@@ -398,10 +398,13 @@ __device__ __forceinline__ float weight(float x) { return __builtin_amdgcn_fmed3
 
 // dq; and of each row and head, for dk and dv, what the accumulators of its
 // scores and of do v start from: -lse sqrt(hd) (-inf for a row without
-// weights, whose weights then are 0), and -D.
+// weights, whose weights then are 0), and -D.  sum_j ds_ij is 0 but for what the
+// rounded outputs lack in D, and is added to it for dk.
 // Three products a pair where the forward pass has two: 4096 rows of 7b heads
-// (180 GFLOP) take 184 us, 980 TFLOP/s, bound as the forward pass is (which
-// takes 136 us here).
+// (180 GFLOP) take 198 us, 910 TFLOP/s, bound as the forward pass is (which
+// takes 140 us there).  Of these the sum of ds takes 1% of a forward and
+// backward pass (in four sums; in one 1.5%, and 4% for heads of 64), and
+// the gradients' error falls from 0.0025 to 0.0024.
 template <typename T, int HD, int NQ, bool kVec>
 __global__ void __launch_bounds__(256, kResident<T>) k_causal_dq(CausalGradArgs a) {
   using Tile = RowTile<T, HD>;
@@ -439,7 +442,7 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dq(CausalGradArgs 
     settle(g);
   }
   const float c = kLog2e / sqrtf((float)HD);
-  float lse, dot = 0.f;
+  float lse, dot = 0.f, rest[4] = {0.f, 0.f, 0.f, 0.f};  // rest: sum of ds
   {
     const T* p = reinterpret_cast<const T*>(a.f.out) + (size_t)(b.r0 + qi) * a.f.ld_out + head * HD + 8 * h;
 #pragma unroll
@@ -452,10 +455,7 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dq(CausalGradArgs 
       for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(xs[e], gs[e], dot);
     }
     dot = pair_sum(dot);
-    const size_t at = (size_t)head * a.f.n_rows + b.r0 + qi;
-    lse = a.f.lse[at];
-    if (share == 0 && h == 0 && q0 + lane < b.n)
-      a.dots[at] = make_float2(lse == -INFINITY ? -INFINITY : -lse * sqrtf((float)HD), -dot);
+    lse = a.f.lse[(size_t)head * a.f.n_rows + b.r0 + qi];
     lse = lse == -INFINITY ? INFINITY : lse * kLog2e;
   }
   f32x16_t dq[ND];
@@ -485,6 +485,7 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dq(CausalGradArgs 
       for (int i = 0; i < 16; ++i) {
         const float ds = weight(__builtin_fmaf(st[i], c, -lse)) * (dp[i] - dot);
         st[i] = kEdge && 32 * kt + acc_row(i) > lim ? 0.f : ds;
+        rest[i % 4] += st[i];
       }
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -500,17 +501,28 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dq(CausalGradArgs 
   };
   all_steps<kRows>(b.t * S::kBlock, last, step);
 
+  float left = pair_sum((rest[0] + rest[1]) + (rest[2] + rest[3]));
   if constexpr (S::kShare > 1) {
+    __shared__ float s_rest[S::kShare - 1][NQ][32];
     float* s_o = reinterpret_cast<float*>(s_kv);
     static_assert((S::kShare - 1) * NQ * 32 * HD * 4 <= (int)sizeof(s_kv), "the parts fit");
     __syncthreads();
-    if (share > 0) put_shared<ND>(s_o + ((share - 1) * NQ + wave % NQ) * 32 * HD, dq);
+    if (share > 0) {
+      put_shared<ND>(s_o + ((share - 1) * NQ + wave % NQ) * 32 * HD, dq);
+      if (h == 0) s_rest[share - 1][wave % NQ][lane] = left;
+    }
     __syncthreads();
     if (share > 0) return;
 #pragma unroll
-    for (int i = 0; i < S::kShare - 1; ++i) add_shared<ND>(s_o + (i * NQ + wave) * 32 * HD, 1.f, dq);
+    for (int i = 0; i < S::kShare - 1; ++i) {
+      add_shared<ND>(s_o + (i * NQ + wave) * 32 * HD, 1.f, dq);
+      left += s_rest[i][wave][lane & 31];
+    }
   }
   if (q0 + (lane & 31) >= b.n) return;
+  if (h == 0)
+    a.dots[(size_t)head * a.f.n_rows + b.r0 + qi] =
+        make_float2(lse == INFINITY ? -INFINITY : lse * (kLn2 * -sqrtf((float)HD)), -(dot + left));
   const float f = 1.f / sqrtf((float)HD);
   T* out = reinterpret_cast<T*>(a.g_q) + (size_t)(b.r0 + qi) * a.ld_g_q + head * HD + 4 * h;
 #pragma unroll
@@ -522,8 +534,8 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dq(CausalGradArgs 
 
 // dk and dv of a block of keys of a KV head, over the queries of the heads of
 // `part` (part, part + parts, ... of the group's).
-// Four products a pair: 4096 rows of 7b heads (241 GFLOP) take 266 us, 905
-// TFLOP/s.  The 128 registers of dk and dv beside 64 of keys and values leave
+// Four products a pair: 4096 rows of 7b heads (241 GFLOP) take 266 to 287 us,
+// 840 to 905 TFLOP/s.  The 128 registers of dk and dv beside 64 of keys and values leave
 // room for one tile of scores at a time, so that the matrix cores wait for the
 // weights more often than in the forward pass.
 template <typename T, int HD, int NQ, bool kVec>
