@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+from operator import index
 
 import numpy as np
 
@@ -464,7 +465,8 @@ def kv_read(batch, n_kv_heads, head_dim, kv_dtype, d_kv, d_k, d_v, d_flags=None,
         check(status)
 
 
-def _kv8_ws_bytes(batch, shape):
+def _kv8_ws_bytes(batch, n_heads, n_kv_heads, head_dim):
+    shape = index(n_heads), index(n_kv_heads), index(head_dim)
     n = batch.ws.get(shape)
     if n is None:
         n = batch.ws[shape] = lib().jf_attention_kv8_ws_bytes(batch.ref, *shape)
@@ -472,7 +474,7 @@ def _kv8_ws_bytes(batch, shape):
 
 
 def attention_kv8_ws_bytes(batch, n_heads, n_kv_heads, head_dim):
-    n = _kv8_ws_bytes(batch, (n_heads, n_kv_heads, head_dim))
+    n = _kv8_ws_bytes(batch, n_heads, n_kv_heads, head_dim)
     if n == 0:
         raise JfError(JF_E_SHAPE, "no batch or heads that jf_attention_kv8 takes")
     return n
@@ -487,16 +489,21 @@ def attention_kv8(batch, n_heads, n_kv_heads, head_dim, act_dtype, d_q, d_kv, d_
                                     _buf(dev, d_kv, _pool_bytes(batch, n_kv_heads, head_dim, JF_E4M3)),
                                     _buf(dev, d_vis, n * 8 * JF_VIS_WORDS),
                                     _act(dev, d_out, act_dtype, (n + 15) // 16 * 16 * row),  # 16 rows a tile
-                                    _buf(dev, d_ws, _kv8_ws_bytes(batch, (n_heads, n_kv_heads, head_dim))),
+                                    _buf(dev, d_ws, _kv8_ws_bytes(batch, n_heads, n_kv_heads, head_dim)),
                                     _vec(dev, d_flags, _I32, 1), _on(dev, stream))
     if status:
         check(status)
 
 
+# Sizes and parameters are remembered by their numbers: a tensor that changes in place stays the same key.
 @functools.lru_cache(4096)
-def token_logprobs_ws_bytes(R, V, k=0):
+def _logprobs_ws(R, V, k):
     _count(R, V, k)
-    return lib().jf_token_logprobs_ws_bytes(int(R), int(V), int(k))
+    return lib().jf_token_logprobs_ws_bytes(R, V, k)
+
+
+def token_logprobs_ws_bytes(R, V, k=0):
+    return _logprobs_ws(int(R), int(V), int(k))
 
 
 def token_logprobs(d_logits, d_ws, d_tokens=None, k=0, d_logprob=None, d_entropy=None, d_norm=None, d_top_ids=None,
@@ -562,12 +569,16 @@ def attention_causal(d_row_start, n_heads, n_kv_heads, head_dim, d_q, d_k, d_v, 
 
 
 @functools.lru_cache(4096)
-def attention_causal_grad_ws_bytes(n_seqs, n_rows, n_heads, n_kv_heads, head_dim):
+def _causal_grad_ws(n_seqs, n_rows, n_heads, n_kv_heads, head_dim):
     _count(n_seqs, n_rows)
     n = lib().jf_attention_causal_grad_ws_bytes(n_seqs, n_rows, n_heads, n_kv_heads, head_dim)
     if n == 0:
         raise JfError(JF_E_SHAPE, "no rows or heads that jf_attention_causal_grad takes")
     return n
+
+
+def attention_causal_grad_ws_bytes(n_seqs, n_rows, n_heads, n_kv_heads, head_dim):
+    return _causal_grad_ws(index(n_seqs), index(n_rows), index(n_heads), index(n_kv_heads), index(head_dim))
 
 
 def attention_causal_grad(d_row_start, n_heads, n_kv_heads, head_dim, d_q, d_k, d_v, d_out, d_lse, d_g_out, d_g_q, d_g_k,
@@ -619,7 +630,8 @@ class Prefix:
         return self.ref
 
 
-def _shared_ws_bytes(batch, prefix, shape):
+def _shared_ws_bytes(batch, prefix, n_heads, n_kv_heads, head_dim):
+    shape = "shared", index(n_heads), index(n_kv_heads), index(head_dim)
     key = shape if prefix is None else shape + (prefix.c.n_groups, prefix.c.max_rows, prefix.c.max_pages)
     n = batch.ws.get(key)
     if n is None:
@@ -629,7 +641,7 @@ def _shared_ws_bytes(batch, prefix, shape):
 
 
 def attention_shared_ws_bytes(batch, prefix, n_heads, n_kv_heads, head_dim):
-    n = _shared_ws_bytes(batch, prefix, ("shared", n_heads, n_kv_heads, head_dim))
+    n = _shared_ws_bytes(batch, prefix, n_heads, n_kv_heads, head_dim)
     if n == 0:
         raise JfError(JF_E_SHAPE, "no batch, prefix or heads that jf_attention_shared takes")
     return n
@@ -646,20 +658,23 @@ def attention_shared(batch, prefix, n_heads, n_kv_heads, head_dim, dtype, d_q, d
                                        _buf(dev, d_kv, _pool_bytes(batch, n_kv_heads, head_dim, dtype)),
                                        _buf(dev, d_vis, n * 8 * JF_VIS_WORDS),
                                        _act(dev, d_out, dtype, (n + 15) // 16 * 16 * row),  # 16 rows a tile
-                                       _buf(dev, d_ws, _shared_ws_bytes(batch, prefix,
-                                                                        ("shared", n_heads, n_kv_heads, head_dim))),
+                                       _buf(dev, d_ws, _shared_ws_bytes(batch, prefix, n_heads, n_kv_heads, head_dim)),
                                        _vec(dev, d_flags, _I32, 1), _on(dev, stream))
     if status:
         check(status)
 
 
 @functools.lru_cache(4096)
-def policy_loss_ws_bytes(n_seqs, n_rows):
+def _policy_ws(n_seqs, n_rows):
     _count(n_seqs, n_rows)
     n = lib().jf_policy_loss_ws_bytes(n_seqs, n_rows)
     if n == 0:
         raise JfError(JF_E_CAPACITY, "more sequences or rows than jf_policy_loss takes")
     return n
+
+
+def policy_loss_ws_bytes(n_seqs, n_rows):
+    return _policy_ws(index(n_seqs), index(n_rows))
 
 
 @functools.lru_cache(256)
@@ -677,7 +692,8 @@ def policy_loss(d_row_start, d_tokens, d_logprob, d_old_logprob, d_advantage, d_
     n = d_logprob.numel()
     dev = _current_device()
     start, n_seqs = _starts(dev, d_row_start)
-    params = _policy(clip_low, clip_high, kl_weight, entropy_weight, scale, mean, 1 if adv_rows else 0)
+    params = _policy(float(clip_low), float(clip_high), float(kl_weight), float(entropy_weight), float(scale), index(mean),
+                     1 if adv_rows else 0)
     status = lib().jf_policy_loss(ctypes.byref(params), n_seqs, n, start, _vec(dev, d_tokens, _I32, n),
                                   _vec(dev, d_logprob, _F32, n), _vec(dev, d_old_logprob, _F32, n),
                                   _vec(dev, d_ref_logprob, _F32, n), _vec(dev, d_entropy, _F32, n),
