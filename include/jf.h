@@ -554,8 +554,9 @@ jf_status jf_attention_causal(int32_t n_seqs, int32_t n_rows, const int32_t *d_r
  * of that sequence, and none of another's.  Weights are computed anew from
  * d_lse, whose fp32 digits hold them for scores up to 2^20 or so (beyond,
  * they are still at most 1).  d_ws, on a 16-byte boundary, holds
- * jf_attention_causal_grad_ws_bytes(...) bytes, needs no clearing and
- * may be shared by calls that do not overlap. */
+ * jf_attention_causal_grad_ws_bytes(...) bytes, which are enough for fewer
+ * rows and sequences of these heads too, needs no clearing and may be shared
+ * by calls that do not overlap. */
 size_t jf_attention_causal_grad_ws_bytes(int32_t n_seqs, int32_t n_rows, int32_t n_heads, int32_t n_kv_heads,
                                          int32_t head_dim);
 jf_status jf_attention_causal_grad(int32_t n_seqs, int32_t n_rows, const int32_t *d_row_start, int32_t n_heads,
@@ -597,7 +598,9 @@ typedef struct {
  * JF_MAX_ROWS.  d_q, d_kv, d_out and d_ws must start on 16-byte boundaries;
  * d_ws holds jf_attention_shared_ws_bytes(...) bytes (0: the call would be
  * refused), needs no clearing and may be shared by calls that do not overlap.
- * prefix NULL: nothing is shared. */
+ * The size is that of this batch and prefix: one with fewer sequences, groups
+ * or rows is cut into more parts and can need more, so a workspace for several
+ * holds the largest of their sizes.  prefix NULL: nothing is shared. */
 size_t jf_attention_shared_ws_bytes(const jf_batch *batch, const jf_prefix *prefix, int32_t n_heads,
                                     int32_t n_kv_heads, int32_t head_dim);
 jf_status jf_attention_shared(const jf_batch *batch, const jf_prefix *prefix, int32_t n_heads, int32_t n_kv_heads,

@@ -773,11 +773,26 @@ void causal_plan(CausalArgs& a) { causal_shape(a, false); }
 // in parts of as many as leave enough of them, and a pass that adds the parts
 // (28 query and 4 KV heads, 4096 rows: one part 1500 us, a head a part 471; 32
 // sequences of 500 rows: 383 and 540).
+static int grad_parts(int64_t one, int64_t grp) {  // one: workgroups of one part; fewer parts the more there are
+  const int64_t heads = one >= 500 ? grp : std::max<int64_t>(grp * one / 1024, 1);
+  return (int)((grp + heads - 1) / heads);
+}
 void causal_grad_plan(CausalGradArgs& a) {
   causal_shape(a.f, true);
-  const int64_t one = (int64_t)a.f.blocks * a.f.G, grp = a.f.H / a.f.G;
-  const int64_t heads = one >= 500 ? grp : std::max<int64_t>(grp * one / 1024, 1);
-  a.parts = (int)((grp + heads - 1) / heads);
+  a.parts = grad_parts((int64_t)a.f.blocks * a.f.G, a.f.H / a.f.G);
+}
+// Bound on parts times rows of the calls with n_rows rows or fewer (those with
+// one part have no parts to hold).  Rows between 128 (b - 1) and 128 b - 1, of
+// however many sequences, make b blocks or more.
+size_t causal_most_part_rows(int n_rows, int H, int G) {
+  size_t most = 0;
+  for (int64_t b = 1;; ++b) {
+    const int64_t rows = std::min<int64_t>(128 * b - 1, n_rows);
+    const int parts = grad_parts(b * G, H / G);
+    if (parts == 1) return most;
+    most = std::max(most, (size_t)(parts * rows));
+    if (rows == n_rows) return most;
+  }
 }
 
 template <typename F> static hipError_t with_shape(int hd, int groups, bool vec, F f) {

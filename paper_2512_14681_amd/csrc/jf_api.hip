@@ -1241,14 +1241,8 @@ extern "C" size_t jf_attention_causal_grad_ws_bytes(int32_t n_seqs, int32_t n_ro
   static const int32_t some = 0;
   if (check_causal(n_seqs, n_rows, &some, n_heads, n_kv_heads, head_dim, JF_F32, &none) != JF_OK) return 0;
   if (none) return 256;
-  size_t part = 0;  // the larger of what both types need
-  for (int f32 = 0; f32 < 2; ++f32) {
-    CausalGradArgs a{};
-    a.f.n_seqs = n_seqs; a.f.n_rows = n_rows; a.f.H = n_heads; a.f.G = n_kv_heads; a.f.hd = head_dim; a.f.f32 = f32;
-    causal_grad_plan(a);
-    if (a.parts > 1) part = std::max(part, (size_t)2 * a.parts * n_rows * n_kv_heads * head_dim * 4);
-  }
-  return causal_dots_bytes(n_rows, n_heads) + part + 256;
+  // the keys' and the values' parts, of calls with fewer rows or sequences too: these may be cut into more
+  return causal_dots_bytes(n_rows, n_heads) + causal_most_part_rows(n_rows, n_heads, n_kv_heads) * 2 * n_kv_heads * head_dim * 4 + 256;
 }
 
 extern "C" jf_status jf_attention_causal_grad(int32_t n_seqs, int32_t n_rows, const int32_t* d_row_start,

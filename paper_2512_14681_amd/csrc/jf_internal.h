@@ -391,6 +391,7 @@ struct CausalGradArgs {
   int parts;                 // shares of a group's heads
 };
 void causal_grad_plan(CausalGradArgs& a);  // also parts
+size_t causal_most_part_rows(int n_rows, int H, int G);  // parts times rows, of calls with n_rows rows or fewer
 hipError_t launch_causal_grad(int dtype, const CausalGradArgs& a, hipStream_t stream);
 
 // attention_shared.hip

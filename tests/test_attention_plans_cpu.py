@@ -1,0 +1,63 @@
+"""How the causal and the shared-prefix attention cut their launches: the planners are host functions of libjf
+(paper_2512_14681_amd/csrc/jf_internal.h), called here by their C++ names, without a GPU."""
+import ctypes
+import os
+
+import pytest
+
+from paper_2512_14681_amd import jf
+
+I, P, SZ = ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
+
+
+def _fields(text):
+    kinds = {"i": I, "p": P, "z": SZ, "l": ctypes.c_int64}
+    return [(n, kinds[k]) for k, names in (part.split(":") for part in text.split()) for n in names.split(",")]
+
+
+class CausalArgs(ctypes.Structure):
+    _fields_ = _fields("i:n_seqs,n_rows,H,G,hd p:row_start,flags,q,k,v z:ld_q,ld_k,ld_v i:vec p:out z:ld_out i:vec_out "
+                       "p:lse i:f32,groups,blocks")
+
+
+class CausalGradArgs(ctypes.Structure):
+    _fields_ = [("f", CausalArgs)] + _fields("p:g_out z:ld_g_out i:vec_dot p:g_q,g_k,g_v z:ld_g_q,ld_g_k,ld_g_v i:vec_q,vec_kv "
+                                             "p:dots,kv_part i:parts")
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(jf.LIB_PATH):
+        pytest.skip("libjf.so not built (python -m paper_2512_14681_amd.build)")
+    return ctypes.CDLL(jf.LIB_PATH)
+
+
+def grad_plan(L, n_seqs, n_rows, H, G, hd, f32):
+    a = CausalGradArgs()
+    a.f.n_seqs, a.f.n_rows, a.f.H, a.f.G, a.f.hd, a.f.f32 = n_seqs, n_rows, H, G, hd, f32
+    f = L._ZN2jf16causal_grad_planERNS_14CausalGradArgsE
+    f.restype, f.argtypes = None, [ctypes.POINTER(CausalGradArgs)]
+    f(ctypes.byref(a))
+    return a
+
+
+ROWS = [*range(1, 40), *range(40, 2000, 61), *range(2000, 20000, 509), 40000, 100000]
+SEQS = [1, 2, 3, 9, 33, 64, 65, 100, 1000]
+
+
+@pytest.mark.parametrize("H,G,hd", [(28, 4, 128), (16, 2, 64), (4, 4, 32), (8, 1, 128), (64, 1, 64), (6, 2, 64)])
+def test_a_larger_calls_gradient_workspace_holds_smaller_calls(L, H, G, hd):
+    """Every call's need (two floats a row and head; the shares' gradients) is within what the size query gives for that
+    call, and for any with more rows or sequences."""
+    size = jf.lib().jf_attention_causal_grad_ws_bytes
+    most = [0] * len(SEQS)
+    for n in ROWS:
+        for i, s in enumerate(SEQS):
+            got = size(s, n, H, G, hd)
+            for f32 in (0, 1):
+                parts = grad_plan(L, s, n, H, G, hd, f32).parts
+                assert 1 <= parts <= H // G
+                assert got >= n * H * 8 + (2 * parts * n * G * hd * 4 if parts > 1 else 0)
+            # all smaller counts are at or before this place of the lists
+            assert got >= max(most[:i + 1]), (s, n)
+            most[i] = max(most[:i + 1] + [got])
