@@ -576,8 +576,9 @@ jf_status jf_attention_causal_grad(int32_t n_seqs, int32_t n_rows, const int32_t
  * Sequences of no group share nothing.  The host gives bounds: at most
  * max_rows rows of one group and max_pages (<= table_stride) shared pages.
  * What the device holds beyond these, or a sequence with fewer committed
- * tokens than it is said to share, raises JF_FLAG_CAPACITY, and the rows of
- * such a group or sequence are left as they were. */
+ * tokens than it is said to share or with rows outside its group's, raises
+ * JF_FLAG_CAPACITY, and the rows of such a group or sequence are left as they
+ * were. */
 typedef struct {
   int32_t n_groups, max_rows, max_pages;
   const int32_t *d_seq_start; /* [n_groups + 1] */

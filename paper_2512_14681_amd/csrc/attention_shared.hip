@@ -64,10 +64,12 @@ __device__ __forceinline__ void mul(f32x16_t& acc, const Frag<bf16_t>& a, const 
 __device__ __forceinline__ void mul(f32x16_t& acc, const Frag<float>& a, const Query<float>& b) { mfma32(acc, a, b.v); }
 
 // What a sequence shares: the first `pages` pages, if its group is what the
-// host announced (else false, with JF_FLAG_CAPACITY raised).
-__device__ __forceinline__ bool group_ok(const SharedArgs& a, int s0, int s1, int pages) {
+// host announced and its rows are among the group's, which r0 and r1 get (else
+// false, with JF_FLAG_CAPACITY raised).
+__device__ __forceinline__ bool group_ok(const SharedArgs& a, int s0, int s1, int pages, int& r0, int& r1) {
   if (s0 < 0 || s1 < s0 || s1 > a.b.n_seqs || pages < 0 || pages > a.max_pages) return false;
-  const int r0 = a.b.row_start[s0], r1 = a.b.row_start[s1];
+  r0 = a.b.row_start[s0];
+  r1 = a.b.row_start[s1];
   return r0 >= 0 && r1 >= r0 && r1 <= a.b.n_rows && r1 - r0 <= a.max_group_rows;
 }
 __device__ __forceinline__ bool shared_pages(const SharedArgs& a, int s, const Seq& q, int& pages) {
@@ -80,8 +82,10 @@ __device__ __forceinline__ bool shared_pages(const SharedArgs& a, int s, const S
     const uint64_t hit = __ballot(s0 <= s && s < s1);
     if (hit) {
       const int l = __builtin_ctzll(hit);
+      int r0, r1;
       pages = a.pages[g0 + l];
-      ok = group_ok(a, __builtin_amdgcn_readlane(s0, l), __builtin_amdgcn_readlane(s1, l), pages) && pages <= q.C / kPage;
+      ok = group_ok(a, __builtin_amdgcn_readlane(s0, l), __builtin_amdgcn_readlane(s1, l), pages, r0, r1) &&
+           pages <= q.C / kPage && q.r0 >= r0 && q.r0 + q.n <= r1;  // row starts within a group may go beyond its ends
       break;
     }
   }
@@ -325,13 +329,13 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_share
   Seq q{};
   if (shared) {
     const int s0 = a.seq_start[unit], s1 = a.seq_start[unit + 1], pages = a.pages[unit];
-    if (!group_ok(a, s0, s1, pages)) {
+    int r1;
+    if (!group_ok(a, s0, s1, pages, r0, r1)) {
       if (a.b.flags && threadIdx.x == 0) atomicOr(a.b.flags, kFlagCapacity);
       return;
     }
     if (s0 == s1) return;
-    r0 = a.b.row_start[s0];
-    n = a.b.row_start[s1] - r0;
+    n = r1 - r0;
     table = a.b.table + (size_t)s0 * a.b.stride;
     const int chunk = part_pages(pages, splits);
     p0 = split * chunk;
