@@ -575,10 +575,10 @@ jf_status jf_attention_causal_grad(int32_t n_seqs, int32_t n_rows, const int32_t
  * whole pages of committed tokens are shared: 64 d_pages[g] <= d_ctx of each.
  * Sequences of no group share nothing.  The host gives bounds: at most
  * max_rows rows of one group and max_pages (<= table_stride) shared pages.
- * What the device holds beyond these, or a sequence with fewer committed
- * tokens than it is said to share or with rows outside its group's, raises
- * JF_FLAG_CAPACITY, and the rows of such a group or sequence are left as they
- * were. */
+ * What the device holds beyond these, a group that starts before an earlier
+ * one's start, or a sequence with fewer committed tokens than it is said to
+ * share or with rows outside its group's, raises JF_FLAG_CAPACITY, and the rows
+ * of such a group or sequence are left as they were. */
 typedef struct {
   int32_t n_groups, max_rows, max_pages;
   const int32_t *d_seq_start; /* [n_groups + 1] */

@@ -72,8 +72,16 @@ __device__ __forceinline__ bool group_ok(const SharedArgs& a, int s0, int s1, in
   r1 = a.b.row_start[s1];
   return r0 >= 0 && r1 >= r0 && r1 <= a.b.n_rows && r1 - r0 <= a.max_group_rows;
 }
+// Whether no start among the first n is beyond s0, where group n starts: the
+// group then overlaps none before it, whose work it would do once more.
+__device__ __forceinline__ bool group_in_order(const SharedArgs& a, int n, int s0) {
+  bool beyond = false;
+  for (int g = threadIdx.x & 63; g < n; g += 64) beyond |= a.seq_start[g] > s0;
+  return !__any(beyond);
+}
 __device__ __forceinline__ bool shared_pages(const SharedArgs& a, int s, const Seq& q, int& pages) {
   const int lane = threadIdx.x & 63;
+  int top = 0;  // of the starts before
   pages = 0;
   bool ok = true;
   for (int g0 = 0; g0 < a.n_groups; g0 += 64) {
@@ -82,12 +90,15 @@ __device__ __forceinline__ bool shared_pages(const SharedArgs& a, int s, const S
     const uint64_t hit = __ballot(s0 <= s && s < s1);
     if (hit) {
       const int l = __builtin_ctzll(hit);
+      const int at = __builtin_amdgcn_readlane(s0, l);
       int r0, r1;
       pages = a.pages[g0 + l];
-      ok = group_ok(a, __builtin_amdgcn_readlane(s0, l), __builtin_amdgcn_readlane(s1, l), pages, r0, r1) &&
-           pages <= q.C / kPage && q.r0 >= r0 && q.r0 + q.n <= r1;  // row starts within a group may go beyond its ends
+      ok = group_ok(a, at, __builtin_amdgcn_readlane(s1, l), pages, r0, r1) && pages <= q.C / kPage && q.r0 >= r0 &&
+           q.r0 + q.n <= r1 &&  // row starts within a group may go beyond its ends
+           !(__ballot(s0 > at) & ((1ull << l) - 1)) && !__any(top > at);  // as group_in_order
       break;
     }
+    top = max(top, s0);
   }
   if (!ok && a.b.flags && threadIdx.x == 0) atomicOr(a.b.flags, kFlagCapacity);
   return ok;
@@ -330,7 +341,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_share
   if (shared) {
     const int s0 = a.seq_start[unit], s1 = a.seq_start[unit + 1], pages = a.pages[unit];
     int r1;
-    if (!group_ok(a, s0, s1, pages, r0, r1)) {
+    if (!group_ok(a, s0, s1, pages, r0, r1) || !group_in_order(a, unit, s0)) {
       if (a.b.flags && threadIdx.x == 0) atomicOr(a.b.flags, kFlagCapacity);
       return;
     }
