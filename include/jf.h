@@ -526,9 +526,10 @@ jf_status jf_token_logprobs_grad(int32_t R, int32_t V, int32_t dtype, const void
  * read nor written.  A captured call takes new starts at every replay.  A
  * sequence whose start or end lies outside [0, n_rows], or whose end lies
  * before its start, is left as it was and JF_FLAG_CAPACITY is raised in
- * d_flags (optional, one int32, ORed; the caller clears it); others may then
- * be left as they were too (among more than 64 sequences, or where those
- * that remain overlap).
+ * d_flags (optional, one int32, ORed; the caller clears it).  Of those that
+ * remain, one that starts before an earlier one's end is left as it was too,
+ * among up to 64 sequences; among more, others may be left as they were, and
+ * rows that several hold get the results of any of them.
  * d_q, d_out [n_rows][n_heads * head_dim], d_k, d_v [n_rows][n_kv_heads *
  * head_dim] are rows of dtype (JF_F32 or JF_BF16), ld_* elements apart (views
  * into one fused projection, for instance); query head j reads KV head j /

@@ -45,7 +45,9 @@ struct RowBlock {
 // more, sequence s's blocks have the numbers from (its start) / kBlock + s on,
 // which no two sequences share, and s is searched for, 64 places at a time.
 // The first workgroup raises JF_FLAG_CAPACITY for row starts beyond the rows
-// or decreasing ones; no address is formed from those.
+// or decreasing ones; no address is formed from those.  Only where there are
+// such can sequences overlap: among up to 64, one that starts before an
+// earlier one's end has no blocks then.
 template <int kBlock, bool kFirst> __device__ __forceinline__ RowBlock search_block(const CausalArgs& a, int rank) {
   constexpr int kMostSearched = 256;  // blocks of a sequence, for which the order is looked for
   const int lane = threadIdx.x & 63;
@@ -62,7 +64,18 @@ template <int kBlock, bool kFirst> __device__ __forceinline__ RowBlock search_bl
       r0 = a.row_start[lane];
       r1 = a.row_start[lane + 1];
     }
-    const int blocks = valid(r0, r1) ? (r1 - r0 + kBlock - 1) / kBlock : 0;
+    bool good = valid(r0, r1);
+    if (__any(!good)) {
+      int end = good ? r1 : 0;  // the latest one up to here
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const int before = __shfl_up(end, d);
+        if (lane >= d) end = max(end, before);
+      }
+      end = __shfl_up(end, 1);
+      good = good && (lane == 0 || r0 >= end);
+    }
+    const int blocks = good ? (r1 - r0 + kBlock - 1) / kBlock : 0;
     int total = blocks, most = blocks;
     if (a.n_seqs > 1) {
 #pragma unroll
