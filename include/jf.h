@@ -552,7 +552,9 @@ jf_status jf_attention_causal(int32_t n_seqs, int32_t n_rows, const int32_t *d_r
  * tensors are of dtype; the gradients must overlap no input (but may be
  * columns of one tensor).  Nothing depends on the order in which workgroups
  * run.  An infinity or NaN among a sequence's inputs may reach every gradient
- * of that sequence, and none of another's.  Weights are computed anew from
+ * of that sequence, and none of another's; a NaN score makes the gradients of
+ * its row's query and of the keys and values that the row sees NaN.  Weights
+ * are computed anew from
  * d_lse, whose fp32 digits hold them for scores up to 2^20 or so (beyond,
  * they are still at most 1).  d_ws, on a 16-byte boundary, holds
  * jf_attention_causal_grad_ws_bytes(...) bytes, which are enough for fewer

@@ -407,7 +407,8 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal(CausalArgs a) {
 // ---- gradient ------------------------------------------------------------------------
 
 // 2^x, at most 1: scores beyond 2^20 are too coarse beside the rounded lse.
-__device__ __forceinline__ float weight(float x) { return __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(x), 0.f, 1.f); }
+// NaN stays, so that no gradient looks finite that is not.
+__device__ __forceinline__ float weight(float x) { return __builtin_elementwise_minimum(__builtin_amdgcn_exp2f(x), 1.f); }
 
 // dq; and of each row and head, for dk and dv, what the accumulators of its
 // scores and of do v start from: -lse sqrt(hd) (-inf for a row without

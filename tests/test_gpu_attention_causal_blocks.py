@@ -1,8 +1,10 @@
 """jf_attention_causal and its gradient where test_gpu_attention_causal.py, whose oracle and tolerances these are, does not
-go: row starts that leave sequences over each other."""
+go: row starts that leave sequences over each other, gradients of scores that are no numbers."""
+import math
+
 import pytest
 
-from test_gpu_attention_causal import Call, case, close, reference
+from test_gpu_attention_causal import DIMS, Call, case, close, reference
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +35,29 @@ def test_sequences_that_overlap(dims, name, starts, used):
     for n in ("out", "dq", "dk", "dv"):
         assert bool((got[n][free] == 7.0).all()), n
     assert bool((got["lse"][:, free] == 7.0).all())
+
+
+@pytest.mark.parametrize("dims,name", [("grp3", "bf16"), ("grp3", "f32"), ("tiny", "f32"), ("tiny", "bf16"), ("wide", "bf16")])
+def test_a_nan_score_makes_gradients_nan(dims, name):
+    """A NaN in row 70's query of one head: by the formulas the gradients of that query, and of the keys and values up to
+    row 70 of the KV head that it reads, are NaN.  Values behind it, other KV heads, other rows' queries and the other
+    sequence have what they have without it."""
+    lens, at = [100, 141], 170   # row 70 of the second sequence
+    c = case(lens, dims, name, seed=42)
+    want = reference(c, lens, dims, name)
+    H, G, hd = DIMS[dims]
+    c["q"][at, 5] = math.nan
+    call = Call(c, [0, 100, 241], dims, name)
+    call.forward()
+    call.backward()
+    got = call.results()
+    assert bool(got["dq"][at, :hd].isnan().all())
+    for n in ("dk", "dv"):
+        assert bool(got[n][100:at + 1, :hd].isnan().all()), n
+    for n in ("dq", "dk", "dv"):
+        ok = (got[n] - want[n][0]).abs() <= want[n][1]
+        if n == "dq":
+            ok[at, :hd] = True
+        else:       # dk: 0 times the query, where a key is behind the row
+            ok[100:241 if n == "dk" else at + 1, :hd] = True
+        assert bool(ok.all()), n
