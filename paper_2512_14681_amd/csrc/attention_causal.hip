@@ -407,8 +407,10 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal(CausalArgs a) {
 // ---- gradient ------------------------------------------------------------------------
 
 // 2^x, at most 1: scores beyond 2^20 are too coarse beside the rounded lse.
-// NaN stays, so that no gradient looks finite that is not.
-__device__ __forceinline__ float weight(float x) { return __builtin_elementwise_minimum(__builtin_amdgcn_exp2f(x), 1.f); }
+// The bound is part of the instruction, and gives 0 for NaN: a row with a NaN
+// score has NaN for its lse and D, which bring it to dq and dk; dv looks for it.
+// (A minimum that keeps NaN costs 1.4% of 4096 rows' forward and gradient, that look 0.3%.)
+__device__ __forceinline__ float weight(float x) { return __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(x), 0.f, 1.f); }
 
 // dq; and of each row and head, for dk and dv, what the accumulators of its
 // scores and of do v start from: -lse sqrt(hd) (-inf for a row without
@@ -635,6 +637,15 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dkv(CausalGradArgs
         const int skip = from + 32 * kt;
         const uint32_t q_tile = lds_address(s_qg[buf][0]) + skip * Tile::kRowBytes;
         const uint32_t g_tile = lds_address(s_qg[buf][1]) + skip * Tile::kRowBytes;
+        const float start = s_dots[buf][0][skip + (lane & 31)];
+        if (const uint32_t nans = (uint32_t)__ballot(start != start); __builtin_expect(nans != 0, 0)) {
+          // rows without numbers: the gradients of the values that they see have none
+          const float f = 31 - __builtin_clz(nans) >= ki - at - skip ? NAN : 0.f;
+#pragma unroll
+          for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) dv[d][i] += f;
+        }
         const uint32_t qs = Tile::row_base(q_tile), gs = Tile::row_base(g_tile);
         const uint32_t q_columns = Tile::column_base(q_tile), g_columns = Tile::column_base(g_tile);
         f32x16_t st, dp, off;
