@@ -25,11 +25,34 @@ class CausalGradArgs(ctypes.Structure):
                                              "p:dots,kv_part i:parts")
 
 
+# Calls for every kernel of the causal attention and its gradient, {(type, head_dim, rows of a block / 32): (rows of the
+# sequences, query heads, KV heads)}: sequences of several blocks, with steps before the masked ones, and of a few rows.
+NARROW, MIDDLE, WIDE = [400, 1, 130, 70], [400, 1, 130, 70], [400, 1, 130, 0] + [5] * 30
+CAUSAL_BLOCKS = {(name, hd, n): call
+                 for name in ("f32", "bf16") for hd in (32, 64, 128)
+                 for n, call in ((1, (NARROW, 6, 2)), (2, (MIDDLE, 28, 4)), (4, (WIDE, 28, 4))) if n > 1 or hd < 128}
+
+
+# Calls whose gradient sums a group's heads in so many shares: (type, rows of the sequences, query heads, KV heads, head_dim).
+CAUSAL_SHARES = {1: ("bf16", [5] * 150 + [300], 28, 4, 64),     # one workgroup goes over all heads
+                 4: ("bf16", [5] * 75 + [300], 28, 4, 128),     # 7 heads: shares of 2, 2, 2 and 1
+                 8: ("f32", [5] * 35 + [300], 64, 4, 32)}       # 16 heads in pairs
+
+
 @pytest.fixture(scope="module")
 def L():
     if not os.path.exists(jf.LIB_PATH):
         pytest.skip("libjf.so not built (python -m paper_2512_14681_amd.build)")
     return ctypes.CDLL(jf.LIB_PATH)
+
+
+def causal_plan(L, n_seqs, n_rows, H, G, hd, f32):
+    a = CausalArgs()
+    a.n_seqs, a.n_rows, a.H, a.G, a.hd, a.f32 = n_seqs, n_rows, H, G, hd, f32
+    f = L._ZN2jf11causal_planERNS_10CausalArgsE
+    f.restype, f.argtypes = None, [ctypes.POINTER(CausalArgs)]
+    f(ctypes.byref(a))
+    return a
 
 
 def grad_plan(L, n_seqs, n_rows, H, G, hd, f32):
@@ -61,3 +84,31 @@ def test_a_larger_calls_gradient_workspace_holds_smaller_calls(L, H, G, hd):
             # all smaller counts are at or before this place of the lists
             assert got >= max(most[:i + 1]), (s, n)
             most[i] = max(most[:i + 1] + [got])
+
+
+@pytest.mark.parametrize("name,hd,n", CAUSAL_BLOCKS, ids=lambda x: str(x))
+def test_every_block_height_has_a_case(L, name, hd, n):
+    """Which calls of CAUSAL_BLOCKS run on blocks of which height, forward and gradient; there are no others."""
+    lens, H, G = CAUSAL_BLOCKS[name, hd, n]
+    f32 = int(name == "f32")
+    fwd, grad = causal_plan(L, len(lens), sum(lens), H, G, hd, f32), grad_plan(L, len(lens), sum(lens), H, G, hd, f32)
+    assert (fwd.groups, grad.f.groups) == (n, n)
+    assert grad.parts == H // G     # a join of several shares as well
+
+
+def test_no_other_block_heights(L):
+    for f32 in (0, 1):
+        for hd in (32, 64, 128):
+            seen = set()
+            for H in (1, 4, 28, 64):
+                for rows in (1, 60, 500, 3000, 20000):
+                    for seqs in (1, 4, 80):
+                        seen.add(causal_plan(L, seqs, rows, H, 1, hd, f32).groups)
+                        seen.add(grad_plan(L, seqs, rows, H, 1, hd, f32).f.groups)
+            assert seen == {n for t, d, n in CAUSAL_BLOCKS if (t, d) == (("bf16", "f32")[f32], hd)}
+
+
+@pytest.mark.parametrize("parts", CAUSAL_SHARES)
+def test_every_kind_of_share_has_a_case(L, parts):
+    name, lens, H, G, hd = CAUSAL_SHARES[parts]
+    assert grad_plan(L, len(lens), sum(lens), H, G, hd, int(name == "f32")).parts == parts
