@@ -25,6 +25,25 @@ class CausalGradArgs(ctypes.Structure):
                                              "p:dots,kv_part i:parts")
 
 
+class BatchArgs(ctypes.Structure):
+    _fields_ = _fields("i:n_seqs,n_rows,max_rows,max_ctx,n_pages,stride p:row_start,ctx,table,flags")
+
+
+class SharedArgs(ctypes.Structure):
+    _fields_ = [("b", BatchArgs)] + _fields(
+        "i:n_groups,max_group_rows,max_pages p:seq_start,pages i:H,G,hd p:q z:q_plane p:kv,vis,out z:out_plane p:o_part,ml_part "
+        "i:shared_few,own_few,shared_groups,own_groups,shared_splits,own_splits,parts l:shared_jobs64,own_jobs64 i:shared_jobs")
+
+
+# Calls for both forms of the shared-prefix attention on either side, {(shared pages: four tiles of 32 queries a workgroup,
+# the sequences' own: the same): (groups of (shared pages, [(own tokens, rows)]), (own tokens, rows) of sequences of no
+# group, query heads, KV heads)}.
+SHARED_TILES = {(True, True): ([(5, [(30, 140), (5, 2)]), (2, [(100, 7)])], [(64, 3)], 16, 2),
+                (True, False): ([(4, [(70, 12)] * 7 + [(3, 60)]), (1, [(0, 1)])], [(200, 2)], 16, 2),
+                (False, True): ([(3, [(9, 3)] * 4)], [(130, 150)], 16, 2),
+                (False, False): ([(5, [(30, 40), (5, 2)]), (2, [(100, 7)])], [(64, 3)], 16, 2)}
+
+
 # Calls for every kernel of the causal attention and its gradient, {(type, head_dim, rows of a block / 32): (rows of the
 # sequences, query heads, KV heads)}: sequences of several blocks, with steps before the masked ones, and of a few rows.
 NARROW, MIDDLE, WIDE = [400, 1, 130, 70], [400, 1, 130, 70], [400, 1, 130, 0] + [5] * 30
@@ -112,3 +131,21 @@ def test_no_other_block_heights(L):
 def test_every_kind_of_share_has_a_case(L, parts):
     name, lens, H, G, hd = CAUSAL_SHARES[parts]
     assert grad_plan(L, len(lens), sum(lens), H, G, hd, int(name == "f32")).parts == parts
+
+
+@pytest.mark.parametrize("wide", SHARED_TILES, ids=str)
+def test_every_form_of_shared_prefixes_has_a_case(L, wide):
+    """Which form the calls of SHARED_TILES take on either side."""
+    groups, loners, H, G = SHARED_TILES[wide]
+    members = [(p, c, r) for p, seqs in groups for c, r in seqs] + [(0, c, r) for c, r in loners]
+    a = SharedArgs()
+    a.b.n_seqs, a.b.n_rows = len(members), sum(r for _, _, r in members)
+    a.b.max_rows, a.b.max_ctx = max(r for _, _, r in members), max(64 * p + c + r for p, c, r in members)
+    a.n_groups, a.H, a.G, a.hd = len(groups), H, G, 64
+    a.max_group_rows = max(sum(r for _, r in seqs) for p, seqs in groups)
+    a.max_pages = max(p for p, _ in groups)
+    f = L._ZN2jf11shared_planERNS_10SharedArgsE
+    f.restype, f.argtypes = None, [ctypes.POINTER(SharedArgs)]
+    f(ctypes.byref(a))
+    assert (not a.shared_few, not a.own_few) == wide
+    assert a.parts == a.shared_splits + a.own_splits > 1
