@@ -398,12 +398,13 @@ jf_status jf_trajectory_select(const int32_t *d_traj, const int32_t *d_len,
  * max_rows rows a sequence, at most max_ctx slots a sequence (committed and
  * rows; at most 64 table_stride).  What the device holds beyond these bounds
  * is not followed: such a sequence's rows are left as they were and
- * JF_FLAG_CAPACITY is raised; a page table entry outside [0, n_pages) raises
- * JF_FLAG_BAD_PAGE and its tokens are skipped.  d_flags (optional, one int32)
- * gets these bits ORed in; the caller clears it.  n_seqs, n_rows or max_rows
- * = 0 does nothing; n_pages = 0 otherwise is JF_E_CAPACITY.  n_seqs times the
- * workgroups that max_rows and max_ctx call for must stay within 2^22
- * (JF_E_CAPACITY). */
+ * JF_FLAG_CAPACITY is raised (starts that decrease can leave sequences that fit
+ * over each other: rows that two of them hold get the results of either); a
+ * page table entry outside [0, n_pages) raises JF_FLAG_BAD_PAGE and its tokens
+ * are skipped.  d_flags (optional, one int32) gets these bits ORed in; the
+ * caller clears it.  n_seqs, n_rows or max_rows = 0 does nothing; n_pages = 0
+ * otherwise is JF_E_CAPACITY.  n_seqs times the workgroups that max_rows and
+ * max_ctx call for must stay within 2^22 (JF_E_CAPACITY). */
 typedef struct {
   int32_t n_seqs, n_rows, max_rows, max_ctx, n_pages, table_stride;
   const int32_t *d_row_start;  /* [n_seqs + 1] */
@@ -474,7 +475,8 @@ jf_status jf_kv_read(const jf_batch *batch, int32_t n_kv_heads, int32_t head_dim
  * head_dim elements per plane with Rp = n_rows rounded up to 16; max_rows <=
  * JF_MAX_ROWS.  d_q, d_kv, d_out and d_ws must start on 16-byte boundaries;
  * d_ws holds jf_attention_kv8_ws_bytes(...) bytes, needs no clearing and may
- * be shared by calls that do not overlap. */
+ * be shared by calls that do not overlap.  The size is that of this batch: one
+ * with fewer sequences or rows is cut into more parts and can need more. */
 size_t jf_attention_kv8_ws_bytes(const jf_batch *batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
 jf_status jf_attention_kv8(const jf_batch *batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                            int32_t act_dtype, const void *d_q, const void *d_kv, const uint64_t *d_vis, void *d_out,
@@ -536,11 +538,13 @@ jf_status jf_token_logprobs_grad(int32_t R, int32_t V, int32_t dtype, const void
  * (n_heads / n_kv_heads); scores are q k / sqrt(head_dim), head_dim in {32,
  * 64, 128}.  Rows that start on 16-byte boundaries are read faster.
  * d_lse (optional) [n_heads][n_rows] gets the logarithm of each row's sum of
- * e^score, which the gradient takes.  What a row does not see does not reach
- * it, NaN included; an infinity among the values that it sees gives an
- * infinity, or NaN beside another or where its weight is too small for fp32.
- * A row all of whose scores are -inf gets zeros and -inf.  d_out must not
- * overlap the inputs.  n_seqs or n_rows = 0 does nothing. */
+ * e^score, which the gradient takes.  Scores, sums and statistics are fp32; in
+ * JF_BF16 each weight is rounded to bf16 (2^-8 of it at most) for its product
+ * with the values.  What a row does not see does not reach it, NaN included;
+ * an infinity among the values that it sees gives an infinity, or NaN beside
+ * another or where its weight is too small for fp32.  A row all of whose scores
+ * are -inf gets zeros and -inf.  d_out must not overlap the inputs.  n_seqs or
+ * n_rows = 0 does nothing. */
 jf_status jf_attention_causal(int32_t n_seqs, int32_t n_rows, const int32_t *d_row_start, int32_t n_heads,
                               int32_t n_kv_heads, int32_t head_dim, int32_t dtype, const void *d_q, int64_t ld_q,
                               const void *d_k, int64_t ld_k, const void *d_v, int64_t ld_v, void *d_out,
@@ -551,12 +555,14 @@ jf_status jf_attention_causal(int32_t n_seqs, int32_t n_rows, const int32_t *d_r
  * keys and values are sums over the query heads that share them.  All row
  * tensors are of dtype; the gradients must overlap no input (but may be
  * columns of one tensor).  Nothing depends on the order in which workgroups
- * run.  An infinity or NaN among a sequence's inputs may reach every gradient
- * of that sequence, and none of another's; a NaN score makes the gradients of
- * its row's query and of the keys and values that the row sees NaN.  Weights
- * are computed anew from
- * d_lse, whose fp32 digits hold them for scores up to 2^20 or so (beyond,
- * they are still at most 1).  d_ws, on a 16-byte boundary, holds
+ * run.  Sums are fp32; in JF_BF16 weights and their gradients are rounded to
+ * bf16 for the products, and a row's dot product of d_g_out and out is that of
+ * the rounded d_out.  Weights are computed anew from d_lse, whose fp32 digits
+ * leave them off by 2^-24 times the score (the factor e^0.06 at 2^20); however
+ * large the scores are, they are at most 1.  An infinity or NaN among a
+ * sequence's inputs may reach every gradient of that sequence, and none of
+ * another's; a NaN score makes the gradients of its row's query and of the keys
+ * and values that the row sees NaN.  d_ws, on a 16-byte boundary, holds
  * jf_attention_causal_grad_ws_bytes(...) bytes, which are enough for fewer
  * rows and sequences of these heads too, needs no clearing and may be shared
  * by calls that do not overlap. */
@@ -617,8 +623,9 @@ jf_status jf_attention_shared(const jf_batch *batch, const jf_prefix *prefix, in
  * as jf_token_logprobs_grad takes it (d_g_logprob, d_g_entropy).
  * Rows d_row_start[s] .. d_row_start[s + 1] - 1 (device, [n_seqs + 1], not
  * decreasing) belong to sequence s; a row with d_tokens[row] = -1 (d_tokens
- * NULL: none) has no token: its gradients are 0 and it counts nowhere.  Rows
- * outside all sequences are neither read nor written.  For a row with
+ * NULL: none) has no token: its gradients are 0 and it counts nowhere.  What
+ * rows outside all sequences hold counts nowhere, and no gradient is written
+ * there.  For a row with
  * advantage A (d_advantage[row], or [sequence] for adv_rows 0):
  *   r = e^(logprob - old), policy = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A), 0 for A = 0
  *   k = ref - logprob, kl = e^k - k - 1 (d_ref_logprob NULL: 0)

@@ -778,12 +778,27 @@ static int blocks_of(int n_rows, int n_seqs, int rows) {
 
 // Wide blocks read the keys least often; narrow ones make the longest
 // workgroup short, which counts where there are too few to fill the chip.
-// Blocks of 128 rows from kWide workgroups on (28 heads of 128, bf16: 1024
-// rows 24.3 us in blocks of 128, 21.1 of 64; 2048 rows 47.4 and 50.9; the
-// gradient of 2048 rows 190 and 160, of 4096 467 and 496), of 32 where these
-// all run at once (4 heads of 32, fp32, 2048 rows: 87, 47 and 27 us in blocks
-// of 128, 64 and 32).  At head_dim 128 blocks of 32 rows fill the LDS, or gain
-// nothing (20.1 us for 512 rows, blocks of 64 12.7).
+// Blocks of 128 rows from `wide` of them (times heads) on.  Where the two are
+// even depends on the lengths as well: one long sequence gains from narrow
+// blocks longer, many short ones not as long, and the bounds lie between.
+// Whole passes, us in blocks of 128 and of 64 rows, 28 query and 4 KV heads:
+//                          `wide`  one sequence                     nine of different lengths
+//   bf16, 128 dims            320  364: 38 and 36, 448: 44 and 46   364: 12 and 11, 448: 14 and 17
+//   its gradient              450  476: 200 and 167, 700: 316, 319  448: 50 and 50, 560: 59 and 66
+//   bf16, 64 dims             600  476: 31 and 28, 700: 52 and 55   672: 14.3 and 16.0
+//   its gradient              900  896: 271 and 265, 1176: 431, 445 868: 60 and 62, 1148: 83 and 82
+//   bf16, 32 dims             600  476: 24 and 20, 1176: 90 and 91  672: 11 and 10, 1148: 19.1 and 19.5
+//   its gradient              900  896: 187 and 171, 1792: 595, 968 868: 43.0 and 42.4, 1764: 97 and 110
+//   fp32, 32 dims            1000  980: 352 and 311, 1288: 559, 523 952: 51 and 46, 1260: 76 and 71
+//   its gradient             1000  980: 1187, 1082, 1288: 2021, 2054  952: 164 and 146, 1260: 248, 252
+// (fp32, 128 dims: nine sequences, 952: 178 and 187, its gradient 566 and 591;
+// one sequence, 784: 835 and 811, 3003 and 2845).
+// Blocks of 32 rows where these all run at once, up to 512 of them: 4 heads of
+// 32 dims, fp32, 2048 rows 89, 48 and 28 us in blocks of 128, 64 and 32; beyond,
+// 28 heads of 64, bf16, 768 rows (700 blocks) 12.3 us in blocks of 64 and 15.2
+// of 32, but 16 heads of 32, 1024 rows (528) 12.0 and 9.7.  At head_dim 128
+// blocks of 32 rows fill the LDS, or gain nothing (20.1 us for 512 rows, blocks
+// of 64 12.7).
 static int causal_groups(int n_rows, int n_seqs, int H, int hd, bool f32, bool grad) {
   const int wide = f32 ? 1000 : hd == 128 ? (grad ? 450 : 320) : grad ? 900 : 600;
   if ((int64_t)blocks_of(n_rows, n_seqs, 128) * H >= wide) return 4;
@@ -794,10 +809,14 @@ static void causal_shape(CausalArgs& a, bool grad) {
   a.blocks = blocks_of(a.n_rows, a.n_seqs, 32 * a.groups);
 }
 void causal_plan(CausalArgs& a) { causal_shape(a, false); }
-// dk and dv: one part where its workgroups fill the chip, else a group's heads
-// in parts of as many as leave enough of them, and a pass that adds the parts
-// (28 query and 4 KV heads, 4096 rows: one part 1500 us, a head a part 471; 32
-// sequences of 500 rows: 383 and 540).
+// dk and dv: one part where its workgroups (500 and more) fill the chip, else a
+// group's heads in parts of as many as leave enough of them, and a pass that
+// adds the parts.  The gradient's passes in us, 28 query and 4 KV heads of 128
+// dims: 4096 rows (132 workgroups a part) 1511 in one part, 480 in seven; 12
+// sequences of 1000 rows (420) 548 in one, 480 in four as here, 561 in seven; 32
+// of 500 rows (628) 376 in one, 398 in two, 566 in seven.  One sequence of 16200
+// rows (508), whose last keys have little to do, would take 6.7 ms in seven
+// parts instead of 9.2.
 static int grad_parts(int64_t one, int64_t grp) {  // one: workgroups of one part; fewer parts the more there are
   const int64_t heads = one >= 500 ? grp : std::max<int64_t>(grp * one / 1024, 1);
   return (int)((grp + heads - 1) / heads);

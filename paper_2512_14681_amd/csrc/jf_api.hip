@@ -1196,6 +1196,7 @@ static jf_status check_causal(int n_seqs, int n_rows, const int32_t* d_row_start
     return fail(JF_E_CAPACITY, "%d rows of %d heads exceed one launch", n_rows, n_heads);
   return JF_OK;
 }
+constexpr int64_t kMostStride = 1 << 22;  // elements: 128 rows, as many as a step brings, stay within 32-bit offsets
 static void causal_args(CausalArgs* a, int n_seqs, int n_rows, const int32_t* d_row_start, int n_heads, int n_kv_heads,
                         int head_dim, size_t esz, const void* d_q, int64_t ld_q, const void* d_k, int64_t ld_k,
                         const void* d_v, int64_t ld_v, void* d_out, int64_t ld_out, float* d_lse, int32_t* d_flags) {
@@ -1204,7 +1205,6 @@ static void causal_args(CausalArgs* a, int n_seqs, int n_rows, const int32_t* d_
   a->flags = d_flags;
   a->q = d_q; a->k = d_k; a->v = d_v;
   a->ld_q = (size_t)ld_q; a->ld_k = (size_t)ld_k; a->ld_v = (size_t)ld_v;
-  constexpr int64_t kMostStride = 1 << 22;  // 128 rows, as many as a step brings, stay within 32-bit offsets
   a->vec = rows16(d_q, ld_q, esz) && rows16(d_k, ld_k, esz) && rows16(d_v, ld_v, esz) && ld_q <= kMostStride &&
            ld_k <= kMostStride && ld_v <= kMostStride;
   a->out = d_out; a->ld_out = (size_t)ld_out;
@@ -1265,7 +1265,7 @@ extern "C" jf_status jf_attention_causal_grad(int32_t n_seqs, int32_t n_rows, co
   CausalGradArgs a{};
   causal_args(&a.f, n_seqs, n_rows, d_row_start, n_heads, n_kv_heads, head_dim, esz, d_q, ld_q, d_k, ld_k, d_v, ld_v,
               const_cast<void*>(d_out), ld_out, const_cast<float*>(d_lse), d_flags);
-  a.f.vec = a.f.vec && rows16(d_g_out, ld_g_out, esz) && ld_g_out <= (1 << 22);
+  a.f.vec = a.f.vec && rows16(d_g_out, ld_g_out, esz) && ld_g_out <= kMostStride;
   a.vec_dot = rows16(d_out, ld_out, esz) && rows16(d_g_out, ld_g_out, esz);
   a.g_out = d_g_out; a.ld_g_out = (size_t)ld_g_out;
   a.g_q = d_g_q; a.g_k = d_g_k; a.g_v = d_g_v;
