@@ -64,24 +64,18 @@ __device__ __forceinline__ void mul(f32x16_t& acc, const Frag<bf16_t>& a, const 
 __device__ __forceinline__ void mul(f32x16_t& acc, const Frag<float>& a, const Query<float>& b) { mfma32(acc, a, b.v); }
 
 // What a sequence shares: the first `pages` pages, if its group is what the
-// host announced and its rows are among the group's, which r0 and r1 get (else
-// false, with JF_FLAG_CAPACITY raised).
+// host announced, no group before starts behind it (it then overlaps none,
+// whose work it would do once more) and the sequence's rows are among the
+// group's, r0 .. r1 - 1 (else false, with JF_FLAG_CAPACITY raised).
 __device__ __forceinline__ bool group_ok(const SharedArgs& a, int s0, int s1, int pages, int& r0, int& r1) {
   if (s0 < 0 || s1 < s0 || s1 > a.b.n_seqs || pages < 0 || pages > a.max_pages) return false;
   r0 = a.b.row_start[s0];
   r1 = a.b.row_start[s1];
   return r0 >= 0 && r1 >= r0 && r1 <= a.b.n_rows && r1 - r0 <= a.max_group_rows;
 }
-// Whether no start among the first n is beyond s0, where group n starts: the
-// group then overlaps none before it, whose work it would do once more.
-__device__ __forceinline__ bool group_in_order(const SharedArgs& a, int n, int s0) {
-  bool beyond = false;
-  for (int g = threadIdx.x & 63; g < n; g += 64) beyond |= a.seq_start[g] > s0;
-  return !__any(beyond);
-}
 __device__ __forceinline__ bool shared_pages(const SharedArgs& a, int s, const Seq& q, int& pages) {
   const int lane = threadIdx.x & 63;
-  int top = 0;  // of the starts before
+  int top = 0;  // of the starts looked through before
   pages = 0;
   bool ok = true;
   for (int g0 = 0; g0 < a.n_groups; g0 += 64) {
@@ -95,7 +89,7 @@ __device__ __forceinline__ bool shared_pages(const SharedArgs& a, int s, const S
       pages = a.pages[g0 + l];
       ok = group_ok(a, at, __builtin_amdgcn_readlane(s1, l), pages, r0, r1) && pages <= q.C / kPage && q.r0 >= r0 &&
            q.r0 + q.n <= r1 &&  // row starts within a group may go beyond its ends
-           !(__ballot(s0 > at) & ((1ull << l) - 1)) && !__any(top > at);  // as group_in_order
+           !(__ballot(s0 > at) & ((1ull << l) - 1)) && !__any(top > at);
       break;
     }
     top = max(top, s0);
@@ -341,7 +335,10 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_attention_share
   if (shared) {
     const int s0 = a.seq_start[unit], s1 = a.seq_start[unit + 1], pages = a.pages[unit];
     int r1;
-    if (!group_ok(a, s0, s1, pages, r0, r1) || !group_in_order(a, unit, s0)) {
+    bool behind = false;  // a group before starts behind this one
+#pragma unroll 4
+    for (int i = lane; i < unit; i += 64) behind |= a.seq_start[i] > s0;
+    if (!group_ok(a, s0, s1, pages, r0, r1) || __any(behind)) {
       if (a.b.flags && threadIdx.x == 0) atomicOr(a.b.flags, kFlagCapacity);
       return;
     }
