@@ -205,9 +205,9 @@ template <int ND> __device__ __forceinline__ void add_shared(const float* at, fl
 
 // Outputs, in one pass over the keys.  Bound by the matrix and vector
 // instructions, which two waves a SIMD overlap in part: 8192 rows of 7b heads
-// (481 GFLOP) take 465 us, 1035 TFLOP/s; the matrix cores are busy in about 60%
+// (481 GFLOP) take 462 us, 1040 TFLOP/s; the matrix cores are busy in about 60%
 // of the cycles, at 1.8 GHz (the chip's power sets the clock), and no LDS access
-// waits for a bank.  2048 rows take 49 us: 448 workgroups on 512 places, of
+// waits for a bank.  2048 rows take 50 us: 448 workgroups on 512 places, of
 // which the longest has 32 steps.  A wave holds its 32 queries (32 registers),
 // 64 x 32 scores and weights (64) and 32 outputs of 128 dims (64); the keys'
 // and values' next step comes to LDS meanwhile.  Not kept: scores of the next
@@ -417,8 +417,8 @@ __device__ __forceinline__ float weight(float x) { return __builtin_amdgcn_fmed3
 // weights, whose weights then are 0), and -D.  sum_j ds_ij is 0 but for what the
 // rounded outputs lack in D, and is added to it for dk.
 // Three products a pair where the forward pass has two: 4096 rows of 7b heads
-// (180 GFLOP) take 198 us, 910 TFLOP/s, bound as the forward pass is (which
-// takes 140 us there).  Of these the sum of ds takes 1% of a forward and
+// (180 GFLOP) take 192 us, 940 TFLOP/s, bound as the forward pass is (which
+// takes 136 us there).  Of these the sum of ds takes 1% of a forward and
 // backward pass (in four sums; in one 1.5%, and 4% for heads of 64), and
 // the gradients' error falls from 0.0025 to 0.0024.
 template <typename T, int HD, int NQ, bool kVec>
@@ -550,8 +550,8 @@ __global__ void __launch_bounds__(256, kResident<T>) k_causal_dq(CausalGradArgs 
 
 // dk and dv of a block of keys of a KV head, over the queries of the heads of
 // `part` (part, part + parts, ... of the group's).
-// Four products a pair: 4096 rows of 7b heads (241 GFLOP) take 266 to 287 us,
-// 840 to 905 TFLOP/s.  The 128 registers of dk and dv beside 64 of keys and values leave
+// Four products a pair: 4096 rows of 7b heads (241 GFLOP) take 260 to 287 us,
+// 840 to 930 TFLOP/s.  The 128 registers of dk and dv beside 64 of keys and values leave
 // room for one tile of scores at a time, so that the matrix cores wait for the
 // weights more often than in the forward pass.
 template <typename T, int HD, int NQ, bool kVec>
