@@ -399,8 +399,8 @@ jf_status jf_trajectory_select(const int32_t *d_traj, const int32_t *d_len,
  * rows; at most 64 table_stride).  What the device holds beyond these bounds
  * is not followed: such a sequence's rows are left as they were and
  * JF_FLAG_CAPACITY is raised (starts that decrease can leave sequences that fit
- * over each other: rows that two of them hold get the results of either); a
- * page table entry outside [0, n_pages) raises JF_FLAG_BAD_PAGE and its tokens
+ * over each other: rows that two of them hold get values of no meaning); a page
+ * table entry outside [0, n_pages) raises JF_FLAG_BAD_PAGE and its tokens
  * are skipped.  d_flags (optional, one int32) gets these bits ORed in; the
  * caller clears it.  n_seqs, n_rows or max_rows = 0 does nothing; n_pages = 0
  * otherwise is JF_E_CAPACITY.  n_seqs times the workgroups that max_rows and
@@ -531,7 +531,7 @@ jf_status jf_token_logprobs_grad(int32_t R, int32_t V, int32_t dtype, const void
  * d_flags (optional, one int32, ORed; the caller clears it).  Of those that
  * remain, one that starts before an earlier one's end is left as it was too,
  * among up to 64 sequences; among more, others may be left as they were, and
- * rows that several hold get the results of any of them.
+ * rows that several hold get values of no meaning.
  * d_q, d_out [n_rows][n_heads * head_dim], d_k, d_v [n_rows][n_kv_heads *
  * head_dim] are rows of dtype (JF_F32 or JF_BF16), ld_* elements apart (views
  * into one fused projection, for instance); query head j reads KV head j /
